@@ -562,6 +562,40 @@ int twn_avgpool_bwd(const void *dY, int64_t B, int64_t HW, int64_t C, void *dX, 
 int twn_act_bwd(const void *dY, const void *Y, const float *scale, int64_t n, int64_t C, void *dZ,
                 void *dPre, twn_stream_t stream);
 
+/*
+ * Layer norm over the channels of a row (a token, or a pixel of an NHWC tensor):
+ *   mean = sum_c x / C,  var = sum_c (x - mean)^2 / C,  rstd = 1 / sqrt(var + eps)
+ *   Y[m,c] = (X[m,c] - mean) * rstd * gamma[c] + beta[c]
+ *   X      TWN_F32 or TWN_BF16 (x_dtype) [M, ldx], ldx >= C;  Y likewise (y_dtype, ldy); both aligned to their
+ *          element.  Y may be X itself (same type and pitch).  Columns C.. of Y's rows are not touched.
+ *   gamma, beta   fp32 [C] or NULL (1, 0);  mean, rstd  fp32 [M] outputs for the backward pass, or NULL.
+ *   1 <= C <= 2^31, eps >= 0.  M = 0 is fine and launches nothing.
+ * Arithmetic is fp32, the variance that of the differences from the mean, each output rounded once.  A row with a NaN
+ * or an infinity gives NaNs in that row alone.  With eps = 0 a row of equal values gives NaNs (0 * inf).
+ * Deterministic, and a row has the same bits in every batch.  Rows and bases on 16-byte boundaries, C % 8 == 0 and
+ * 16-byte aligned gamma and beta take the fast path.
+ */
+int twn_layer_norm_fwd(const void *X, int32_t x_dtype, int64_t ldx, int64_t M, int64_t C, const float *gamma,
+                       const float *beta, double eps, void *Y, int32_t y_dtype, int64_t ldy, float *mean, float *rstd,
+                       twn_stream_t stream);
+
+/*
+ * Its backward pass.  With xh = (X - mean) * rstd and g = dY * gamma:
+ *   dX[m,c]   = rstd * (g - sum_c g / C - xh * sum_c (g * xh) / C)
+ *   dgamma[c] = sum_m dY[m,c] * xh[m,c],   dbeta[c] = sum_m dY[m,c]
+ *   dY, X, dX  each TWN_F32 or TWN_BF16 with its own pitch, as above; dX may be dY or X itself (same type and pitch).
+ *   gamma      fp32 [C] or NULL (1);  mean, rstd  fp32 [M], what twn_layer_norm_fwd wrote.
+ *   dX, dgamma, dbeta (fp32 [C]) are overwritten; each may be NULL.  M = 0 gives zero gradients.
+ *   workspace  at least twn_layer_norm_bwd_workspace_bytes(M, C) bytes, 256-byte aligned; contents need not be
+ *              preserved or initialised.  Two calls that overlap on the device must not share it.
+ * The sums over the rows are fp32, split by M and C and added in a fixed order (deterministic).
+ */
+size_t twn_layer_norm_bwd_workspace_bytes(int64_t M, int64_t C);
+int twn_layer_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy, const void *X, int32_t x_dtype, int64_t ldx,
+                       int64_t M, int64_t C, const float *gamma, const float *mean, const float *rstd, void *dX,
+                       int32_t dx_dtype, int64_t lddx, float *dgamma, float *dbeta, void *workspace,
+                       size_t workspace_bytes, twn_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -139,6 +139,100 @@ template <auto Fn> PyObject *entry(PyObject *, PyObject *const *v, Py_ssize_t n)
     }
 }
 
+// ---- calls on tensors of either type: the type is the tensor's, and what a call reads and writes lies inside its tensors ----
+struct Typed {
+    void *p;
+    int32_t dtype;
+    size_t elements;
+};
+
+[[noreturn]] void assertion(const char *what)
+{
+    PyErr_SetString(PyExc_AssertionError, what);
+    throw PyError{};
+}
+
+Typed typed_tensor(Args &a)
+{
+    PyObject *o = a.take();
+    if (o == Py_None) return {nullptr, TWN_F32, 0};
+    size_t bytes;
+    void *p = tensor_ptr(o, &bytes);
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (t.device().index() != c10::cuda::current_device()) assertion("a tensor is on another device than the current one");
+    if (t.scalar_type() == at::kFloat) return {p, TWN_F32, bytes / 4};
+    if (t.scalar_type() == at::kBFloat16) return {p, TWN_BF16, bytes / 2};
+    type_error("expected a tensor of fp32 or bf16");
+}
+// M rows of C elements, ld apart.  (Sizes that the library refuses are left to it.)
+void has_rows(const Typed &t, int64_t ld, int64_t M, int64_t C)
+{
+    if (t.p && M > 0 && ld >= C && C > 0 && (__int128)(M - 1) * ld + C > (__int128)t.elements) assertion("a tensor has fewer elements than its rows");
+}
+float *float_vector(Args &a, int64_t n)
+{
+    const Typed t = typed_tensor(a);
+    if (t.p && t.dtype != TWN_F32) type_error("expected a tensor of fp32");
+    if (t.p && n > 0 && (size_t)n > t.elements) assertion("a vector has too few elements");
+    return static_cast<float *>(t.p);
+}
+void no_more(const Args &a)
+{
+    if (a.next != a.n) type_error("too many arguments");
+}
+
+// (X, ldx, M, C, gamma, beta, eps, Y, ldy, mean, rstd, stream)
+PyObject *layer_norm_fwd(Args &a)
+{
+    const Typed X = typed_tensor(a);
+    const int64_t ldx = integer_of(a.take()), M = integer_of(a.take()), C = integer_of(a.take());
+    has_rows(X, ldx, M, C);
+    float *const gamma = float_vector(a, C), *const beta = float_vector(a, C);
+    const double eps = real_of(a.take());
+    const Typed Y = typed_tensor(a);
+    const int64_t ldy = integer_of(a.take());
+    has_rows(Y, ldy, M, C);
+    float *const mean = float_vector(a, M), *const rstd = float_vector(a, M);
+    const twn_stream_t stream = get<twn_stream_t>(a);
+    no_more(a);
+    return finish(twn_layer_norm_fwd, std::make_tuple(X.p, X.dtype, ldx, M, C, gamma, beta, eps, Y.p, Y.dtype, ldy, mean, rstd, stream));
+}
+
+// (dY, lddy, X, ldx, M, C, gamma, mean, rstd, dX, lddx, dgamma, dbeta, workspace, stream)
+PyObject *layer_norm_bwd(Args &a)
+{
+    const Typed dY = typed_tensor(a);
+    const int64_t lddy = integer_of(a.take());
+    const Typed X = typed_tensor(a);
+    const int64_t ldx = integer_of(a.take()), M = integer_of(a.take()), C = integer_of(a.take());
+    has_rows(dY, lddy, M, C);
+    has_rows(X, ldx, M, C);
+    float *const gamma = float_vector(a, C), *const mean = float_vector(a, M), *const rstd = float_vector(a, M);
+    const Typed dX = typed_tensor(a);
+    const int64_t lddx = integer_of(a.take());
+    has_rows(dX, lddx, M, C);
+    float *const dgamma = float_vector(a, C), *const dbeta = float_vector(a, C);
+    void *const ws = get<void *>(a);
+    const size_t ws_bytes = a.last_bytes;
+    const twn_stream_t stream = get<twn_stream_t>(a);
+    no_more(a);
+    return finish(twn_layer_norm_bwd, std::make_tuple(dY.p, dY.dtype, lddy, X.p, X.dtype, ldx, M, C, gamma, mean, rstd, dX.p, dX.dtype, lddx,
+                                                      dgamma, dbeta, ws, ws_bytes, stream));
+}
+
+template <PyObject *(*F)(Args &)> PyObject *entry_typed(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    try {
+        Args a{v, n, 0, 0};
+        return F(a);
+    } catch (const PyError &) {
+        return nullptr;
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
 // ---- batched calls: a list of tuples, one per tensor ----------------------------------------
 template <typename Item> void read_item(Args &a, Item *it);
 template <> void read_item(Args &a, twn_ternarize_item_t *it)       // (W, rows, cols, stats, packed, ld_codes, codes_i8)
@@ -210,6 +304,7 @@ template <auto Fn> PyObject *entry_batch(PyObject *, PyObject *const *v, Py_ssiz
 }
 
 #define TWN_ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<twn_##name>)), METH_FASTCALL, nullptr}
+#define TWN_TYPED(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry_typed<name>)), METH_FASTCALL, nullptr}
 #define TWN_BATCH(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry_batch<twn_##name>)), METH_FASTCALL, nullptr}
 
 PyMethodDef methods[] = {
@@ -221,6 +316,7 @@ PyMethodDef methods[] = {
     TWN_ENTRY(conv2d_bwd_data_b1),
     TWN_ENTRY(im2col), TWN_ENTRY(fold_input), TWN_ENTRY(fold_codes), TWN_ENTRY(maxpool2d_fwd), TWN_ENTRY(maxpool2d_bwd),
     TWN_ENTRY(maxpool2d_bwd_act), TWN_ENTRY(avgpool_fwd), TWN_ENTRY(avgpool_bwd), TWN_ENTRY(act_bwd),
+    TWN_TYPED(layer_norm_fwd), TWN_TYPED(layer_norm_bwd),
     TWN_BATCH(ternarize_batch), TWN_BATCH(ternarize_codes_batch), TWN_BATCH(sgd_update_batch), TWN_BATCH(transpose_codes_batch),
     {nullptr, nullptr, 0, nullptr}};
 

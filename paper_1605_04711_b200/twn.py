@@ -83,6 +83,7 @@ def lib() -> C.CDLL:
         l.twn_conv2d_bwd_weight_folded_workspace_bytes.restype = C.c_size_t
         l.twn_binarize_workspace_bytes.restype = C.c_size_t
         l.twn_conv2d_fwd_bn_workspace_bytes.restype = C.c_size_t
+        l.twn_layer_norm_bwd_workspace_bytes.restype = C.c_size_t
         _lib = l
     return _lib
 
@@ -402,6 +403,21 @@ def avgpool_bwd(dY, B, HW, Cc, dX, stream=None) -> None:
 
 def act_bwd(dY, Y, scale, n, Cc, dZ, dPre=None, stream=None) -> None:
     _check(_C.act_bwd(dY, Y, scale, n, Cc, dZ, dPre, stream), "twn_act_bwd")
+
+
+def layer_norm_fwd(X, ldx, M, Cc, gamma, beta, eps, Y, ldy, mean=None, rstd=None, stream=None) -> None:
+    """twn_layer_norm_fwd.  X and Y are fp32 or bf16, the type that each tensor has."""
+    _check(_C.layer_norm_fwd(X, ldx, M, Cc, gamma, beta, eps, Y, ldy, mean, rstd, stream), "twn_layer_norm_fwd")
+
+
+def layer_norm_bwd_workspace_bytes(M: int, Cc: int) -> int:
+    return int(lib().twn_layer_norm_bwd_workspace_bytes(C.c_int64(M), C.c_int64(Cc)))
+
+
+def layer_norm_bwd(dY, lddy, X, ldx, M, Cc, gamma, mean, rstd, dX, lddx, dgamma, dbeta, workspace, stream=None) -> None:
+    """twn_layer_norm_bwd.  dY, X and dX are fp32 or bf16, the type that each tensor has; dX, dgamma and dbeta may be None."""
+    _check(_C.layer_norm_bwd(dY, lddy, X, ldx, M, Cc, gamma, mean, rstd, dX, lddx, dgamma, dbeta, workspace, stream),
+           "twn_layer_norm_bwd")
 
 
 def conv2d_bwd_weight_workspace_bytes(desc: ConvDesc) -> int:
