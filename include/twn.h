@@ -254,6 +254,59 @@ int twn_ternarize_codes_batch(const twn_ternarize_item_t *items, int count, void
                               size_t workspace_bytes, twn_stream_t stream);
 
 /*
+ * Orthogonalised updates.  An update matrix G (a momentum of gradients) is replaced by a matrix with the same singular vectors
+ * and singular values near 1, by Newton-Schulz steps: with X the transpose of G / max(|G|_F, eps) where G has more rows than
+ * columns, else G / max(|G|_F, eps) itself,
+ *   X <- a X + (b A + c A^2) X,  A = X X^T,   (a, b, c) = (3.4445, -4.7750, 2.0315), `steps` times;  O = X (or its transpose).
+ * The coefficients are those of the Muon optimiser: five steps bring singular values from 2e-3 of |G|_F to 1 into 0.68 .. 1.21;
+ * smaller ones grow by a factor of a a step.  A matrix of zeros gives zeros.
+ *   items      HOST array of up to 32 matrices, read during the call only; their tiles share the launches.
+ *     G        TWN_F32 or TWN_BF16 [rows, cols], contiguous;  O likewise, its own type; both aligned to their element.
+ *              O may be G (same type).  An empty matrix is skipped.  min(rows, cols) <= 32768, max <= 2^24.
+ *   steps      1 .. 32;  eps  1e-30 .. 1e30 (1e-7 is usual).
+ *   workspace  at least twn_orthogonalize_workspace_bytes(items, count) bytes (only rows and cols are read; 0 for shapes that
+ *              the call refuses), 256-byte aligned; contents need not be preserved or initialised.  Two calls that overlap on
+ *              the device must not share it.
+ *   dev_status optional device int32, zero before the call: TWN_ERR_NONFINITE where a G holds a NaN or an infinity (its O is
+ *              then NaNs, the other matrices are unaffected), TWN_ERR_TIMEOUT as in twn_gemm.
+ * fp16 products, fp32 sums; X is carried in 22 bits and the diagonals of A and of b A + c A^2 in fp32, so five steps are within
+ * 1e-3 (2-norm, relative) of 64-bit arithmetic for matrices of independent elements, and within 4e-3 for low rank (one included)
+ * and for singular values that fall off.  Where blocks of equal elements make the roundings of the products align it can be
+ * more (up to 1e-2 seen in 150 such matrices, 1.3e-3 in the middle).  Deterministic, and a matrix has the same bits alone and in a batch.
+ */
+typedef struct {
+    const void *G;
+    void *O;
+    int64_t rows, cols;
+    int32_t g_dtype, o_dtype;
+} twn_orthogonalize_item_t;
+size_t twn_orthogonalize_workspace_bytes(const twn_orthogonalize_item_t *items, int count);
+int twn_orthogonalize_batch(const twn_orthogonalize_item_t *items, int count, int steps, double eps,
+                            void *workspace, size_t workspace_bytes, int32_t *dev_status, twn_stream_t stream);
+
+/*
+ * Parameter update with orthogonalised momentum (the Muon rule) on the fp32 master weights, in place, beside
+ * twn_sgd_update_batch.  For every matrix, a layer's filters as rows:
+ *   V = momentum * V + dW;   U = dW + momentum * V (look_ahead = 1) or V (0);   O = the orthogonalised U, as above;
+ *   W = W - lr * (s * O + weight_decay * W),   s = sqrt(max(1, rows / cols))
+ * V and U are separately rounded fp32 operations, defined to the bit, and so is W as a function of O (which is fp32).
+ *   W, dW, V   fp32 [rows, cols], 16-byte aligned;  stats_next as in twn_sgd_update (optional): sum_abs, delta and status
+ *              of the updated weights, for twn_ternarize_codes.
+ *   look_ahead 0 or 1; steps, eps, dev_status as above; workspace at least twn_muon_workspace_bytes(items, count).
+ */
+typedef struct {
+    float *W;
+    const float *dW;
+    float *V;
+    int64_t rows, cols;
+    twn_stats_t *stats_next;   /* optional */
+} twn_muon_item_t;
+size_t twn_muon_workspace_bytes(const twn_muon_item_t *items, int count);
+int twn_muon_update_batch(const twn_muon_item_t *items, int count, float lr, float momentum, float weight_decay,
+                          int look_ahead, int steps, double eps, double delta_factor, void *workspace,
+                          size_t workspace_bytes, int32_t *dev_status, twn_stream_t stream);
+
+/*
  * Per-filter threshold ternarization fused with 2-bit packing: Algorithm 1 as printed,
  * whose first loop runs over the filters of a layer.  Row r of W is one filter and gets
  *   delta_r = delta_factor * (1/cols) * sum_i |W_r,i|          (Sec. 2.3, n = cols)

@@ -267,6 +267,36 @@ template <> void read_item(Args &a, twn_transpose_item_t *it)       // (packed_f
     it->ld_bwd = get<int64_t>(a);
 }
 
+// R rows of C elements without gaps.
+void has_matrix(const Typed &t, int64_t rows, int64_t cols) { has_rows(t, cols, rows, cols); }
+
+template <> void read_item(Args &a, twn_orthogonalize_item_t *it)   // (G, rows, cols, O)
+{
+    const Typed G = typed_tensor(a);
+    it->rows = get<int64_t>(a);
+    it->cols = get<int64_t>(a);
+    const Typed O = typed_tensor(a);
+    has_matrix(G, it->rows, it->cols);
+    has_matrix(O, it->rows, it->cols);
+    it->G = G.p; it->g_dtype = G.dtype;
+    it->O = O.p; it->o_dtype = O.dtype;
+}
+template <> void read_item(Args &a, twn_muon_item_t *it)            // (W, dW, V, rows, cols, stats_next)
+{
+    Typed t[3];
+    for (Typed &x : t) {
+        x = typed_tensor(a);
+        if (x.p && x.dtype != TWN_F32) type_error("expected a tensor of fp32");
+    }
+    it->rows = get<int64_t>(a);
+    it->cols = get<int64_t>(a);
+    for (const Typed &x : t) has_matrix(x, it->rows, it->cols);
+    it->W = static_cast<float *>(t[0].p);
+    it->dW = static_cast<const float *>(t[1].p);
+    it->V = static_cast<float *>(t[2].p);
+    it->stats_next = get<twn_stats_t *>(a);
+}
+
 template <typename Item, typename... A> PyObject *invoke_batch(int (*fn)(const Item *, int, A...), Args &a)
 {
     PyObject *seq = PySequence_Fast(a.take(), "expected a list of tuples");
@@ -318,6 +348,7 @@ PyMethodDef methods[] = {
     TWN_ENTRY(maxpool2d_bwd_act), TWN_ENTRY(avgpool_fwd), TWN_ENTRY(avgpool_bwd), TWN_ENTRY(act_bwd),
     TWN_TYPED(layer_norm_fwd), TWN_TYPED(layer_norm_bwd),
     TWN_BATCH(ternarize_batch), TWN_BATCH(ternarize_codes_batch), TWN_BATCH(sgd_update_batch), TWN_BATCH(transpose_codes_batch),
+    TWN_BATCH(orthogonalize_batch), TWN_BATCH(muon_update_batch),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_twn", "Entry points of libtwn.so.", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -59,6 +59,14 @@ def conv_desc(B, H, W, Cin, Cout, k, stride=1, pad=0) -> ConvDesc:
     return ConvDesc(B, H, W, Cin, Cout, kh, kw, stride, stride, pad, pad)
 
 
+class _OrthogonalizeItem(C.Structure):
+    _fields_ = [("G", C.c_void_p), ("O", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("g_dtype", C.c_int32), ("o_dtype", C.c_int32)]
+
+
+class _MuonItem(C.Structure):
+    _fields_ = [("W", C.c_void_p), ("dW", C.c_void_p), ("V", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("stats_next", C.c_void_p)]
+
+
 class Epilogue(C.Structure):
     _fields_ = [("scale", C.c_void_p), ("shift", C.c_void_p), ("residual", C.c_void_p),
                 ("residual_dtype", C.c_int32), ("relu", C.c_int32), ("out_dtype", C.c_int32),
@@ -84,6 +92,8 @@ def lib() -> C.CDLL:
         l.twn_binarize_workspace_bytes.restype = C.c_size_t
         l.twn_conv2d_fwd_bn_workspace_bytes.restype = C.c_size_t
         l.twn_layer_norm_bwd_workspace_bytes.restype = C.c_size_t
+        l.twn_orthogonalize_workspace_bytes.restype = C.c_size_t
+        l.twn_muon_workspace_bytes.restype = C.c_size_t
         _lib = l
     return _lib
 
@@ -187,6 +197,32 @@ def ternarize_codes_batch(items, workspace: torch.Tensor, stream=None) -> None:
 def transpose_codes_batch(items, stream=None) -> None:
     """twn_transpose_codes_batch.  items: list of (packed_fwd, ld_fwd, desc, packed_bwd, ld_bwd)."""
     _check(_C.transpose_codes_batch(items, stream), "twn_transpose_codes_batch")
+
+
+def _shapes(item_type, shapes):
+    return (item_type * max(1, len(shapes)))(*[item_type(rows=r, cols=c) for r, c in shapes]), C.c_int(len(shapes))
+
+
+def orthogonalize_workspace_bytes(shapes) -> int:
+    """Scratch of orthogonalize_batch for matrices of these (rows, cols); 0 where it refuses them."""
+    return int(lib().twn_orthogonalize_workspace_bytes(*_shapes(_OrthogonalizeItem, shapes)))
+
+
+def orthogonalize_batch(items, steps: int, eps: float, workspace: torch.Tensor, dev_status=None, stream=None) -> None:
+    """twn_orthogonalize_batch.  items: list of (G, rows, cols, O); G and O are fp32 or bf16, the type that each tensor has."""
+    _check(_C.orthogonalize_batch(items, steps, eps, workspace, dev_status, stream), "twn_orthogonalize_batch")
+
+
+def muon_workspace_bytes(shapes) -> int:
+    """Scratch of muon_update_batch for matrices of these (rows, cols); 0 where it refuses them."""
+    return int(lib().twn_muon_workspace_bytes(*_shapes(_MuonItem, shapes)))
+
+
+def muon_update_batch(items, lr: float, momentum: float, weight_decay: float, look_ahead: bool, steps: int, eps: float,
+                      delta_factor: float, workspace: torch.Tensor, dev_status=None, stream=None) -> None:
+    """twn_muon_update_batch.  items: list of (W, dW, V, rows, cols, stats_next or None)."""
+    _check(_C.muon_update_batch(items, lr, momentum, weight_decay, look_ahead, steps, eps, delta_factor, workspace, dev_status, stream),
+           "twn_muon_update_batch")
 
 
 def ternarize_rows(W: torch.Tensor, delta_factor: float, stats: torch.Tensor, packed: torch.Tensor,
