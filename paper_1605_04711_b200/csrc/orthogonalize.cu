@@ -18,22 +18,29 @@
 //
 // Layout.  X, A and B live in the workspace as blocks of 64x64 fp16 (8 KB), in the 128-byte swizzle that the tensor core
 // wants, the row blocks of a column block one after the other.  A tile of 128 rows by 64 columns is then 16 KB in a row, one
-// bulk copy, K-major; and the same blocks serve as the MN-major operand of B X, whose reduction runs over the rows of X.
-// No tensor maps, and the blocks are padded with zeros, so ragged sizes need no special code.
+// copy, K-major; and the same blocks serve as the MN-major operand of B X, whose reduction runs over the rows of X.
+// The blocks are padded with zeros, so ragged sizes need no special code.
 //
 // A and B are symmetric: only tiles on or below the diagonal are computed, and written twice.
 //
-// One launch per product, for up to 32 matrices at once (their tiles in one list):
-//   warp 0     bulk copies into a ring of four 48 KB stages       warp 1   one MMA-issuing thread, 128x256 tiles
-//   warps 2-9  epilogue, two per tensor-memory lane quadrant; two accumulators, so it runs beside the next tile
+// One launch per product, for up to 32 matrices at once (their tiles in one list), in one of two kernels:
+//   ns_pair_kernel   256x256 tiles, each by a pair of blocks (cta_group::2), persistent: large products.  What bounds it is the
+//                    feed from L2, about 57 bytes a cycle and SM: a single block's 128x256 tile needs 94 at the rate
+//                    of the tensor core and took 850 cycles for a reduction of 64, a pair needs 64.
+//   ns_tile_kernel   a 128x128 tile a block, two blocks on an SM: small products; the reduction of a symmetric
+//                    one may be split over up to eight blocks of a cluster, whose sums meet through distributed shared memory.
+// The epilogues are the same: a warp has 32 rows by 64 columns in shared memory in fp32, walks them four rows at a time, so
+// that what it reads and writes in the blocks is 512 bytes in a row, and writes the mirror image from the transposed reads.
 #include <algorithm>
 #include <cmath>
 #include <cstddef>
+#include <cstring>
 
 #include <cuda_fp16.h>
 
 #include "common.cuh"
 #include "tc_ptx.cuh"
+#include "tconv_host.cuh"
 
 namespace {
 
@@ -41,12 +48,13 @@ constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kStart = 256.0f;             // X of the first step is this much larger
 constexpr int kMaxItems = 32;
 constexpr int kBlockBytes = 8192, kBlockHalves = kBlockBytes / 2;
-constexpr int kStages = 4, kABytes = 2 * kBlockBytes, kBBytes = 4 * kBlockBytes, kStageBytes = kABytes + kBBytes;
-constexpr int kAccCols = 256;
-constexpr int kEpiWarps = 8;
+constexpr int kOpBytes = 2 * kBlockBytes, kStageBytes = 2 * kOpBytes;     // 128 rows (or columns) of each operand by 64
+constexpr int kPairStages = 5, kTileStages = 3;
+constexpr int kEpiWarps = 8, kWarpTile = 32 * 64;
 constexpr int kNsThreads = 32 * (2 + kEpiWarps);
-constexpr int kMaxParts = 148;               // of a matrix's sum of squares
-constexpr long long kPartElements = 16384;
+constexpr int kMaxSplit = 8;                 // blocks of a cluster
+constexpr int kMaxParts = 512;               // of a matrix's sum of squares
+constexpr long long kPartElements = 8192;
 constexpr int kSweepBlock = 256;
 
 enum { kGram = 0, kSquare = 1, kApply = 2 };
@@ -58,13 +66,15 @@ struct NsItem {
     void *O;
     uint16_t *x[2], *lo, *A, *B; // blocks
     float *alpha, *beta;         // diagonals
-    float *squares;              // [2 cb][64 rb]: sums of squares of 32 elements of a row of X
+    float *squares;              // [cb][64 rb]: sums of squares of 64 elements of a row of X
     double *part;                // sums of squares
     long long count;             // elements
-    int m, n, rb, cb;            // shorter and longer side; row blocks of X (even) and column blocks
-    int parts, part_first, block_first, sym_first, apply_first;
+    int m, n, rb, cb;            // shorter and longer side; row and column blocks of X
+    int parts;
+    int first;                   // its first unit in the list of the launch
+    int split;                   // blocks that share a reduction of the launch
     float out_scale;
-    uint8_t g_bf16, o_bf16, tall;
+    uint8_t g_bf16, o_bf16, tall, vec_in, vec_out, sym_pair, apply_pair;
 };
 
 struct NsParams {
@@ -73,17 +83,13 @@ struct NsParams {
     float momentum, eps;
     int look_ahead;
     int32_t *status;
+    const uint16_t *base;        // of the blocks: rows of the tensor maps count from here
 };
 
-enum { kPartList, kBlockList, kSymList, kApplyList };
-template <int LIST> __device__ __forceinline__ int first_of(const NsItem &it)
-{
-    return LIST == kPartList ? it.part_first : LIST == kBlockList ? it.block_first : LIST == kSymList ? it.sym_first : it.apply_first;
-}
-template <int LIST> __device__ __forceinline__ int item_of(const NsParams &P, int unit)
+__device__ __forceinline__ int item_of(const NsParams &P, int unit)
 {
     int t = 0;
-    while (t + 1 < P.count && unit >= first_of<LIST>(P.item[t + 1])) ++t;
+    while (t + 1 < P.count && unit >= P.item[t + 1].first) ++t;
     return t;
 }
 
@@ -91,6 +97,8 @@ template <int LIST> __device__ __forceinline__ int item_of(const NsParams &P, in
 __device__ __forceinline__ size_t block_at(int R, int C, int rb) { return ((size_t)C * rb + R) * kBlockHalves; }
 // Element (r, c) of a block: rows of 128 bytes, their 16-byte pieces exchanged by the row's number modulo 8.
 __device__ __forceinline__ int in_block(int r, int c) { return r * 64 + ((((c >> 3) ^ r) & 7) << 3) + (c & 7); }
+// Eight elements of row r of the whole matrix from column c on (a multiple of 8).
+__device__ __forceinline__ size_t piece_at(int r, int c, int rb) { return block_at(r >> 6, c >> 6, rb) + in_block(r & 63, c & 63); }
 
 __device__ __forceinline__ float muon_update(const NsParams &P, float v, float d)
 {
@@ -114,19 +122,60 @@ __device__ __forceinline__ double block_sum(double s, double *red)
     return s;
 }
 
+// Eight elements from i on, a multiple of 8 in an aligned tensor; for Muon's first sweep with the momentum updated.
+template <bool UPDATE> __device__ __forceinline__ void elements8(const NsItem &it, const NsParams &P, long long i, float (&g)[8])
+{
+    if (it.V) {
+        float4 *v4 = reinterpret_cast<float4 *>(it.V + i);
+        const float4 *d4 = reinterpret_cast<const float4 *>(it.dW + i);
+        float4 v[2] = {v4[0], v4[1]};
+        const float4 d[2] = {d4[0], d4[1]};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float *const vp = &v[h].x;
+            const float *const dp = &d[h].x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (UPDATE) vp[j] = __fadd_rn(__fmul_rn(P.momentum, vp[j]), dp[j]);
+                g[4 * h + j] = muon_update(P, vp[j], dp[j]);
+            }
+            if (UPDATE) v4[h] = v[h];
+        }
+    } else if (it.g_bf16) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(it.G) + i);
+        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { g[2 * j] = __uint_as_float(ws[j] << 16); g[2 * j + 1] = __uint_as_float(ws[j] & 0xFFFF0000u); }
+    } else {
+        const float4 *g4 = reinterpret_cast<const float4 *>(static_cast<const float *>(it.G) + i);
+        const float4 a = g4[0], b = g4[1];
+        g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w; g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
+    }
+}
+
 // Sum of squares of every matrix, in fp64 and in a fixed order; for Muon the momentum is updated on the way.
 __global__ void __launch_bounds__(kSweepBlock) ns_norm_kernel(const __grid_constant__ NsParams P)
 {
     __shared__ double red[kSweepBlock / 32];
     pdl_begin();
     for (int u = blockIdx.x; u < P.units; u += gridDim.x) {
-        const NsItem &it = P.item[item_of<kPartList>(P, u)];
-        const int part = u - it.part_first;
-        const long long per = ((it.count + it.parts - 1) / it.parts + 1023) / 1024 * 1024;
-        const long long end = min(it.count, (part + 1) * per);
-        double s = 0.0;
-#pragma unroll 4
-        for (long long i = part * per + threadIdx.x; i < end; i += kSweepBlock) {
+        const NsItem &it = P.item[item_of(P, u)];
+        const int part = u - it.first;
+        const long long per = ((it.count + it.parts - 1) / it.parts + 2047) / 2048 * 2048;
+        const long long begin = min(it.count, part * per), end = min(it.count, begin + per);
+        const long long whole = it.vec_in ? begin + (end - begin) / 8 * 8 : begin;
+        double s0 = 0.0, s1 = 0.0;
+#pragma unroll 2
+        for (long long i = begin + 8 * threadIdx.x; i < whole; i += 8 * kSweepBlock) {
+            float g[8];
+            elements8<true>(it, P, i, g);
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                s0 += (double)g[j] * (double)g[j];
+                s1 += (double)g[j + 1] * (double)g[j + 1];
+            }
+        }
+        for (long long i = whole + threadIdx.x; i < end; i += kSweepBlock) {
             double g;
             if (it.V) {
                 const float d = it.dW[i], v = __fadd_rn(__fmul_rn(P.momentum, it.V[i]), d);
@@ -135,11 +184,50 @@ __global__ void __launch_bounds__(kSweepBlock) ns_norm_kernel(const __grid_const
             } else {
                 g = element(it, P, i);
             }
-            s += g * g;
+            s0 += g * g;
         }
-        s = block_sum(s, red);
+        const double s = block_sum(s0 + s1, red);
         if (threadIdx.x == 0) it.part[part] = s;
     }
+}
+
+// Eight values as two fp16 numbers each: the upper halves in one 16-byte piece, what they leave in another.
+__device__ __forceinline__ uint32_t half2_bits(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ float2 half2_of(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+__device__ __forceinline__ uint4 pack_half8(const float (&f)[8])
+{
+    return make_uint4(half2_bits(f[0], f[1]), half2_bits(f[2], f[3]), half2_bits(f[4], f[5]), half2_bits(f[6], f[7]));
+}
+__device__ __forceinline__ void unpack_half8(const uint4 &w, float (&f)[8])
+{
+    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 v = half2_of(ws[j]);
+        f[2 * j] = v.x;
+        f[2 * j + 1] = v.y;
+    }
+}
+__device__ __forceinline__ uint4 pack_rest8(const float (&f)[8], const uint4 &hi)
+{
+    float h[8], l[8];
+    unpack_half8(hi, h);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) l[j] = f[j] - h[j];
+    return pack_half8(l);
+}
+// The sum of squares of a row's 64 elements in a block, from the eight lanes that have them, in lanes 0, 8, 16, 24.
+__device__ __forceinline__ float row_squares(const float (&f)[8])
+{
+    float q = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q = fmaf(f[j], f[j], q);
+    for (int o = 1; o < 8; o <<= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
+    return q;
 }
 
 // X of the first step, a block of 64x64 at a time: normalised, split into two fp16 numbers, padded with zeros.
@@ -147,125 +235,529 @@ __global__ void __launch_bounds__(kSweepBlock) ns_start_kernel(const __grid_cons
 {
     __shared__ double red[kSweepBlock / 32];
     __shared__ float tile[64][65];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int have = -1;
+    float pre = 1.0f, factor = 0.0f, nan = 0.0f;
     pdl_begin();
     for (int u = blockIdx.x; u < P.units; u += gridDim.x) {
-        const NsItem &it = P.item[item_of<kBlockList>(P, u)];
-        const int b = u - it.block_first, R = b % it.rb, C = b / it.rb;
-        double s = 0.0;
-        for (int p = threadIdx.x; p < it.parts; p += kSweepBlock) s += it.part[p];
-        const double norm = sqrt(block_sum(s, red));
-        if (b == 0 && threadIdx.x == 0 && P.status && !isfinite(norm)) atomicMin(P.status, (int)TWN_ERR_NONFINITE);
-        // in two factors, so that neither leaves the range of fp32
-        const float pre = norm > 1e18 ? 0x1p-100f : 1.0f;
-        const float factor = norm == 0.0 ? 0.0f : (float)((double)kStart / (fmax(norm, (double)P.eps) * (double)pre));
-        const float nan = norm == norm ? 0.0f : __uint_as_float(0x7FC00000u);      // fmax drops a NaN
+        const int t = item_of(P, u);
+        const NsItem &it = P.item[t];
+        const int b = u - it.first, R = b % it.rb, C = b / it.rb;
+        if (t != have) {
+            double s = 0.0;
+            for (int p = threadIdx.x; p < it.parts; p += kSweepBlock) s += it.part[p];
+            const double norm = sqrt(block_sum(s, red));
+            if (b == 0 && threadIdx.x == 0 && P.status && !isfinite(norm)) atomicMin(P.status, (int)TWN_ERR_NONFINITE);
+            // in two factors, so that neither leaves the range of fp32
+            pre = norm > 1e18 ? 0x1p-100f : 1.0f;
+            factor = norm == 0.0 ? 0.0f : (float)((double)kStart / (fmax(norm, (double)P.eps) * (double)pre));
+            nan = norm == norm ? 0.0f : __uint_as_float(0x7FC00000u);      // fmax drops a NaN
+            have = t;
+        }
         const int r0 = 64 * R, c0 = 64 * C;
-        // rows of G along the threads of a warp
-        for (int e = threadIdx.x; e < 4096; e += kSweepBlock) {
-            const int i = e >> 6, j = e & 63;
-            const int r = r0 + (it.tall ? j : i), c = c0 + (it.tall ? i : j);
-            float v = 0.0f;
-            if (r < it.m && c < it.n) v = element(it, P, it.tall ? (long long)c * it.m + r : (long long)r * it.n + c) * pre * factor + nan;
-            tile[it.tall ? j : i][it.tall ? i : j] = v;
+        const bool direct = it.vec_in && !it.tall && it.n % 8 == 0;
+        if (!direct) {
+            // rows of G along the threads of a warp
+            __syncthreads();
+            for (int e = threadIdx.x; e < 4096; e += kSweepBlock) {
+                const int i = e >> 6, j = e & 63;
+                const int r = r0 + (it.tall ? j : i), c = c0 + (it.tall ? i : j);
+                float v = 0.0f;
+                if (r < it.m && c < it.n) v = element(it, P, it.tall ? (long long)c * it.m + r : (long long)r * it.n + c);
+                tile[it.tall ? j : i][it.tall ? i : j] = v;
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        uint16_t *const hi = it.x[0] + block_at(R, C, it.rb), *const lo = it.lo + block_at(R, C, it.rb);
-        for (int e = threadIdx.x; e < 2048; e += kSweepBlock) {
-            const int r = e >> 5, c = 2 * (e & 31);
-            const float v0 = tile[r][c], v1 = tile[r][c + 1];
-            const __half2 h = __floats2half2_rn(v0, v1);
-            const float2 back = __half22float2(h);
-            const __half2 l = __floats2half2_rn(v0 - back.x, v1 - back.y);
-            *reinterpret_cast<__half2 *>(hi + in_block(r, c)) = h;
-            *reinterpret_cast<__half2 *>(lo + in_block(r, c)) = l;
-        }
-        if (threadIdx.x < 128) {
-            const int r = threadIdx.x & 63, half = threadIdx.x >> 6;
-            float q = 0.0f;
-            for (int c = 32 * half; c < 32 * half + 32; ++c) q = fmaf(tile[r][c], tile[r][c], q);
-            it.squares[(size_t)(2 * C + half) * (64 * it.rb) + r0 + r] = q;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int rr = 8 * warp + 4 * k + (lane >> 3), cc = 8 * (lane & 7), r = r0 + rr, c = c0 + cc;
+            const bool in = r < it.m && c < it.n;
+            float f[8];
+            if (direct) {
+                if (in) elements8<false>(it, P, (long long)r * it.n + c, f);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = tile[rr][cc + j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = in && c + j < it.n ? f[j] * pre * factor + nan : 0.0f;
+            const size_t at = block_at(R, C, it.rb) + in_block(rr, cc);
+            const uint4 hi = pack_half8(f);
+            *reinterpret_cast<uint4 *>(it.x[0] + at) = hi;
+            *reinterpret_cast<uint4 *>(it.lo + at) = pack_rest8(f, hi);
+            const float q = row_squares(f);
+            if ((lane & 7) == 0) it.squares[(size_t)C * (64 * it.rb) + r] = q;
         }
     }
 }
 
-struct __align__(1024) NsSmem {
-    uint8_t ring[kStages][kStageBytes];
-    unsigned long long full[kStages], empty[kStages], acc_full[2], acc_empty[2];
-    uint32_t tmem_base;
-    volatile int abort_flag;
-};
-
+// ---- PTX of the products ---------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, void *bar)
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
-
-// D[tmem] (+)= A[smem] B[smem]^T, fp16, issued by the calling thread alone.
-__device__ __forceinline__ void ns_mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc)
+// Rows of 128 bytes from row `row` of a matrix of blocks on, by either block of a pair; the barrier is at this address in the
+// first of them.
+__device__ __forceinline__ void pair_load(void *dst, const CUtensorMap *map, uint32_t bar, int row)
 {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(acc)
-        : "memory");
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(row) : "memory");
+}
+// D[tmem] (+)= A[smem] B[smem]^T, fp16, issued by the calling thread alone; PAIR: by that of the first block for both.
+template <bool PAIR> __device__ __forceinline__ void ns_mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc)
+{
+    if (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(acc) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(acc) : "memory");
+}
+// The barrier at this address in both blocks gets one arrival when the MMAs so far are done.
+__device__ __forceinline__ void pair_commit(void *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ uint32_t of_block(uint32_t addr, uint32_t rank)
+{
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ float4 ld_block(uint32_t cluster_addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float ld_block1(uint32_t cluster_addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
 }
 
-// A tile: 128 rows from block row 2 i on, `nb` (at most 4) blocks of columns from block 4 J on, a reduction of kb blocks.
-struct Tile {
-    int i, J, nb, kb;
-};
-template <int PHASE> __device__ __forceinline__ Tile tile_of(const NsItem &it, int u)
+// ---- epilogue ----------------------------------------------------------------------------------------------------------------
+// A warp's 32 x 64 sums in shared memory: 16-byte piece 2 p + h of row r lies where a warp's row-wise writes, reads of four
+// rows by eight pieces of like h, and reads of eight columns by four runs of eight rows are all free of bank conflicts.
+__device__ __forceinline__ int slot_of(int r, int p, int h) { return r * 64 + h * 32 + (((p ^ r ^ (r >> 3) ^ (h << 2)) & 7) << 2); }
+
+// 64 columns of the accumulator of a warp's 32 rows.
+__device__ __forceinline__ void dump_sums(uint32_t taddr, float *buf)
 {
-    Tile t;
-    const int pairs = it.rb >> 1;                      // row tiles
-    if (PHASE == kApply) {
-        u -= it.apply_first;
-        t.i = u % pairs;
-        t.J = u / pairs;
-        t.nb = min(4, it.cb - 4 * t.J);
-        t.kb = (it.m + 63) >> 6;
-    } else {
-        // row tiles 2p and 2p + 1 have p + 1 tiles each, on or below the diagonal
-        u -= it.sym_first;
-        int p = (int)((sqrtf(4.0f * (float)u + 1.0f) - 1.0f) * 0.5f);
-        while (p * (p + 1) > u) --p;
-        while ((p + 1) * (p + 2) <= u) ++p;
-        const int rem = u - p * (p + 1);
-        t.i = 2 * p + (rem > p);
-        t.J = rem > p ? rem - p - 1 : rem;
-        t.nb = min(4, it.rb - 4 * t.J);
-        t.kb = PHASE == kGram ? it.cb : (it.m + 63) >> 6;
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+        uint32_t v[32];
+        tmem_ld32(taddr + 32 * g, v);
+        tmem_wait_ld(v);
+#pragma unroll
+        for (int p = 0; p < 8; ++p)
+            *reinterpret_cast<uint4 *>(buf + slot_of(lane, 4 * g + (p >> 1), p & 1)) = make_uint4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
     }
-    return t;
 }
 
-__device__ __forceinline__ uint32_t half2_bits(float a, float b)
+// The sums of a warp's tile: in its own buffer, or spread over the blocks of a cluster, added in their order.
+struct OwnSums {
+    const float *buf;
+    __device__ __forceinline__ void row8(int r, int p, float (&v)[8]) const
+    {
+        const float4 a = *reinterpret_cast<const float4 *>(buf + slot_of(r, p, 0)), b = *reinterpret_cast<const float4 *>(buf + slot_of(r, p, 1));
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+    __device__ __forceinline__ void column8(int r, int c, float (&v)[8]) const      // rows r .. r + 7
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = buf[slot_of(r + e, c >> 3, (c >> 2) & 1) + (c & 3)];
+    }
+};
+struct ClusterSums {
+    uint32_t addr, first;        // the buffer's address; rank of the first block that shares the tile
+    int split;
+    __device__ __forceinline__ void row8(int r, int p, float (&v)[8]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+#pragma unroll 4
+        for (int g = 0; g < split; ++g) {
+            const uint32_t at = of_block(addr, first + g);
+            const float4 a = ld_block(at + 4 * slot_of(r, p, 0)), b = ld_block(at + 4 * slot_of(r, p, 1));
+            v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+        }
+    }
+    __device__ __forceinline__ void column8(int r, int c, float (&v)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+#pragma unroll 2
+        for (int g = 0; g < split; ++g) {
+            const uint32_t at = of_block(addr, first + g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += ld_block1(at + 4 * (slot_of(r + e, c >> 3, (c >> 2) & 1) + (c & 3)));
+        }
+    }
+};
+
+// Symmetric products: the warp's tile from row r0 and column c0 on, and its mirror image; of its eight units of work those
+// that are `me` modulo `split`.
+template <int PHASE, typename Sums>
+__device__ __forceinline__ void finish_symmetric(const NsItem &it, const NsParams &P, const Sums &sums, int r0, int c0, bool mirror, int me, int split)
 {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
+    const int lane = threadIdx.x & 31;
+    const bool diagonal = r0 >= c0 && r0 < c0 + 64;
+    const float unscale = P.step == 0 ? 1.0f / (kStart * kStart) : 1.0f;
+    uint16_t *const to = PHASE == kGram ? it.A : it.B;
+    if (PHASE == kGram && diagonal && me == 0) {
+        float a = 0.0f;
+#pragma unroll 16
+        for (int g = 0; g < it.cb; ++g) a += it.squares[(size_t)g * (64 * it.rb) + r0 + lane];
+        it.alpha[r0 + lane] = a * unscale;
+    }
+    auto eight = [&](int r, int c, float (&v)[8]) {              // row r, columns c ..: sums to elements
+        if (PHASE == kGram) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= unscale;
+        } else {
+            float a[8];
+            unpack_half8(*reinterpret_cast<const uint4 *>(it.A + piece_at(r, c, it.rb)), a);
+            const float ar = it.alpha[r];
+            const float4 a0 = *reinterpret_cast<const float4 *>(it.alpha + c), a1 = *reinterpret_cast<const float4 *>(it.alpha + c + 4);
+            const float ac[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (c + j == r) it.beta[r] = kB * ar + kC * (v[j] + ar * ar);
+                v[j] = kB * a[j] + kC * (v[j] + (ar + ac[j]) * a[j]);
+            }
+        }
+    };
+#pragma unroll 2
+    for (int u = me; u < 8; u += split) {
+        const int r = 4 * u + (lane >> 3), p = lane & 7;
+        float v[8];
+        sums.row8(r, p, v);
+        eight(r0 + r, c0 + 8 * p, v);
+        if (diagonal)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c0 + 8 * p + j == r0 + r) v[j] = 0.0f;
+        *reinterpret_cast<uint4 *>(to + piece_at(r0 + r, c0 + 8 * p, it.rb)) = pack_half8(v);
+    }
+    if (!mirror) return;
+#pragma unroll 2
+    for (int u = me; u < 8; u += split) {
+        const int c = 8 * u + (lane >> 2), r = 8 * (lane & 3);
+        float v[8];
+        sums.column8(r, c, v);
+        eight(c0 + c, r0 + r, v);
+        *reinterpret_cast<uint4 *>(to + piece_at(c0 + c, r0 + r, it.rb)) = pack_half8(v);
+    }
 }
-__device__ __forceinline__ float2 half2_of(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+
+__device__ __forceinline__ void store_out(const NsItem &it, long long at, float v)
+{
+    if (it.o_bf16) static_cast<__nv_bfloat16 *>(it.O)[at] = __float2bfloat16_rn(v);
+    else static_cast<float *>(it.O)[at] = v;
+}
+__device__ __forceinline__ void store_out8(const NsItem &it, long long at, const float (&v)[8])
+{
+    if (it.o_bf16) {
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(it.O) + at) =
+            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    } else {
+        float4 *o = reinterpret_cast<float4 *>(static_cast<float *>(it.O) + at);
+        o[0] = make_float4(v[0], v[1], v[2], v[3]);
+        o[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+}
+
+// X of the next step, or the result.
+__device__ __forceinline__ void finish_apply(const NsItem &it, const NsParams &P, float *buf, int r0, int c0)
+{
+    const int lane = threadIdx.x & 31, p = lane & 7, cur = P.step & 1;
+    const float unscale = P.step == 0 ? 1.0f / kStart : 1.0f;
+    const OwnSums sums{buf};
+#pragma unroll 4
+    for (int u = 0; u < 8; ++u) {
+        const int r = 4 * u + (lane >> 3);
+        const size_t at = piece_at(r0 + r, c0 + 8 * p, it.rb);
+        const uint4 hi = *reinterpret_cast<const uint4 *>(it.x[cur] + at), lo = *reinterpret_cast<const uint4 *>(it.lo + at);
+        const float k = kA + it.beta[r0 + r];
+        float v[8], h[8], l[8];
+        sums.row8(r, p, v);
+        unpack_half8(hi, h);
+        unpack_half8(lo, l);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (k * (h[j] + l[j]) + v[j]) * unscale;
+        if (P.last) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= it.out_scale;
+            if (it.vec_out && !it.tall) {
+                if (r0 + r < it.m && c0 + 8 * p < it.n) store_out8(it, (long long)(r0 + r) * it.n + c0 + 8 * p, v);
+            } else {
+                *reinterpret_cast<float4 *>(buf + slot_of(r, p, 0)) = make_float4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<float4 *>(buf + slot_of(r, p, 1)) = make_float4(v[4], v[5], v[6], v[7]);
+            }
+        } else {
+            const uint4 h2 = pack_half8(v);
+            *reinterpret_cast<uint4 *>(it.x[cur ^ 1] + at) = h2;
+            *reinterpret_cast<uint4 *>(it.lo + at) = pack_rest8(v, h2);
+            const float q = row_squares(v);
+            if (p == 0) it.squares[(size_t)(c0 >> 6) * (64 * it.rb) + r0 + r] = q;
+        }
+    }
+    if (!P.last || (it.vec_out && !it.tall)) return;
+    __syncwarp();
+    if (it.tall && it.vec_out) {
+#pragma unroll 2
+        for (int u = 0; u < 8; ++u) {
+            const int c = 8 * u + (lane >> 2), r = 8 * (lane & 3);
+            float v[8];
+            sums.column8(r, c, v);
+            if (c0 + c < it.n && r0 + r < it.m) store_out8(it, (long long)(c0 + c) * it.m + r0 + r, v);
+        }
+    } else if (it.tall) {
+        if (r0 + lane < it.m)
+            for (int c = 0; c < 64 && c0 + c < it.n; ++c)
+                store_out(it, (long long)(c0 + c) * it.m + r0 + lane, buf[slot_of(lane, c >> 3, (c >> 2) & 1) + (c & 3)]);
+    } else {
+        for (int r = 0; r < 32 && r0 + r < it.m; ++r)
+            for (int c = lane; c < 64 && c0 + c < it.n; c += 32)
+                store_out(it, (long long)(r0 + r) * it.n + c0 + c, buf[slot_of(r, c >> 3, (c >> 2) & 1) + (c & 3)]);
+    }
+}
+
+// Row `u` of a triangle that is written row by row, and what is left of u in it.
+__device__ __forceinline__ int triangle_row(int u, int *column)
+{
+    int i = (int)((sqrtf(8.0f * (float)u + 1.0f) - 1.0f) * 0.5f);
+    while (i * (i + 1) / 2 > u) --i;
+    while ((i + 1) * (i + 2) / 2 <= u) ++i;
+    *column = u - i * (i + 1) / 2;
+    return i;
+}
+
+template <int PHASE> __device__ __forceinline__ int reduction_blocks(const NsItem &it) { return PHASE == kGram ? (it.n + 63) >> 6 : (it.m + 63) >> 6; }
+
+// fp16 operands, fp32 accumulator; B MN-major where it is X
+template <int PHASE> __host__ __device__ constexpr uint32_t ns_idesc(int M, int N)
+{
+    return (1u << 4) | (PHASE == kApply ? 1u << 16 : 0u) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// One reduction block: four MMAs of 16.
+template <int PHASE, bool PAIR> __device__ __forceinline__ void ns_mma_block(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool first)
+{
+    constexpr uint64_t kStep = PHASE == kApply ? (16 * 128) >> 4 : 32 >> 4;      // 16 rows of the reduction, or 16 columns
+    ns_mma<PAIR>(d, a, b, idesc, first ? 0u : 1u);
+    ns_mma<PAIR>(d, a + 2, b + kStep, idesc, 1u);
+    ns_mma<PAIR>(d, a + 4, b + 2 * kStep, idesc, 1u);
+    ns_mma<PAIR>(d, a + 6, b + 3 * kStep, idesc, 1u);
+}
+
+// ---- large products ------------------------------------------------------------------------------------------------------
+// 256x256 tiles by pairs of blocks: a block has 128 rows of A and 128 of B's 256 columns in shared memory and 128 rows by 256
+// columns of the result in tensor memory, twice, so the epilogue of a tile runs beside the next one.  Both blocks' copies count on the
+// barrier of the first, whose thread issues the MMAs for both.
+struct __align__(1024) PairSmem {
+    uint8_t ring[kPairStages][kStageBytes];
+    float sums[kEpiWarps][kWarpTile];
+    unsigned long long full[kPairStages], empty[kPairStages], acc_full[2], acc_empty[2];
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
 
 template <int PHASE>
-__global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_constant__ NsParams P)
+__global__ void __launch_bounds__(kNsThreads, 1)
+ns_pair_kernel(const __grid_constant__ CUtensorMap rows128, const __grid_constant__ CUtensorMap rows64, const __grid_constant__ NsParams P)
 {
-    constexpr int LIST = PHASE == kApply ? kApplyList : kSymList;
     if (gridDim.x <= kPdlBlocks) pdl_launch_dependents();
     extern __shared__ uint8_t smem_raw[];
-    NsSmem *sm = reinterpret_cast<NsSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    PairSmem *sm = reinterpret_cast<PairSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     volatile int *abort_flag = &sm->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) { mbar_init(&sm->full[s], 1); mbar_init(&sm->empty[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&sm->acc_full[s], 1); mbar_init(&sm->acc_empty[s], kEpiWarps); }
+        for (int s = 0; s < kPairStages; ++s) { mbar_init(&sm->full[s], 1); mbar_init(&sm->empty[s], 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&sm->acc_full[s], 1); mbar_init(&sm->acc_empty[s], 2 * kEpiWarps); }
         sm->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(512u) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+    pdl_wait();
+    const uint32_t tmem = sm->tmem_base;
+    const int cur = P.step & 1;
+    const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
+
+    // tile (I, J) of unit u
+    auto tile_of = [&](const NsItem &it, int u, int &I, int &J) {
+        u -= it.first;
+        if (PHASE == kApply) {
+            const int rows = it.rb >> 2;
+            I = u % rows;
+            J = u / rows;
+        } else {
+            I = triangle_row(u, &J);
+        }
+    };
+
+    if (warp == 0) {
+        if (elect_one()) {
+            uint32_t s = 0, ph = 0;
+            bool ok = true;
+            for (int u = pair; u < P.units && ok; u += pairs) {
+                const NsItem &it = P.item[item_of(P, u)];
+                int I, J;
+                tile_of(it, u, I, J);
+                const uint16_t *const src_a = PHASE == kGram ? it.x[cur] : PHASE == kSquare ? it.A : it.B;
+                const uint16_t *const src_b = PHASE == kSquare ? it.A : it.x[cur];
+                // rows of 128 bytes from the first of the workspace's blocks on
+                const int a_row = (int)((src_a - P.base) >> 6), b_row = (int)((src_b - P.base) >> 6);
+                const int kb = reduction_blocks<PHASE>(it);
+                // a tile on the diagonal has the same rows on both sides, in both blocks
+                const bool same = PHASE != kApply && I == J;
+                for (int k = 0; k < kb; ++k) {
+                    uint8_t *const st = sm->ring[s];
+                    if (!mbar_wait(&sm->empty[s], ph ^ 1u, abort_flag, P.status, 20)) { ok = false; break; }
+                    if (rank == 0) mbar_expect_tx(&sm->full[s], same ? 2 * kOpBytes : 2 * kStageBytes);
+                    const uint32_t bar = of_block(smem_u32(&sm->full[s]), 0);
+                    pair_load(st, &rows128, bar, a_row + 64 * (k * it.rb + 4 * I + 2 * (int)rank));
+                    if (PHASE == kApply) {
+                        for (int j = 0; j < 2; ++j)
+                            pair_load(st + kOpBytes + j * kBlockBytes, &rows64, bar, b_row + 64 * ((4 * J + 2 * (int)rank + j) * it.rb + k));
+                    } else if (!same) {
+                        pair_load(st + kOpBytes, &rows128, bar, b_row + 64 * (k * it.rb + 4 * J + 2 * (int)rank));
+                    }
+                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && elect_one()) {
+            uint32_t s = 0, ph = 0, lu = 0;
+            bool ok = true;
+            const uint32_t ring = smem_u32(sm->ring);
+            const uint64_t a0 = smem_desc_sw128(ring);
+            const uint64_t b0 = PHASE == kApply ? smem_desc_mn_sw128(ring + kOpBytes, kBlockBytes) : smem_desc_sw128(ring + kOpBytes);
+            constexpr uint32_t idesc = ns_idesc<PHASE>(256, 256);
+            for (int u = pair; u < P.units && ok; u += pairs, ++lu) {
+                const NsItem &it = P.item[item_of(P, u)];
+                int I, J;
+                tile_of(it, u, I, J);
+                const int kb = reduction_blocks<PHASE>(it);
+                const uint64_t bt = PHASE != kApply && I == J ? a0 : b0;
+                if (!mbar_wait(&sm->acc_empty[lu & 1], ((lu >> 1) & 1u) ^ 1u, abort_flag, P.status, 0)) break;
+                tc_fence_after();
+                for (int k = 0; k < kb; ++k) {
+                    if (!mbar_wait(&sm->full[s], ph, abort_flag, P.status, 0)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint64_t off = s * (uint64_t)(kStageBytes >> 4);
+                    ns_mma_block<PHASE, true>(tmem + (lu & 1) * 256, a0 + off, bt + off, idesc, k == 0);
+                    pair_commit(&sm->empty[s]);
+                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                }
+                if (ok) pair_commit(&sm->acc_full[lu & 1]);
+            }
+        }
+    } else {
+        const int q = warp & 3, set = (warp - 2) >> 2;
+        float *const buf = sm->sums[warp - 2];
+        uint32_t lu = 0;
+        for (int u = pair; u < P.units; u += pairs, ++lu) {
+            const NsItem &it = P.item[item_of(P, u)];
+            int I, J;
+            tile_of(it, u, I, J);
+            if (!mbar_wait_warp(&sm->acc_full[lu & 1], (lu >> 1) & 1u, abort_flag, P.status, 32)) break;
+            tc_fence_after();
+            const int r0 = 256 * I + 128 * (int)rank + 32 * q;
+#pragma unroll 1
+            for (int b = set; b < 4; b += 2) {
+                const int c0 = 256 * J + 64 * b;
+                dump_sums(tmem + ((uint32_t)(32 * q) << 16) + (lu & 1) * 256 + 64 * b, buf);
+                __syncwarp();
+                if (b >= 2) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_at(of_block(smem_u32(&sm->acc_empty[lu & 1]), 0));
+                }
+                if (PHASE == kApply) finish_apply(it, P, buf, r0, c0);
+                else finish_symmetric<PHASE>(it, P, OwnSums{buf}, r0, c0, J < I, 0, 1);
+                __syncwarp();
+            }
+        }
+    }
+
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (sm->abort_flag) {
+        // copies and products in flight end well within this
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);
+    }
+    __syncthreads();
+    cluster_sync();                                    // neither block's memory goes while the other may use it
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+// ---- small products ------------------------------------------------------------------------------------------------------
+// A 128x128 tile a block, two blocks on an SM.  `split` blocks of a cluster share a tile's reduction; each leaves its sums in
+// the shared memory that was its ring, and finishes every split-th unit of the whole tile.
+struct __align__(1024) TileSmem {
+    union {
+        uint8_t ring[kTileStages][kStageBytes];
+        float sums[kEpiWarps][kWarpTile];
+    };
+    unsigned long long full[kTileStages], empty[kTileStages], acc_full;
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
+
+template <int PHASE>
+__global__ void __launch_bounds__(kNsThreads, 2) ns_tile_kernel(const __grid_constant__ NsParams P)
+{
+    pdl_launch_dependents();
+    extern __shared__ uint8_t smem_raw[];
+    TileSmem *sm = reinterpret_cast<TileSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    volatile int *abort_flag = &sm->abort_flag;
+    const int warp = threadIdx.x >> 5;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kTileStages; ++s) { mbar_init(&sm->full[s], 1); mbar_init(&sm->empty[s], 1); }
+        mbar_init(&sm->acc_full, 1);
+        sm->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(128u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -275,197 +767,103 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_
     const uint32_t tmem = sm->tmem_base;
     const int cur = P.step & 1;
 
+    const int u = blockIdx.x;
+    const bool live = u < P.units;
+    const NsItem &it = P.item[item_of(P, live ? u : 0)];
+    const int split = PHASE == kApply ? 1 : it.split;
+    int i = 0, j = 0, me = 0, k0 = 0, k1 = 0;
+    if (live) {
+        int t = u - it.first;
+        if (PHASE == kApply) {
+            const int rows = it.rb >> 1;
+            i = t % rows;
+            j = t / rows;
+        } else {
+            me = t & (split - 1);
+            i = triangle_row(t / split, &j);
+        }
+        const int kb = reduction_blocks<PHASE>(it);
+        k0 = (int)((long long)kb * me / split);        // a split leaves every block four reduction blocks or more
+        k1 = (int)((long long)kb * (me + 1) / split);
+    }
+    const bool same = PHASE != kApply && i == j;       // the same rows on both sides
+
     if (warp == 0) {
         if (elect_one()) {
+            const uint16_t *const src_a = PHASE == kGram ? it.x[cur] : PHASE == kSquare ? it.A : it.B;
+            const uint16_t *const src_b = PHASE == kSquare ? it.A : it.x[cur];
             uint32_t s = 0, ph = 0;
-            bool ok = true;
-            for (int u = blockIdx.x; u < P.units && ok; u += gridDim.x) {
-                const NsItem &it = P.item[item_of<LIST>(P, u)];
-                const Tile t = tile_of<PHASE>(it, u);
-                const uint16_t *const src_a = PHASE == kGram ? it.x[cur] : PHASE == kSquare ? it.A : it.B;
-                const uint16_t *const src_b = PHASE == kSquare ? it.A : it.x[cur];
-                const uint32_t b_bytes = (uint32_t)t.nb * kBlockBytes;
-                for (int k = 0; k < t.kb; ++k) {
-                    uint8_t *const st = sm->ring[s];
-                    if (!mbar_wait(&sm->empty[s], ph ^ 1u, abort_flag, P.status, 20)) { ok = false; break; }
-                    mbar_expect_tx(&sm->full[s], kABytes + b_bytes);
-                    bulk_load(st, src_a + block_at(2 * t.i, k, it.rb), kABytes, &sm->full[s]);
-                    if (PHASE == kApply) {
-                        for (int j = 0; j < t.nb; ++j)
-                            bulk_load(st + kABytes + j * kBlockBytes, src_b + block_at(k, 4 * t.J + j, it.rb), kBlockBytes, &sm->full[s]);
-                    } else {
-                        bulk_load(st + kABytes, src_b + block_at(4 * t.J, k, it.rb), b_bytes, &sm->full[s]);
-                    }
-                    if (++s == kStages) { s = 0; ph ^= 1u; }
+            for (int k = k0; k < k1; ++k) {
+                uint8_t *const st = sm->ring[s];
+                if (!mbar_wait(&sm->empty[s], ph ^ 1u, abort_flag, P.status, 20)) break;
+                mbar_expect_tx(&sm->full[s], same ? kOpBytes : kStageBytes);
+                bulk_load(st, src_a + block_at(2 * i, k, it.rb), kOpBytes, &sm->full[s]);
+                if (PHASE == kApply) {
+                    for (int b = 0; b < 2; ++b)
+                        bulk_load(st + kOpBytes + b * kBlockBytes, src_b + block_at(k, 2 * j + b, it.rb), kBlockBytes, &sm->full[s]);
+                } else if (!same) {
+                    bulk_load(st + kOpBytes, src_b + block_at(2 * j, k, it.rb), kOpBytes, &sm->full[s]);
                 }
+                if (++s == kTileStages) { s = 0; ph ^= 1u; }
             }
         }
     } else if (warp == 1) {
         if (elect_one()) {
-            uint32_t s = 0, ph = 0, lu = 0;
-            bool ok = true;
             const uint32_t ring = smem_u32(sm->ring);
             const uint64_t a0 = smem_desc_sw128(ring);
-            const uint64_t b0 = PHASE == kApply ? smem_desc_mn_sw128(ring + kABytes, kBlockBytes) : smem_desc_sw128(ring + kABytes);
-            constexpr uint64_t kStageStep = kStageBytes >> 4;
-            constexpr uint64_t kBStep = PHASE == kApply ? (16 * 128) >> 4 : 32 >> 4;      // 16 rows of the reduction, or 16 columns
-            for (int u = blockIdx.x; u < P.units && ok; u += gridDim.x, ++lu) {
-                const NsItem &it = P.item[item_of<LIST>(P, u)];
-                const Tile t = tile_of<PHASE>(it, u);
-                // fp16 operands, fp32 accumulator, B MN-major where it is X
-                const uint32_t idesc = (1u << 4) | (PHASE == kApply ? 1u << 16 : 0u) | ((uint32_t)(t.nb * 8) << 17) | (8u << 24);
-                if (!mbar_wait(&sm->acc_empty[lu & 1], ((lu >> 1) & 1u) ^ 1u, abort_flag, P.status, 0)) break;
+            const uint64_t b0 = same ? a0 : PHASE == kApply ? smem_desc_mn_sw128(ring + kOpBytes, kBlockBytes) : smem_desc_sw128(ring + kOpBytes);
+            constexpr uint32_t idesc = ns_idesc<PHASE>(128, 128);
+            uint32_t s = 0, ph = 0;
+            bool ok = true;
+            for (int k = k0; k < k1; ++k) {
+                if (!mbar_wait(&sm->full[s], ph, abort_flag, P.status, 0)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t d = tmem + (lu & 1) * kAccCols;
-                for (int k = 0; k < t.kb; ++k) {
-                    if (!mbar_wait(&sm->full[s], ph, abort_flag, P.status, 0)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint64_t a = a0 + s * kStageStep, b = b0 + s * kStageStep;
-                    ns_mma(d, a, b, idesc, k > 0);
-                    ns_mma(d, a + 2, b + kBStep, idesc, 1u);
-                    ns_mma(d, a + 4, b + 2 * kBStep, idesc, 1u);
-                    ns_mma(d, a + 6, b + 3 * kBStep, idesc, 1u);
-                    tc_commit(&sm->empty[s]);
-                    if (++s == kStages) { s = 0; ph ^= 1u; }
-                }
-                if (ok) tc_commit(&sm->acc_full[lu & 1]);
+                const uint64_t off = s * (uint64_t)(kStageBytes >> 4);
+                ns_mma_block<PHASE, false>(tmem, a0 + off, b0 + off, idesc, k == k0);
+                tc_commit(&sm->empty[s]);
+                if (++s == kTileStages) { s = 0; ph ^= 1u; }
             }
+            if (ok) tc_commit(&sm->acc_full);
         }
-    } else {
-        const int q = warp & 3, set = (warp - 2) >> 2;
-        uint32_t lu = 0;
-        for (int u = blockIdx.x; u < P.units; u += gridDim.x, ++lu) {
-            const NsItem &it = P.item[item_of<LIST>(P, u)];
-            const Tile t = tile_of<PHASE>(it, u);
-            if (!mbar_wait_warp(&sm->acc_full[lu & 1], (lu >> 1) & 1u, abort_flag, P.status, 32)) break;
+    }
+    __syncwarp();
+
+    const int w = warp - 2, q = warp & 3, half = w >> 2;
+    const int r0 = 128 * i + 32 * q, c0 = 128 * j + 64 * half;
+    if (warp >= 2 && live) {
+        // all products are done, so all copies have landed: the ring is free
+        if (mbar_wait_warp(&sm->acc_full, 0u, abort_flag, P.status, 32)) {
             tc_fence_after();
-            const int r = 128 * t.i + 32 * q + lane;
-            const float unscale = P.step == 0 ? 1.0f / kStart : 1.0f;
-            const float row_diag = PHASE == kSquare ? it.alpha[r] : PHASE == kApply ? it.beta[r] : 0.0f;
-            // a warp has every other chunk of 32 columns
-#pragma unroll 1
-            for (int ch = set; ch < 2 * t.nb; ch += 2) {
-                const int c0 = 256 * t.J + 32 * ch;
-                if (PHASE != kApply && (c0 >> 7) > t.i) break;             // above the diagonal: another tile's mirror image
-                uint32_t v[32];
-                tmem_ld32(tmem + ((uint32_t)(32 * q) << 16) + (lu & 1) * kAccCols + 32 * ch, v);
-                tmem_wait_ld(v);
-                // this thread's 32 elements of the row: four 16-byte pieces
-                const size_t block = block_at(r >> 6, c0 >> 6, it.rb);
-                uint16_t *const to = PHASE == kGram ? it.A : PHASE == kSquare ? it.B : it.x[cur ^ 1];
-                float f[32];
-                if (PHASE == kGram) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]) * (unscale * unscale);
-                } else if (PHASE == kSquare) {
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        const uint4 w = *reinterpret_cast<const uint4 *>(it.A + block + in_block(r & 63, (c0 & 63) + 8 * p));
-                        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int e = 8 * p + 2 * j;
-                            const float2 a = half2_of(ws[j]);
-                            const float2 al = *reinterpret_cast<const float2 *>(it.alpha + c0 + e);
-                            f[e] = kB * a.x + kC * (__uint_as_float(v[e]) + (row_diag + al.x) * a.x);
-                            f[e + 1] = kB * a.y + kC * (__uint_as_float(v[e + 1]) + (row_diag + al.y) * a.y);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        const int at = in_block(r & 63, (c0 & 63) + 8 * p);
-                        const uint4 h = *reinterpret_cast<const uint4 *>(it.x[cur] + block + at);
-                        const uint4 l = *reinterpret_cast<const uint4 *>(it.lo + block + at);
-                        const uint32_t hs[4] = {h.x, h.y, h.z, h.w}, ls[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int e = 8 * p + 2 * j;
-                            const float2 x = half2_of(hs[j]), y = half2_of(ls[j]);
-                            f[e] = ((kA + row_diag) * (x.x + y.x) + __uint_as_float(v[e])) * unscale;
-                            f[e + 1] = ((kA + row_diag) * (x.y + y.y) + __uint_as_float(v[e + 1])) * unscale;
-                        }
-                    }
-                }
-                if (PHASE != kApply && (unsigned)(r - c0) < 32u) {
-                    // the diagonal, apart: selected without indexing registers by a variable
-                    float dia = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (r - c0 == j) {
-                            if (PHASE == kSquare) dia = kB * row_diag + kC * (__uint_as_float(v[j]) + row_diag * row_diag);
-                            f[j] = 0.0f;
-                        }
-                    if (PHASE == kGram) {
-#pragma unroll 8
-                        for (int g = 0; g < 2 * it.cb; ++g) dia += it.squares[(size_t)g * (64 * it.rb) + r];
-                        dia *= unscale * unscale;
-                    }
-                    (PHASE == kGram ? it.alpha : it.beta)[r] = dia;
-                }
-                if (PHASE == kApply && P.last) {
-                    if (r < it.m) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const int c = c0 + j;
-                            if (c < it.n) {
-                                const long long at = it.tall ? (long long)c * it.m + r : (long long)r * it.n + c;
-                                const float o = f[j] * it.out_scale;
-                                if (it.o_bf16) static_cast<__nv_bfloat16 *>(it.O)[at] = __float2bfloat16_rn(o);
-                                else static_cast<float *>(it.O)[at] = o;
-                            }
-                        }
-                    }
-                    continue;
-                }
-                if (PHASE == kApply) {
-                    float sq = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) sq = fmaf(f[j], f[j], sq);
-                    it.squares[(size_t)(c0 >> 5) * (64 * it.rb) + r] = sq;
-                }
-                uint32_t h[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) h[j] = half2_bits(f[2 * j], f[2 * j + 1]);
-#pragma unroll
-                for (int p = 0; p < 4; ++p)
-                    *reinterpret_cast<uint4 *>(to + block + in_block(r & 63, (c0 & 63) + 8 * p)) =
-                        make_uint4(h[4 * p], h[4 * p + 1], h[4 * p + 2], h[4 * p + 3]);
-                if (PHASE == kApply) {
-                    uint32_t l[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float2 x = half2_of(h[j]);
-                        l[j] = half2_bits(f[2 * j] - x.x, f[2 * j + 1] - x.y);
-                    }
-#pragma unroll
-                    for (int p = 0; p < 4; ++p)
-                        *reinterpret_cast<uint4 *>(it.lo + block + in_block(r & 63, (c0 & 63) + 8 * p)) =
-                            make_uint4(l[4 * p], l[4 * p + 1], l[4 * p + 2], l[4 * p + 3]);
-                } else if ((c0 >> 7) < t.i) {
-                    // the mirror image
-                    const size_t mirror = block_at(c0 >> 6, r >> 6, it.rb);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        to[mirror + in_block((c0 & 63) + j, r & 63)] = (uint16_t)((j & 1) ? h[j >> 1] >> 16 : h[j >> 1] & 0xFFFFu);
-                }
-            }
+            dump_sums(tmem + ((uint32_t)(32 * q) << 16) + 64 * half, sm->sums[w]);
             tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm->acc_empty[lu & 1]);
         }
+        __syncwarp();
+        if (split == 1 && !*abort_flag) {
+            if (PHASE == kApply) finish_apply(it, P, sm->sums[w], r0, c0);
+            else finish_symmetric<PHASE>(it, P, OwnSums{sm->sums[w]}, r0, c0, j < i, 0, 1);
+        }
+    }
+    __syncwarp();
+    if (PHASE != kApply) {
+        cluster_sync();
+        if (warp >= 2 && live && split > 1) {
+            const uint32_t first = cluster_rank() & ~(uint32_t)(split - 1);
+            finish_symmetric<PHASE>(it, P, ClusterSums{smem_u32(sm->sums[w]), first, split}, r0, c0, j < i, me, split);
+        }
+        __syncwarp();
+        cluster_sync();                                // no block's memory goes while another reads it
     }
 
     tc_fence_before();
     __syncthreads();
     if (sm->abort_flag) {
         // copies and products in flight end well within this
-        for (int i = 0; i < 64; ++i) __nanosleep(1000);
+        for (int k = 0; k < 64; ++k) __nanosleep(1000);
         __syncthreads();
     }
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(128u) : "memory");
     }
 }
 
@@ -474,24 +872,39 @@ size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Shape {
     int64_t m, n, rb, cb, parts;
-    bool fits;
+    bool fits, sym_pair, apply_pair;
 };
 constexpr int64_t kMaxShort = 32768, kMaxLong = 1 << 24;
+// How a matrix is served goes by its own sizes alone, so it has the same bits in every batch.
 Shape shape_of(int64_t rows, int64_t cols)
 {
-    Shape s;
+    Shape s = {};
     s.m = std::min(rows, cols);
     s.n = std::max(rows, cols);
     s.fits = s.m <= kMaxShort && s.n <= kMaxLong;
-    s.rb = (s.m + 127) / 128 * 2;
-    s.cb = (s.n + 63) / 64;
-    s.parts = s.fits ? std::max<int64_t>(1, std::min<int64_t>(kMaxParts, (s.m * s.n + kPartElements - 1) / kPartElements)) : 0;
+    if (!s.fits || s.m == 0) return s;
+    const int64_t m256 = (s.m + 255) / 256, n256 = (s.n + 255) / 256, m128 = (s.m + 127) / 128;
+    s.sym_pair = m256 > 8;
+    s.apply_pair = m256 * n256 >= 40;
+    const bool wide = s.sym_pair || s.apply_pair;
+    s.rb = wide ? 4 * m256 : 2 * m128;
+    s.cb = wide ? 4 * n256 : (s.n + 127) / 128 * 2;
+    s.parts = std::max<int64_t>(1, std::min<int64_t>(kMaxParts, (s.m * s.n + kPartElements - 1) / kPartElements));
     return s;
+}
+// Blocks that share a tile of a symmetric product of m rows whose reduction is k long: as many as one round of the GPU takes, four
+// reduction blocks each at least.
+int split_of(int64_t m, int64_t k)
+{
+    const int64_t tiles = ((m + 127) / 128) * ((m + 127) / 128 + 1) / 2, kb = (k + 63) / 64;
+    int split = 1;
+    while (split < kMaxSplit && 2 * split * tiles <= 160 && 8 * split <= kb) split *= 2;
+    return split;
 }
 size_t scratch_bytes(const Shape &s)
 {
     if (s.m == 0) return 0;
-    return 3 * (size_t)(s.rb * s.cb) * kBlockBytes + 2 * (size_t)(s.rb * s.rb) * kBlockBytes + (2 + 2 * (size_t)s.cb) * (size_t)s.rb * 64 * sizeof(float) +
+    return 3 * (size_t)(s.rb * s.cb) * kBlockBytes + 2 * (size_t)(s.rb * s.rb) * kBlockBytes + (2 + (size_t)s.cb) * (size_t)s.rb * 64 * sizeof(float) +
            align256((size_t)s.parts * sizeof(double));
 }
 // Points an item at its scratch and returns what comes after it.
@@ -506,53 +919,136 @@ char *place(NsItem &it, const Shape &s, char *p)
     it.B = reinterpret_cast<uint16_t *>(take(as));
     it.alpha = reinterpret_cast<float *>(take((size_t)s.rb * 64 * sizeof(float)));
     it.beta = reinterpret_cast<float *>(take((size_t)s.rb * 64 * sizeof(float)));
-    it.squares = reinterpret_cast<float *>(take(2 * (size_t)s.cb * (size_t)s.rb * 64 * sizeof(float)));
+    it.squares = reinterpret_cast<float *>(take((size_t)s.cb * (size_t)s.rb * 64 * sizeof(float)));
     it.part = reinterpret_cast<double *>(take(align256((size_t)s.parts * sizeof(double))));
     it.m = (int)s.m; it.n = (int)s.n; it.rb = (int)s.rb; it.cb = (int)s.cb; it.parts = (int)s.parts;
+    it.sym_pair = s.sym_pair; it.apply_pair = s.apply_pair;
     it.count = s.m * s.n;
     return p;
 }
 
-template <int PHASE> int launch_product(NsParams &P, int units, const twn_device_info &dev, cudaStream_t s)
+// The matrices of P that a kernel serves, `units` of each in one list: by falling split, so that no tile's blocks straddle two
+// clusters, then longest reductions first, so that the last tiles are short ones.
+template <typename Pick, typename Split, typename Units> bool select(const NsParams &P, NsParams &to, Pick pick, Split split, Units units)
 {
-    static bool attr_set[64] = {false};
-    const int smem = (int)sizeof(NsSmem) + 1024;
-    if (!attr_set[dev.ordinal]) {
-        TWN_CUDA_OK(cudaFuncSetAttribute(ns_product_kernel<PHASE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-        attr_set[dev.ordinal] = true;
+    memcpy(reinterpret_cast<char *>(&to) + sizeof(to.item), reinterpret_cast<const char *>(&P) + sizeof(P.item), sizeof(P) - sizeof(P.item));
+    to.count = 0;
+    for (int t = 0; t < P.count; ++t) {
+        if (!pick(P.item[t])) continue;
+        NsItem &it = to.item[to.count++];
+        it = P.item[t];
+        it.split = split(it);
     }
-    P.units = units;
-    TWN_CUDA_OK(twn_launch_pdl(true, ns_product_kernel<PHASE>, std::min(units, dev.sm_count), kNsThreads, (size_t)smem, s, P));
+    std::sort(to.item, to.item + to.count, [](const NsItem &a, const NsItem &b) {
+        return a.split != b.split ? a.split > b.split : a.n != b.n ? a.n > b.n : a.m > b.m;
+    });
+    int64_t first = 0;
+    for (int t = 0; t < to.count; ++t) {
+        to.item[t].first = (int)first;
+        first += units(to.item[t]) * to.item[t].split;
+        if (first >= 1ll << 31) return false;
+    }
+    to.units = (int)first;
+    return true;
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_clusters(void (*kernel)(KArgs...), int grid, int cluster, size_t smem, cudaStream_t s, const Args &...args)
+{
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kNsThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+template <typename Kernel> int allow_smem(Kernel kernel, size_t bytes, bool &done)
+{
+    if (!done) TWN_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    done = true;
+    return TWN_OK;
+}
+template <int PHASE> int launch_pair(const NsParams &P, const CUtensorMap (&map)[2], const twn_device_info &dev, cudaStream_t s)
+{
+    static bool done[64] = {false};
+    const size_t smem = sizeof(PairSmem) + 1024;
+    const int rc = allow_smem(ns_pair_kernel<PHASE>, smem, done[dev.ordinal]);
+    if (rc != TWN_OK) return rc;
+    TWN_CUDA_OK(launch_clusters(ns_pair_kernel<PHASE>, 2 * std::min(P.units, dev.sm_count / 2), 2, smem, s, map[0], map[1], P));
+    return TWN_OK;
+}
+template <int PHASE> int launch_tile(const NsParams &P, const twn_device_info &dev, cudaStream_t s)
+{
+    static bool done[64] = {false};
+    const size_t smem = sizeof(TileSmem) + 1024;
+    const int rc = allow_smem(ns_tile_kernel<PHASE>, smem, done[dev.ordinal]);
+    if (rc != TWN_OK) return rc;
+    int cluster = 1;
+    if (PHASE != kApply)
+        for (int t = 0; t < P.count; ++t) cluster = std::max(cluster, P.item[t].split);
+    TWN_CUDA_OK(launch_clusters(ns_tile_kernel<PHASE>, (P.units + cluster - 1) / cluster * cluster, cluster, smem, s, P));
     return TWN_OK;
 }
 
-// The items of P are placed; longest reductions first, so that the last tiles are short ones.
-int run_steps(NsParams &P, int steps, cudaStream_t s)
+// All blocks of the workspace as one matrix of 128-byte rows, in copies of 128 and of 64 of them.
+int make_maps(CUtensorMap (&map)[2], void *base, size_t bytes)
 {
-    std::sort(P.item, P.item + P.count, [](const NsItem &a, const NsItem &b) { return a.n != b.n ? a.n > b.n : a.m > b.m; });
-    int64_t parts = 0, blocks = 0, sym = 0, apply = 0;
-    for (int t = 0; t < P.count; ++t) {
-        NsItem &it = P.item[t];
-        it.part_first = (int)parts; it.block_first = (int)blocks; it.sym_first = (int)sym; it.apply_first = (int)apply;
-        const int64_t pairs = it.rb / 2, p = pairs / 2;
-        parts += it.parts;
-        blocks += (int64_t)it.rb * it.cb;
-        sym += p * (p + 1) + (pairs % 2 ? p + 1 : 0);
-        apply += pairs * ((it.cb + 3) / 4);
+    auto encode = twn_detail::encode_fn();
+    TWN_REQUIRE(encode != nullptr, TWN_ERR_CUDA);
+    const cuuint64_t dims[2] = {64, (cuuint64_t)(bytes / 128)}, strides[1] = {128};
+    const cuuint32_t ones[2] = {1, 1};
+    for (int k = 0; k < 2; ++k) {
+        const cuuint32_t box[2] = {64, k == 0 ? 128u : 64u};
+        TWN_REQUIRE(encode(&map[k], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS,
+                    TWN_ERR_CUDA);
     }
-    TWN_REQUIRE(blocks < (1ll << 31), TWN_ERR_TOO_LARGE);
+    return TWN_OK;
+}
+
+// The items of P are placed from `base` on, within `bytes`.
+int run_steps(NsParams &P, int steps, char *base, size_t bytes, cudaStream_t s)
+{
+    P.base = reinterpret_cast<const uint16_t *>(base);
+    enum { kNorm, kStartList, kSymPair, kGramTile, kSquareTile, kApplyPair, kApplyTile, kLists };
+    NsParams list[kLists];
+    auto all = [](const NsItem &) { return true; };
+    auto sym_pair = [](const NsItem &it) { return it.sym_pair != 0; };
+    auto sym_tile = [](const NsItem &it) { return it.sym_pair == 0; };
+    auto one = [](const NsItem &) { return 1; };
+    auto triangle = [](int64_t n) { return n * (n + 1) / 2; };
+    auto tiles = [&](const NsItem &it) { return triangle(it.rb / 2); };
+    const bool fits = select(P, list[kNorm], all, one, [](const NsItem &it) { return (int64_t)it.parts; }) &&
+        select(P, list[kStartList], all, one, [](const NsItem &it) { return (int64_t)it.rb * it.cb; }) &&
+        select(P, list[kSymPair], sym_pair, one, [&](const NsItem &it) { return triangle(it.rb / 4); }) &&
+        select(P, list[kGramTile], sym_tile, [](const NsItem &it) { return split_of(it.m, it.n); }, tiles) &&
+        select(P, list[kSquareTile], sym_tile, [](const NsItem &it) { return split_of(it.m, it.m); }, tiles) &&
+        select(P, list[kApplyPair], [](const NsItem &it) { return it.apply_pair != 0; }, one, [](const NsItem &it) { return (int64_t)(it.rb / 4) * (it.cb / 4); }) &&
+        select(P, list[kApplyTile], [](const NsItem &it) { return it.apply_pair == 0; }, one, [](const NsItem &it) { return (int64_t)(it.rb / 2) * (it.cb / 2); });
+    TWN_REQUIRE(fits && bytes / 128 < (1ull << 31), TWN_ERR_TOO_LARGE);
     twn_device_info dev;
     int rc = twn_current_device(&dev);
     if (rc != TWN_OK) return rc;
-    P.units = (int)parts;
-    TWN_CUDA_OK(twn_launch_small(ns_norm_kernel, (int)std::min<int64_t>(parts, 148 * 8), kSweepBlock, 0, s, P));
-    P.units = (int)blocks;
-    TWN_CUDA_OK(twn_launch_small(ns_start_kernel, (int)std::min<int64_t>(blocks, 148 * 8), kSweepBlock, 0, s, P));
-    for (P.step = 0; P.step < steps; ++P.step) {
-        P.last = P.step + 1 == steps;
-        if ((rc = launch_product<kGram>(P, (int)sym, dev, s)) != TWN_OK) return rc;
-        if ((rc = launch_product<kSquare>(P, (int)sym, dev, s)) != TWN_OK) return rc;
-        if ((rc = launch_product<kApply>(P, (int)apply, dev, s)) != TWN_OK) return rc;
+    CUtensorMap map[2];
+    if (list[kSymPair].count + list[kApplyPair].count > 0 && (rc = make_maps(map, base, bytes)) != TWN_OK) return rc;
+    TWN_CUDA_OK(twn_launch_small(ns_norm_kernel, std::min(list[kNorm].units, dev.sm_count * 8), kSweepBlock, 0, s, list[kNorm]));
+    TWN_CUDA_OK(twn_launch_small(ns_start_kernel, std::min(list[kStartList].units, dev.sm_count * 8), kSweepBlock, 0, s, list[kStartList]));
+    for (int step = 0; step < steps; ++step) {
+        for (NsParams &l : list) { l.step = step; l.last = step + 1 == steps; }
+        if (list[kSymPair].count && (rc = launch_pair<kGram>(list[kSymPair], map, dev, s)) != TWN_OK) return rc;
+        if (list[kGramTile].count && (rc = launch_tile<kGram>(list[kGramTile], dev, s)) != TWN_OK) return rc;
+        if (list[kSymPair].count && (rc = launch_pair<kSquare>(list[kSymPair], map, dev, s)) != TWN_OK) return rc;
+        if (list[kSquareTile].count && (rc = launch_tile<kSquare>(list[kSquareTile], dev, s)) != TWN_OK) return rc;
+        if (list[kApplyPair].count && (rc = launch_pair<kApply>(list[kApplyPair], map, dev, s)) != TWN_OK) return rc;
+        if (list[kApplyTile].count && (rc = launch_tile<kApply>(list[kApplyTile], dev, s)) != TWN_OK) return rc;
     }
     return TWN_OK;
 }
@@ -608,14 +1104,17 @@ extern "C" int twn_orthogonalize_batch(const twn_orthogonalize_item_t *items, in
         it.G = in.G; it.O = in.O;
         it.g_bf16 = in.g_dtype == TWN_BF16; it.o_bf16 = in.o_dtype == TWN_BF16;
         it.tall = in.rows > in.cols;
+        it.vec_in = twn_aligned(in.G, 16);
+        it.vec_out = twn_aligned(in.O, 16) && in.cols % 8 == 0;      // rows of O on 16-byte boundaries, in runs of eight
         it.out_scale = 1.0f;
     }
-    TWN_REQUIRE(workspace_bytes >= twn_orthogonalize_workspace_bytes(items, count), TWN_ERR_WORKSPACE);
+    const size_t need = twn_orthogonalize_workspace_bytes(items, count);
+    TWN_REQUIRE(workspace_bytes >= need, TWN_ERR_WORKSPACE);
     TWN_REQUIRE(twn_aligned(workspace, 256) && twn_aligned(dev_status, 4), TWN_ERR_MISALIGNED);
     if (P.count == 0) return TWN_OK;
     P.eps = (float)eps;
     P.status = dev_status;
-    return run_steps(P, steps, twn_cu(stream));
+    return run_steps(P, steps, static_cast<char *>(workspace), need, twn_cu(stream));
 }
 
 extern "C" size_t twn_muon_workspace_bytes(const twn_muon_item_t *items, int count)
@@ -654,20 +1153,23 @@ extern "C" int twn_muon_update_batch(const twn_muon_item_t *items, int count, fl
         it.dW = in.dW; it.V = in.V; it.O = p;
         p += align256((size_t)(s.m * s.n) * sizeof(float));
         it.tall = in.rows > in.cols;
+        it.vec_in = 1;
+        it.vec_out = in.cols % 8 == 0;
         it.out_scale = in.rows > in.cols ? (float)std::sqrt((double)in.rows / (double)in.cols) : 1.0f;
         // the update with the orthogonalised matrix as gradient and no momentum; that sweep's V is the matrix itself,
         // every element of which it reads before it writes it
         apply[t].dW = static_cast<const float *>(it.O);
         apply[t].V = static_cast<float *>(it.O);
     }
-    TWN_REQUIRE(workspace_bytes >= twn_muon_workspace_bytes(items, count), TWN_ERR_WORKSPACE);
+    const size_t need = twn_muon_workspace_bytes(items, count);
+    TWN_REQUIRE(workspace_bytes >= need, TWN_ERR_WORKSPACE);
     TWN_REQUIRE(twn_aligned(workspace, 256) && twn_aligned(dev_status, 4), TWN_ERR_MISALIGNED);
     P.eps = (float)eps;
     P.momentum = momentum;
     P.look_ahead = look_ahead;
     P.status = dev_status;
     if (P.count > 0) {
-        const int rc = run_steps(P, steps, twn_cu(stream));
+        const int rc = run_steps(P, steps, static_cast<char *>(workspace), need, twn_cu(stream));
         if (rc != TWN_OK) return rc;
     }
     return twn_sgd_update_batch(apply, count, lr, 0.0f, weight_decay, delta_factor, sweep_ws, sweep_bytes, stream);
