@@ -28,7 +28,7 @@
 //                    feed from L2, about 57 bytes a cycle and SM: a single block's 128x256 tile needs 94 at the rate
 //                    of the tensor core and took 850 cycles for a reduction of 64, a pair needs 64.
 //   ns_tile_kernel   a 128x128 tile a block, two blocks on an SM: small products; the reduction of a symmetric
-//                    one may be split over up to eight blocks of a cluster, whose sums meet through distributed shared memory.
+//                    one may be split over up to four blocks of a cluster, whose sums meet through distributed shared memory.
 // The epilogues are the same: a warp has 32 rows by 64 columns in shared memory in fp32, walks them four rows at a time, so
 // that what it reads and writes in the blocks is 512 bytes in a row, and writes the mirror image from the transposed reads.
 #include <algorithm>
@@ -52,7 +52,7 @@ constexpr int kOpBytes = 2 * kBlockBytes, kStageBytes = 2 * kOpBytes;     // 128
 constexpr int kPairStages = 5, kTileStages = 3;
 constexpr int kEpiWarps = 8, kWarpTile = 32 * 64;
 constexpr int kNsThreads = 32 * (2 + kEpiWarps);
-constexpr int kMaxSplit = 8;                 // blocks of a cluster
+constexpr int kMaxSplit = 4;                 // blocks that share a tile's reduction: a cluster
 constexpr int kMaxParts = 512;               // of a matrix's sum of squares
 constexpr long long kPartElements = 8192;
 constexpr int kSweepBlock = 256;
@@ -338,12 +338,6 @@ __device__ __forceinline__ float4 ld_block(uint32_t cluster_addr)
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
     return v;
 }
-__device__ __forceinline__ float ld_block1(uint32_t cluster_addr)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
-    return v;
-}
 __device__ __forceinline__ uint32_t cluster_rank()
 {
     uint32_t r;
@@ -353,6 +347,12 @@ __device__ __forceinline__ uint32_t cluster_rank()
 __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
+// Without waiting for what this block has written.
+__device__ __forceinline__ void cluster_done()
+{
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
 }
 
@@ -376,100 +376,233 @@ __device__ __forceinline__ void dump_sums(uint32_t taddr, float *buf)
     }
 }
 
-// The sums of a warp's tile: in its own buffer, or spread over the blocks of a cluster, added in their order.
-struct OwnSums {
-    const float *buf;
-    __device__ __forceinline__ void row8(int r, int p, float (&v)[8]) const
-    {
-        const float4 a = *reinterpret_cast<const float4 *>(buf + slot_of(r, p, 0)), b = *reinterpret_cast<const float4 *>(buf + slot_of(r, p, 1));
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    }
-    __device__ __forceinline__ void column8(int r, int c, float (&v)[8]) const      // rows r .. r + 7
-    {
+__device__ __forceinline__ void row_sums8(const float *buf, int r, int p, float (&v)[8])
+{
+    const float4 a = *reinterpret_cast<const float4 *>(buf + slot_of(r, p, 0)), b = *reinterpret_cast<const float4 *>(buf + slot_of(r, p, 1));
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void column_sums8(const float *buf, int r, int c, float (&v)[8])      // rows r .. r + 7
+{
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = buf[slot_of(r + e, c >> 3, (c >> 2) & 1) + (c & 3)];
+    for (int e = 0; e < 8; ++e) v[e] = buf[slot_of(r + e, c >> 3, (c >> 2) & 1) + (c & 3)];
+}
+__device__ __forceinline__ void load8(const float *p, float (&v)[8])
+{
+    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+
+// The diagonal of A for a warp's rows: the sums of squares of whole rows of X.
+__device__ __forceinline__ void write_alpha(const NsItem &it, float unscale, int r)
+{
+    float a = 0.0f;
+#pragma unroll 16
+    for (int g = 0; g < it.cb; ++g) a += it.squares[(size_t)g * (64 * it.rb) + r];
+    it.alpha[r] = a * unscale;
+}
+__device__ __forceinline__ float of_square(float sum, float a, float alphas) { return kB * a + kC * (sum + alphas * a); }
+__device__ __forceinline__ float of_diagonal(float sum, float alpha) { return kB * alpha + kC * (sum + alpha * alpha); }
+
+// Where a lane's pieces of a warp's tile lie: unit u has row r0 + 4 u + lane / 8, piece lane % 8 (an odd unit's row has the other
+// bit 2, which the swizzle exchanges); of the mirror image row c0 + 8 u + lane / 4, piece lane % 4 of the warp's four.
+struct Pieces {
+    size_t even;
+    __device__ __forceinline__ Pieces(const NsItem &it, int r0, int c0)
+    {
+        const int lane = threadIdx.x & 31;
+        even = block_at(r0 >> 6, c0 >> 6, it.rb) + in_block((r0 & 63) + (lane >> 3), 8 * (lane & 7));
+    }
+    __device__ __forceinline__ size_t operator()(int u) const { return (u & 1 ? even ^ 32 : even) + 256 * u; }
+};
+__device__ __forceinline__ size_t mirror_piece(const NsItem &it, int r0, int c0)
+{
+    const int lane = threadIdx.x & 31;
+    return block_at(c0 >> 6, r0 >> 6, it.rb) + in_block(lane >> 2, (r0 & 63) + 8 * (lane & 3));
+}
+
+// What a warp's tile of rows r0 .. r0 + 31 and columns c0 .. c0 + 63 reads from global memory, eight units of four rows: loaded
+// before the sums are there.
+template <int PHASE> struct Ahead;
+template <> struct Ahead<kGram> {
+    __device__ __forceinline__ void load(const NsItem &, const NsParams &, int, int) {}
+};
+template <> struct Ahead<kSquare> {
+    uint4 a[8];
+    float row[8], column[8];
+    __device__ __forceinline__ void load(const NsItem &it, const NsParams &, int r0, int c0)
+    {
+        const int lane = threadIdx.x & 31;
+        const uint16_t *const A = it.A;
+        const float *const alpha = it.alpha + r0 + (lane >> 3);
+        const Pieces at(it, r0, c0);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            a[u] = *reinterpret_cast<const uint4 *>(A + at(u));
+            row[u] = alpha[4 * u];
+        }
+        load8(it.alpha + c0 + 8 * (lane & 7), column);
     }
 };
-struct ClusterSums {
-    uint32_t addr, first;        // the buffer's address; rank of the first block that shares the tile
-    int split;
-    __device__ __forceinline__ void row8(int r, int p, float (&v)[8]) const
+template <> struct Ahead<kApply> {
+    uint4 hi[4], lo[4];          // of the first four units
+    float row[8];
+    __device__ __forceinline__ void load4(const NsItem &it, const NsParams &P, int r0, int c0, int u0)
     {
+        const uint16_t *const x = it.x[P.step & 1], *const rest = it.lo;
+        const Pieces at(it, r0, c0);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-#pragma unroll 4
-        for (int g = 0; g < split; ++g) {
-            const uint32_t at = of_block(addr, first + g);
-            const float4 a = ld_block(at + 4 * slot_of(r, p, 0)), b = ld_block(at + 4 * slot_of(r, p, 1));
-            v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+        for (int u = 0; u < 4; ++u) {
+            hi[u] = *reinterpret_cast<const uint4 *>(x + at(u0 + u));
+            lo[u] = *reinterpret_cast<const uint4 *>(rest + at(u0 + u));
         }
     }
-    __device__ __forceinline__ void column8(int r, int c, float (&v)[8]) const
+    __device__ __forceinline__ void load(const NsItem &it, const NsParams &P, int r0, int c0)
     {
+        load4(it, P, r0, c0, 0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-#pragma unroll 2
-        for (int g = 0; g < split; ++g) {
-            const uint32_t at = of_block(addr, first + g);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += ld_block1(at + 4 * (slot_of(r + e, c >> 3, (c >> 2) & 1) + (c & 3)));
-        }
+        for (int u = 0; u < 8; ++u) row[u] = (it.beta + r0 + ((threadIdx.x & 31) >> 3))[4 * u];
     }
 };
 
-// Symmetric products: the warp's tile from row r0 and column c0 on, and its mirror image; of its eight units of work those
-// that are `me` modulo `split`.
-template <int PHASE, typename Sums>
-__device__ __forceinline__ void finish_symmetric(const NsItem &it, const NsParams &P, const Sums &sums, int r0, int c0, bool mirror, int me, int split)
+// Symmetric products: a warp's tile and its mirror image.
+template <int PHASE>
+__device__ __forceinline__ void finish_symmetric(const NsItem &it, const NsParams &P, const Ahead<PHASE> &ahead, const float *buf, int r0, int c0, bool mirror)
 {
     const int lane = threadIdx.x & 31;
     const bool diagonal = r0 >= c0 && r0 < c0 + 64;
     const float unscale = P.step == 0 ? 1.0f / (kStart * kStart) : 1.0f;
     uint16_t *const to = PHASE == kGram ? it.A : it.B;
-    if (PHASE == kGram && diagonal && me == 0) {
-        float a = 0.0f;
-#pragma unroll 16
-        for (int g = 0; g < it.cb; ++g) a += it.squares[(size_t)g * (64 * it.rb) + r0 + lane];
-        it.alpha[r0 + lane] = a * unscale;
-    }
-    auto eight = [&](int r, int c, float (&v)[8]) {              // row r, columns c ..: sums to elements
-        if (PHASE == kGram) {
+    if (PHASE == kGram && diagonal) write_alpha(it, unscale, r0 + lane);
+    const int p = lane & 7;
+    const Pieces at(it, r0, c0);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        const int r = 4 * u + (lane >> 3);
+        float v[8];
+        row_sums8(buf, r, p, v);
+        if constexpr (PHASE == kSquare) {
+            float a[8];
+            unpack_half8(ahead.a[u], a);
+            if (diagonal)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c0 + 8 * p + j == r0 + r) it.beta[r0 + r] = of_diagonal(v[j], ahead.row[u]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = of_square(v[j], a[j], ahead.row[u] + ahead.column[j]);
+        } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] *= unscale;
-        } else {
-            float a[8];
-            unpack_half8(*reinterpret_cast<const uint4 *>(it.A + piece_at(r, c, it.rb)), a);
-            const float ar = it.alpha[r];
-            const float4 a0 = *reinterpret_cast<const float4 *>(it.alpha + c), a1 = *reinterpret_cast<const float4 *>(it.alpha + c + 4);
-            const float ac[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (c + j == r) it.beta[r] = kB * ar + kC * (v[j] + ar * ar);
-                v[j] = kB * a[j] + kC * (v[j] + (ar + ac[j]) * a[j]);
-            }
         }
-    };
-#pragma unroll 2
-    for (int u = me; u < 8; u += split) {
-        const int r = 4 * u + (lane >> 3), p = lane & 7;
-        float v[8];
-        sums.row8(r, p, v);
-        eight(r0 + r, c0 + 8 * p, v);
         if (diagonal)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (c0 + 8 * p + j == r0 + r) v[j] = 0.0f;
-        *reinterpret_cast<uint4 *>(to + piece_at(r0 + r, c0 + 8 * p, it.rb)) = pack_half8(v);
+        *reinterpret_cast<uint4 *>(to + at(u)) = pack_half8(v);
     }
     if (!mirror) return;
-#pragma unroll 2
-    for (int u = me; u < 8; u += split) {
-        const int c = 8 * u + (lane >> 2), r = 8 * (lane & 3);
+    const int r = 8 * (lane & 3);
+    const size_t mirrored = mirror_piece(it, r0, c0);
+    float alpha_r[8];
+    if (PHASE == kSquare) load8(it.alpha + r0 + r, alpha_r);
+#pragma unroll 4
+    for (int u = 0; u < 8; ++u) {
+        const int c = 8 * u + (lane >> 2);
+        const size_t at = mirrored + 512 * u;
         float v[8];
-        sums.column8(r, c, v);
-        eight(c0 + c, r0 + r, v);
-        *reinterpret_cast<uint4 *>(to + piece_at(c0 + c, r0 + r, it.rb)) = pack_half8(v);
+        column_sums8(buf, r, c, v);
+        if constexpr (PHASE == kSquare) {
+            float a[8];
+            unpack_half8(*reinterpret_cast<const uint4 *>(it.A + at), a);
+            const float alpha_c = it.alpha[c0 + c];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = of_square(v[j], a[j], alpha_r[j] + alpha_c);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= unscale;
+        }
+        *reinterpret_cast<uint4 *>(to + at) = pack_half8(v);
     }
+}
+
+// The same where `split` blocks of a cluster, from rank `first` on, hold a part of the sums each at this address.  Of the four runs of
+// eight rows of a warp's tile a block takes those that are `me` modulo `split`: it reads all parts at once, 128 bytes in a row at a time
+// (a row a thread, 16 bytes each from another one, took 7 to 12 us for four blocks), adds them in the blocks' order, and leaves the
+// sum in its own part, which nobody else reads there, for the mirror image.
+template <int PHASE>
+__device__ __forceinline__ void finish_split(const NsItem &it, const NsParams &P, float *buf, uint32_t first, int r0, int c0, bool mirror, int me, int split)
+{
+    const int lane = threadIdx.x & 31, p = lane & 7;
+    const bool diagonal = r0 >= c0 && r0 < c0 + 64;
+    const float unscale = P.step == 0 ? 1.0f / (kStart * kStart) : 1.0f;
+    uint16_t *const to = PHASE == kGram ? it.A : it.B;
+    const uint32_t addr = smem_u32(buf);
+    const Pieces at(it, r0, c0);
+    float alpha_c[8];
+    if (PHASE == kSquare) load8(it.alpha + c0 + 8 * p, alpha_c);
+#pragma unroll 1
+    for (int k = me; k < 4; k += split) {
+        float4 part[kMaxSplit][4];
+        uint4 aw[2];
+        float alpha[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int g = 0; g < kMaxSplit; ++g) {
+            if (g >= split) break;
+            const uint32_t from = of_block(addr, first + g);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) part[g][h] = ld_block(from + 4 * slot_of(8 * k + 4 * (h >> 1) + (lane >> 3), p, h & 1));
+        }
+        if (PHASE == kSquare)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                aw[h] = *reinterpret_cast<const uint4 *>(it.A + at(2 * k + h));
+                alpha[h] = it.alpha[r0 + 8 * k + 4 * h + (lane >> 3)];
+            }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = 8 * k + 4 * h + (lane >> 3);
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = (&part[0][2 * h + (j >> 2)].x)[j & 3];
+#pragma unroll
+            for (int g = 1; g < kMaxSplit; ++g) {
+                if (g >= split) break;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += (&part[g][2 * h + (j >> 2)].x)[j & 3];
+            }
+            if (PHASE == kSquare) {
+                float a[8];
+                unpack_half8(aw[h], a);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (diagonal && c0 + 8 * p + j == r0 + r) it.beta[r0 + r] = of_diagonal(v[j], alpha[h]);
+                    v[j] = of_square(v[j], a[j], alpha[h] + alpha_c[j]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= unscale;
+            }
+            if (diagonal)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c0 + 8 * p + j == r0 + r) v[j] = 0.0f;
+            *reinterpret_cast<uint4 *>(to + at(2 * k + h)) = pack_half8(v);
+            if (mirror) {
+                *reinterpret_cast<float4 *>(buf + slot_of(r, p, 0)) = make_float4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<float4 *>(buf + slot_of(r, p, 1)) = make_float4(v[4], v[5], v[6], v[7]);
+            }
+        }
+        if (mirror) {
+            __syncwarp();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int c = 32 * h + lane;
+                float v[8];
+                column_sums8(buf, 8 * k, c, v);
+                *reinterpret_cast<uint4 *>(to + piece_at(c0 + c, r0 + 8 * k, it.rb)) = pack_half8(v);
+            }
+        }
+    }
+    if (PHASE == kGram && diagonal && me == 0) write_alpha(it, unscale, r0 + lane);
 }
 
 __device__ __forceinline__ void store_out(const NsItem &it, long long at, float v)
@@ -490,21 +623,21 @@ __device__ __forceinline__ void store_out8(const NsItem &it, long long at, const
 }
 
 // X of the next step, or the result.
-__device__ __forceinline__ void finish_apply(const NsItem &it, const NsParams &P, float *buf, int r0, int c0)
+__device__ __forceinline__ void finish_apply(const NsItem &it, const NsParams &P, Ahead<kApply> &ahead, float *buf, int r0, int c0)
 {
     const int lane = threadIdx.x & 31, p = lane & 7, cur = P.step & 1;
     const float unscale = P.step == 0 ? 1.0f / kStart : 1.0f;
-    const OwnSums sums{buf};
-#pragma unroll 4
+    uint16_t *const next = it.x[cur ^ 1], *const rest = it.lo;
+    const Pieces at(it, r0, c0);
+#pragma unroll
     for (int u = 0; u < 8; ++u) {
+        if (u == 4) ahead.load4(it, P, r0, c0, 4);
         const int r = 4 * u + (lane >> 3);
-        const size_t at = piece_at(r0 + r, c0 + 8 * p, it.rb);
-        const uint4 hi = *reinterpret_cast<const uint4 *>(it.x[cur] + at), lo = *reinterpret_cast<const uint4 *>(it.lo + at);
-        const float k = kA + it.beta[r0 + r];
+        const float k = kA + ahead.row[u];
         float v[8], h[8], l[8];
-        sums.row8(r, p, v);
-        unpack_half8(hi, h);
-        unpack_half8(lo, l);
+        row_sums8(buf, r, p, v);
+        unpack_half8(ahead.hi[u & 3], h);
+        unpack_half8(ahead.lo[u & 3], l);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = (k * (h[j] + l[j]) + v[j]) * unscale;
         if (P.last) {
@@ -518,8 +651,8 @@ __device__ __forceinline__ void finish_apply(const NsItem &it, const NsParams &P
             }
         } else {
             const uint4 h2 = pack_half8(v);
-            *reinterpret_cast<uint4 *>(it.x[cur ^ 1] + at) = h2;
-            *reinterpret_cast<uint4 *>(it.lo + at) = pack_rest8(v, h2);
+            *reinterpret_cast<uint4 *>(next + at(u)) = h2;
+            *reinterpret_cast<uint4 *>(rest + at(u)) = pack_rest8(v, h2);
             const float q = row_squares(v);
             if (p == 0) it.squares[(size_t)(c0 >> 6) * (64 * it.rb) + r0 + r] = q;
         }
@@ -531,7 +664,7 @@ __device__ __forceinline__ void finish_apply(const NsItem &it, const NsParams &P
         for (int u = 0; u < 8; ++u) {
             const int c = 8 * u + (lane >> 2), r = 8 * (lane & 3);
             float v[8];
-            sums.column8(r, c, v);
+            column_sums8(buf, r, c, v);
             if (c0 + c < it.n && r0 + r < it.m) store_out8(it, (long long)(c0 + c) * it.m + r0 + r, v);
         }
     } else if (it.tall) {
@@ -693,12 +826,15 @@ ns_pair_kernel(const __grid_constant__ CUtensorMap rows128, const __grid_constan
             const NsItem &it = P.item[item_of(P, u)];
             int I, J;
             tile_of(it, u, I, J);
-            if (!mbar_wait_warp(&sm->acc_full[lu & 1], (lu >> 1) & 1u, abort_flag, P.status, 32)) break;
-            tc_fence_after();
             const int r0 = 256 * I + 128 * (int)rank + 32 * q;
+            bool ok = true;
 #pragma unroll 1
             for (int b = set; b < 4; b += 2) {
                 const int c0 = 256 * J + 64 * b;
+                Ahead<PHASE> ahead;
+                ahead.load(it, P, r0, c0);
+                if (b < 2 && !mbar_wait_warp(&sm->acc_full[lu & 1], (lu >> 1) & 1u, abort_flag, P.status, 32)) { ok = false; break; }
+                tc_fence_after();
                 dump_sums(tmem + ((uint32_t)(32 * q) << 16) + (lu & 1) * 256 + 64 * b, buf);
                 __syncwarp();
                 if (b >= 2) {
@@ -706,10 +842,11 @@ ns_pair_kernel(const __grid_constant__ CUtensorMap rows128, const __grid_constan
                     __syncwarp();
                     if (lane == 0) arrive_at(of_block(smem_u32(&sm->acc_empty[lu & 1]), 0));
                 }
-                if (PHASE == kApply) finish_apply(it, P, buf, r0, c0);
-                else finish_symmetric<PHASE>(it, P, OwnSums{buf}, r0, c0, J < I, 0, 1);
+                if constexpr (PHASE == kApply) finish_apply(it, P, ahead, buf, r0, c0);
+                else finish_symmetric<PHASE>(it, P, ahead, buf, r0, c0, J < I);
                 __syncwarp();
             }
+            if (!ok) break;
         }
     }
 
@@ -742,7 +879,7 @@ struct __align__(1024) TileSmem {
 };
 
 template <int PHASE>
-__global__ void __launch_bounds__(kNsThreads, 2) ns_tile_kernel(const __grid_constant__ NsParams P)
+__global__ void __launch_bounds__(kNsThreads, 2) ns_tile_kernel(const __grid_constant__ NsParams P, bool clustered)
 {
     pdl_launch_dependents();
     extern __shared__ uint8_t smem_raw[];
@@ -760,13 +897,8 @@ __global__ void __launch_bounds__(kNsThreads, 2) ns_tile_kernel(const __grid_con
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(128u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    pdl_wait();
-    const uint32_t tmem = sm->tmem_base;
+    // the tile's place needs the parameters alone: read while the kernel before this one ends
     const int cur = P.step & 1;
-
     const int u = blockIdx.x;
     const bool live = u < P.units;
     const NsItem &it = P.item[item_of(P, live ? u : 0)];
@@ -787,11 +919,16 @@ __global__ void __launch_bounds__(kNsThreads, 2) ns_tile_kernel(const __grid_con
         k1 = (int)((long long)kb * (me + 1) / split);
     }
     const bool same = PHASE != kApply && i == j;       // the same rows on both sides
+    const uint16_t *const src_a = PHASE == kGram ? it.x[cur] : PHASE == kSquare ? it.A : it.B;
+    const uint16_t *const src_b = PHASE == kSquare ? it.A : it.x[cur];
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();
+    const uint32_t tmem = sm->tmem_base;
 
     if (warp == 0) {
         if (elect_one()) {
-            const uint16_t *const src_a = PHASE == kGram ? it.x[cur] : PHASE == kSquare ? it.A : it.B;
-            const uint16_t *const src_b = PHASE == kSquare ? it.A : it.x[cur];
             uint32_t s = 0, ph = 0;
             for (int k = k0; k < k1; ++k) {
                 uint8_t *const st = sm->ring[s];
@@ -831,27 +968,29 @@ __global__ void __launch_bounds__(kNsThreads, 2) ns_tile_kernel(const __grid_con
     const int w = warp - 2, q = warp & 3, half = w >> 2;
     const int r0 = 128 * i + 32 * q, c0 = 128 * j + 64 * half;
     if (warp >= 2 && live) {
+        Ahead<PHASE> ahead;
+        if (split == 1) ahead.load(it, P, r0, c0);
         // all products are done, so all copies have landed: the ring is free
         if (mbar_wait_warp(&sm->acc_full, 0u, abort_flag, P.status, 32)) {
             tc_fence_after();
             dump_sums(tmem + ((uint32_t)(32 * q) << 16) + 64 * half, sm->sums[w]);
             tc_fence_before();
-        }
-        __syncwarp();
-        if (split == 1 && !*abort_flag) {
-            if (PHASE == kApply) finish_apply(it, P, sm->sums[w], r0, c0);
-            else finish_symmetric<PHASE>(it, P, OwnSums{sm->sums[w]}, r0, c0, j < i, 0, 1);
+            __syncwarp();
+            if (split == 1) {
+                if constexpr (PHASE == kApply) finish_apply(it, P, ahead, sm->sums[w], r0, c0);
+                else finish_symmetric<PHASE>(it, P, ahead, sm->sums[w], r0, c0, j < i);
+            }
         }
     }
     __syncwarp();
-    if (PHASE != kApply) {
-        cluster_sync();
-        if (warp >= 2 && live && split > 1) {
-            const uint32_t first = cluster_rank() & ~(uint32_t)(split - 1);
-            finish_symmetric<PHASE>(it, P, ClusterSums{smem_u32(sm->sums[w]), first, split}, r0, c0, j < i, me, split);
+    if constexpr (PHASE != kApply) {
+        if (clustered) {
+            cluster_sync();
+            if (warp >= 2 && live && split > 1)
+                finish_split<PHASE>(it, P, sm->sums[w], cluster_rank() & ~(uint32_t)(split - 1), r0, c0, j < i, me, split);
+            __syncwarp();
+            cluster_done();                            // no block's memory goes while another reads it
         }
-        __syncwarp();
-        cluster_sync();                                // no block's memory goes while another reads it
     }
 
     tc_fence_before();
@@ -885,7 +1024,7 @@ Shape shape_of(int64_t rows, int64_t cols)
     if (!s.fits || s.m == 0) return s;
     const int64_t m256 = (s.m + 255) / 256, n256 = (s.n + 255) / 256, m128 = (s.m + 127) / 128;
     s.sym_pair = m256 > 8;
-    s.apply_pair = m256 * n256 >= 40;
+    s.apply_pair = m256 * n256 >= 32;
     const bool wide = s.sym_pair || s.apply_pair;
     s.rb = wide ? 4 * m256 : 2 * m128;
     s.cb = wide ? 4 * n256 : (s.n + 127) / 128 * 2;
@@ -893,12 +1032,12 @@ Shape shape_of(int64_t rows, int64_t cols)
     return s;
 }
 // Blocks that share a tile of a symmetric product of m rows whose reduction is k long: as many as one round of the GPU takes, four
-// reduction blocks each at least.
+// reduction blocks each at least (33 clusters of four run at once).
 int split_of(int64_t m, int64_t k)
 {
     const int64_t tiles = ((m + 127) / 128) * ((m + 127) / 128 + 1) / 2, kb = (k + 63) / 64;
     int split = 1;
-    while (split < kMaxSplit && 2 * split * tiles <= 160 && 8 * split <= kb) split *= 2;
+    while (split < kMaxSplit && 2 * split * tiles <= 132 && 8 * split <= kb) split *= 2;
     return split;
 }
 size_t scratch_bytes(const Shape &s)
@@ -994,7 +1133,7 @@ template <int PHASE> int launch_tile(const NsParams &P, const twn_device_info &d
     int cluster = 1;
     if (PHASE != kApply)
         for (int t = 0; t < P.count; ++t) cluster = std::max(cluster, P.item[t].split);
-    TWN_CUDA_OK(launch_clusters(ns_tile_kernel<PHASE>, (P.units + cluster - 1) / cluster * cluster, cluster, smem, s, P));
+    TWN_CUDA_OK(launch_clusters(ns_tile_kernel<PHASE>, (P.units + cluster - 1) / cluster * cluster, cluster, smem, s, P, cluster > 1));
     return TWN_OK;
 }
 
