@@ -14,6 +14,7 @@
 #include <cuda_bf16.h>
 
 #include "common.cuh"
+#include "tc_ptx.cuh"
 
 namespace {
 
@@ -84,22 +85,62 @@ __device__ __forceinline__ void store(float *p, const float (&f)[8])
 __device__ __forceinline__ void store(float *p, const float (&f)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]); }
 __device__ __forceinline__ void store(float *p, const float (&f)[1]) { *p = f[0]; }
 
-// gamma and beta: fp32, `none` where the caller has none
+// gamma and beta: fp32, `none` where the caller has none.  Loads of read-only data, which the compiler may take ahead of the
+// stores of earlier columns.
 template <int V> __device__ __forceinline__ void load_param(float (&f)[V], const float *p, long long col, float none)
 {
     if (p == nullptr) {
 #pragma unroll
         for (int i = 0; i < V; ++i) f[i] = none;
+    } else if constexpr (V == 1) {
+        f[0] = __ldg(p + col);
     } else {
-        Vec<float, V> v;
-        v.load(p + col);
-        v.get(f);
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const float4 v = __ldg(reinterpret_cast<const float4 *>(p + col + i));
+            f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+        }
     }
 }
 
-// Sums over a team of T threads, the same bits in all of them.  Every thread of the block calls it.  `red` holds N floats for
-// each of 32 warps, twice: a buffer is written again one barrier after all have read it.
-template <int N> __device__ __forceinline__ void team_sum(float (&v)[N], int T, float (*red)[32][2], unsigned int &turn)
+// Two fp32 numbers in one register pair: Blackwell adds, multiplies and fuses both in one instruction.
+typedef unsigned long long two_f32;
+__device__ __forceinline__ two_f32 two(float a, float b)
+{
+    two_f32 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void each(two_f32 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ two_f32 add2(two_f32 a, two_f32 b)
+{
+    two_f32 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ two_f32 mul2(two_f32 a, two_f32 b)
+{
+    two_f32 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ two_f32 fma2(two_f32 a, two_f32 b, two_f32 c)
+{
+    two_f32 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float sum2(two_f32 v)
+{
+    float a, b;
+    each(v, a, b);
+    return a + b;
+}
+
+// Sums over a team of T threads, the same bits in all of them.  Every thread of the team calls it (and of the warp, where that
+// has several teams).  `red` holds two floats for each of 32 warps, twice: a buffer is written again one barrier after all
+// have read it.  `barrier`: the team's own, 0 for a block that is one team.
+template <int N> __device__ __forceinline__ void team_sum(float (&v)[N], int T, float (*red)[32][2], unsigned int &turn, int barrier)
 {
     const int span = min(T, 32);
     for (int o = span >> 1; o > 0; o >>= 1)
@@ -108,21 +149,56 @@ template <int N> __device__ __forceinline__ void team_sum(float (&v)[N], int T, 
     if (T > 32) {
         float(*buf)[2] = red[turn & 1];
         ++turn;
-        const int warp = threadIdx.x >> 5, warps = T >> 5;
-        if ((threadIdx.x & 31) == 0)
-#pragma unroll
-            for (int i = 0; i < N; ++i) buf[warp][i] = v[i];
-        __syncthreads();
-        const int first = warp & ~(warps - 1), lane = threadIdx.x & 31;
-        const bool in = lane < warps;
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = in ? buf[first + lane][i] : 0.0f;
-        for (int o = warps >> 1; o > 0; o >>= 1)
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
+        const int warp = threadIdx.x >> 5, warps = T >> 5, first = warp / warps * warps;
+        if ((threadIdx.x & 31) == 0) *reinterpret_cast<float2 *>(buf[warp]) = make_float2(v[0], N > 1 ? v[N - 1] : 0.0f);
+        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(T) : "memory");
+        v[0] = v[N - 1] = 0.0f;
+#pragma unroll 4
+        for (int w = first; w < first + warps; ++w) {
+            const float2 a = *reinterpret_cast<const float2 *>(buf[w]);
+            v[0] += a.x;
+            if (N > 1) v[N - 1] += a.y;
+        }
     }
+}
+
+// Column of a thread's vector j, and whether the vectors j of the whole team lie inside the row (the same for all threads).  TT: the
+// team's size where it is known at compile time, so that single elements (V = 1) lie at constant offsets of one address; with
+// the offsets worked out for each, a row of 1001 took 85 instructions an element.
+template <int V, int TT> struct Columns {
+    int T_, t, C;
+    __device__ __forceinline__ int T() const { return TT ? TT : T_; }
+    __device__ __forceinline__ int operator()(int j) const { return (j * T() + t) * V; }
+    __device__ __forceinline__ bool whole(int j) const { return (j + 1) * T() * V <= C; }
+};
+// N vectors from j on into raw, nothing past the row's end.
+template <typename T, int V, int TT, int N> __device__ __forceinline__ void load_vectors(Vec<T, V> (&raw)[N], const T *row, const Columns<V, TT> &col, bool live)
+{
+    constexpr int K = N < 8 ? N : 8;
+#pragma unroll
+    for (int j0 = 0; j0 < N; j0 += K) {
+        if (live && col.whole(j0 + K - 1)) {
+#pragma unroll
+            for (int j = j0; j < j0 + K; ++j) raw[j].load(row + col(j));
+        } else {
+#pragma unroll
+            for (int j = j0; j < j0 + K; ++j)
+                if (live && col(j) < col.C) raw[j].load(row + col(j));
+                else raw[j].zero();
+        }
+    }
+}
+template <typename T, int V, int TT> __device__ __forceinline__ void read_vector(const T *row, const Columns<V, TT> &col, int j, float (&f)[V])
+{
+    Vec<T, V> v;
+    if (col.whole(j)) {
+        v.load(row + col(j));
+    } else if (col(j) < col.C) {
+        v.load(row + col(j));
+    } else {
+        v.zero();
+    }
+    v.get(f);
 }
 
 struct FwdParams {
@@ -135,61 +211,100 @@ struct FwdParams {
     int T;
 };
 
-// One row per team, in registers.  C <= T * E.
-template <typename TX, typename TY, int V, int E>
-__global__ void __launch_bounds__(1024) norm_fwd_kernel(const __grid_constant__ FwdParams P)
+// One row per team, in registers.  C <= T * E.  A team of more than a warp is a block.
+template <typename TX, typename TY, int V, int E, int TT>
+__global__ void __launch_bounds__(TT > 32 ? TT : TT == 32 || E < 16 ? 128 : 1024) norm_fwd_kernel(const __grid_constant__ FwdParams P)
 {
-    constexpr int NV = E / V;
-    __shared__ float red[2][32][2];
+    constexpr int NV = E / V, P2 = E / 2;
+    __shared__ __align__(16) float red[2][32][2];
     unsigned int turn = 0;
-    const int T = P.T, t = threadIdx.x & (T - 1);
+    const int T = TT ? TT : P.T, t = threadIdx.x & (T - 1), C = (int)P.C;
     const int teams = blockDim.x / T, team = threadIdx.x / T;
-    const float inv = 1.0f / (float)P.C;
+    const float inv = 1.0f / (float)C;
+    const Columns<V, TT> col{T, t, C};
     pdl_begin();
     for (long long r0 = (long long)blockIdx.x * teams; r0 < P.M; r0 += (long long)gridDim.x * teams) {
         const long long r = r0 + team;
         const bool live = r < P.M;
         const TX *x = static_cast<const TX *>(P.X) + (live ? r : 0) * P.ldx;
         Vec<TX, V> raw[NV];
+        load_vectors(raw, x, col, live);
+        two_f32 d[P2], s2 = 0, q2 = 0;
+        {
+            float f[E];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const long long col = (long long)(j * T + t) * V;
-            if (live && col < P.C) raw[j].load(x + col);
-            else raw[j].zero();
-        }
-        float f[NV][V], s[1] = {0.0f};
+            for (int j = 0; j < NV; ++j) raw[j].get(*reinterpret_cast<float(*)[V]>(f + j * V));
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            raw[j].get(f[j]);
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[0] += f[j][i];
-        }
-        team_sum(s, T, red, turn);
-        const float mean = s[0] * inv;
-        float q[1] = {0.0f};
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const bool in = (long long)(j * T + t) * V < P.C;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                f[j][i] -= mean;
-                if (in) q[0] = fmaf(f[j][i], f[j][i], q[0]);
+            for (int i = 0; i < P2; ++i) {
+                d[i] = two(f[2 * i], f[2 * i + 1]);
+                s2 = add2(s2, d[i]);
             }
         }
-        team_sum(q, T, red, turn);
-        const float rstd = 1.0f / sqrtf(fmaf(q[0], inv, P.eps));
+        float s[1] = {sum2(s2)};
+        team_sum(s, T, red, turn, 0);
+        const float mean = s[0] * inv;
+        const two_f32 minus = two(-mean, -mean);
+#pragma unroll
+        for (int i = 0; i < P2; ++i) d[i] = add2(d[i], minus);
+        // nothing of what is past the row's end
+        constexpr int K = NV < 8 ? NV : 8;
+#pragma unroll
+        for (int j0 = 0; j0 < NV; j0 += K)
+            if (!col.whole(j0 + K - 1))
+#pragma unroll
+                for (int i = j0 * V / 2; i < (j0 + K) * V / 2; ++i) {
+                    if (V > 1) {
+                        if (col(2 * i / V) >= C) d[i] = 0;
+                    } else {
+                        float a, b;
+                        each(d[i], a, b);
+                        d[i] = two(col(2 * i) < C ? a : 0.0f, col(2 * i + 1) < C ? b : 0.0f);
+                    }
+                }
+#pragma unroll
+        for (int i = 0; i < P2; ++i) q2 = fma2(d[i], d[i], q2);
+        float q[1] = {sum2(q2)};
+        team_sum(q, T, red, turn, 0);
+        const float rstd = rsqrtf(fmaf(q[0], inv, P.eps));
         if (!live) continue;
+        const two_f32 scale = two(rstd, rstd);
         TY *y = static_cast<TY *>(P.Y) + r * P.ldy;
+        // K vectors: whole where the team's are, so that their loads of gamma and beta go together
+        auto put = [&](int j, const float(&ga)[V], const float(&be)[V]) {
+            float o[V];
+            if constexpr (V > 1) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const long long col = (long long)(j * T + t) * V;
-            if (col >= P.C) continue;
-            float ga[V], be[V];
-            load_param(ga, P.gamma, col, 1.0f);
-            load_param(be, P.beta, col, 0.0f);
+                for (int i = 0; i < V / 2; ++i)
+                    each(fma2(mul2(d[j * V / 2 + i], scale), two(ga[2 * i], ga[2 * i + 1]), two(be[2 * i], be[2 * i + 1])), o[2 * i], o[2 * i + 1]);
+            } else {
+                float a, b;
+                each(d[j / 2], a, b);
+                o[0] = fmaf((j & 1 ? b : a) * rstd, ga[0], be[0]);
+            }
+            store(y + col(j), o);
+        };
 #pragma unroll
-            for (int i = 0; i < V; ++i) ga[i] = fmaf(f[j][i] * rstd, ga[i], be[i]);
-            store(y + col, ga);
+        for (int j0 = 0; j0 < NV; j0 += K) {
+            const bool whole = col.whole(j0 + K - 1);
+            if (whole && V == 1) {
+                float ga[K][V], be[K][V];
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    load_param(ga[j], P.gamma, col(j0 + j), 1.0f);
+                    load_param(be[j], P.beta, col(j0 + j), 0.0f);
+                }
+#pragma unroll
+                for (int j = 0; j < K; ++j) put(j0 + j, ga[j], be[j]);
+            } else {
+#pragma unroll
+                for (int j = j0; j < j0 + K; ++j) {
+                    if (!whole && col(j) >= C) continue;
+                    float ga[V], be[V];
+                    load_param(ga, P.gamma, col(j), 1.0f);
+                    load_param(be, P.beta, col(j), 0.0f);
+                    put(j, ga, be);
+                }
+            }
         }
         if (t == 0) {
             if (P.mean) P.mean[r] = mean;
@@ -198,11 +313,132 @@ __global__ void __launch_bounds__(1024) norm_fwd_kernel(const __grid_constant__ 
     }
 }
 
+// ---- rows through shared memory ---------------------------------------------------------------------------------------------
+// Large tensors of aligned rows.  With 16 elements a thread, all of them in registers, a row of 4096 took 31 instructions an element,
+// most of them the fixed part of a row: two sums, the barriers, the root, the addresses; with more, few rows fit the registers, and
+// too little is on its way.  Here rows come by bulk copies into a ring in shared memory, up to 200 KB an SM on their way, for threads
+// of up to 64 elements.
+constexpr int kMaxRing = 8, kMaxTeams = 32;
+constexpr size_t kRingBytes = 200 * 1024;
+struct Ring {
+    int stages, stage_bytes, second;         // of a stage: where a second tensor's row begins
+    int params;                              // bytes at the front that hold gamma (and beta), 0: they are read from global memory
+};
+
+// gamma or beta in shared memory: as it is, but for V = 8 the lower and the upper halves of eight apart, so that a warp's 16-byte
+// reads are next to each other.
+template <int V> __device__ __forceinline__ int param_at(int c, int C) { return V == 8 ? (c & 4 ? C / 2 : 0) + (c >> 3) * 4 + (c & 3) : c; }
+template <int V> __device__ __forceinline__ void read_param(const float *sm, const float *global, int c, int C, float none, float (&f)[V])
+{
+    if (sm == nullptr) {
+        load_param(f, global, c, none);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(sm + param_at<V>(c + i, C));
+            f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+        }
+    }
+}
+
+template <int E> constexpr int fwd_ring_threads() { return E >= 64 ? 512 : E >= 32 ? 768 : 1024; }
+
+template <typename TX, typename TY, int V, int E>
+__global__ void __launch_bounds__(fwd_ring_threads<E>(), 1) norm_fwd_ring_kernel(const __grid_constant__ FwdParams P, const __grid_constant__ Ring R)
+{
+    constexpr int NV = E / V, P2 = E / 2;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ unsigned long long full[kMaxTeams][kMaxRing];
+    __shared__ __align__(16) float red[2][32][2];
+    __shared__ volatile int gave_up;
+    unsigned int turn = 0;
+    const int T = P.T, team = threadIdx.x / T, t = threadIdx.x - team * T, C = (int)P.C;
+    const int teams = blockDim.x / T, barrier = teams > 1 ? team + 1 : 0;
+    const float inv = 1.0f / (float)C;
+    const Columns<V, 0> col{T, t, C};
+    if (t == 0)
+        for (int s = 0; s < R.stages; ++s) mbar_init(&full[team][s], 1);
+    if (threadIdx.x == 0) gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncthreads();
+    pdl_begin();
+    uint8_t *const mine = ring + R.params + (size_t)team * R.stages * R.stage_bytes;
+    const long long first = (long long)blockIdx.x * teams + team, step = (long long)gridDim.x * teams;
+    auto issue = [&](long long r, int s) {
+        if (r >= P.M) return;
+        mbar_expect_tx(&full[team][s], C * (uint32_t)sizeof(TX));
+        bulk_load(mine + (size_t)s * R.stage_bytes, static_cast<const TX *>(P.X) + r * P.ldx, C * (uint32_t)sizeof(TX), &full[team][s]);
+    };
+    if (t == 0)
+        for (int s = 0; s < R.stages; ++s) issue(first + s * step, s);
+    float *const gammas = R.params ? reinterpret_cast<float *>(ring) : nullptr, *const betas = R.params ? gammas + C : nullptr;
+    if (R.params) {
+        for (int c = threadIdx.x; c < C; c += blockDim.x) {
+            gammas[param_at<V>(c, C)] = P.gamma ? P.gamma[c] : 1.0f;
+            betas[param_at<V>(c, C)] = P.beta ? P.beta[c] : 0.0f;
+        }
+        __syncthreads();
+    }
+    int s = 0;
+    uint32_t ph = 0;
+    for (long long r = first; r < P.M; r += step) {
+        // a wait that ran out is no row: its results are NaNs
+        const bool ok = mbar_wait(&full[team][s], ph, &gave_up, nullptr, 0);
+        const TX *const row = reinterpret_cast<const TX *>(mine + (size_t)s * R.stage_bytes);
+        two_f32 d[P2], s2 = 0, q2 = 0;
+        {
+            float f[E];
+#pragma unroll
+            for (int j = 0; j < NV; ++j) read_vector(row, col, j, *reinterpret_cast<float(*)[V]>(f + j * V));
+#pragma unroll
+            for (int i = 0; i < P2; ++i) {
+                d[i] = two(f[2 * i], f[2 * i + 1]);
+                s2 = add2(s2, d[i]);
+            }
+        }
+        float sum[1] = {ok ? sum2(s2) : __uint_as_float(0x7FC00000u)};
+        team_sum(sum, T, red, turn, barrier);
+        // the whole team has its elements: the stage is free
+        if (T == 32) __syncwarp();
+        if (t == 0) issue(r + R.stages * step, s);
+        const float mean = sum[0] * inv;
+        const two_f32 minus = two(-mean, -mean);
+#pragma unroll
+        for (int i = 0; i < P2; ++i) {
+            d[i] = add2(d[i], minus);
+            // nothing of what is past the row's end
+            if (!col.whole(2 * i / V) && col(2 * i / V) >= C) d[i] = 0;
+            q2 = fma2(d[i], d[i], q2);
+        }
+        float q[1] = {sum2(q2)};
+        team_sum(q, T, red, turn, barrier);
+        const float rstd = rsqrtf(fmaf(q[0], inv, P.eps));
+        const two_f32 scale = two(rstd, rstd);
+        TY *y = static_cast<TY *>(P.Y) + r * P.ldy;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (!col.whole(j) && col(j) >= C) continue;
+            float ga[V], be[V], o[V];
+            read_param<V>(gammas, P.gamma, col(j), C, 1.0f, ga);
+            read_param<V>(betas, P.beta, col(j), C, 0.0f, be);
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i)
+                each(fma2(mul2(d[j * V / 2 + i], scale), two(ga[2 * i], ga[2 * i + 1]), two(be[2 * i], be[2 * i + 1])), o[2 * i], o[2 * i + 1]);
+            store(y + col(j), o);
+        }
+        if (t == 0) {
+            if (P.mean) P.mean[r] = mean;
+            if (P.rstd) P.rstd[r] = rstd;
+        }
+        if (++s == R.stages) { s = 0; ph ^= 1u; }
+    }
+}
+
 // Rows longer than the registers of a block: the row is read three times, from L2 after the first.
 template <typename TX, typename TY, int V>
 __global__ void __launch_bounds__(1024) norm_fwd_long_kernel(const __grid_constant__ FwdParams P)
 {
-    __shared__ float red[2][32][2];
+    __shared__ __align__(16) float red[2][32][2];
     unsigned int turn = 0;
     const float inv = 1.0f / (float)P.C;
     pdl_begin();
@@ -216,7 +452,7 @@ __global__ void __launch_bounds__(1024) norm_fwd_long_kernel(const __grid_consta
 #pragma unroll
             for (int i = 0; i < V; ++i) s[0] += f[i];
         }
-        team_sum(s, 1024, red, turn);
+        team_sum(s, 1024, red, turn, 0);
         const float mean = s[0] * inv;
         float q[1] = {0.0f};
         for (long long col = (long long)threadIdx.x * V; col < P.C; col += 1024 * V) {
@@ -226,8 +462,8 @@ __global__ void __launch_bounds__(1024) norm_fwd_long_kernel(const __grid_consta
 #pragma unroll
             for (int i = 0; i < V; ++i) q[0] = fmaf(f[i] - mean, f[i] - mean, q[0]);
         }
-        team_sum(q, 1024, red, turn);
-        const float rstd = 1.0f / sqrtf(fmaf(q[0], inv, P.eps));
+        team_sum(q, 1024, red, turn, 0);
+        const float rstd = rsqrtf(fmaf(q[0], inv, P.eps));
         TY *y = static_cast<TY *>(P.Y) + r * P.ldy;
         for (long long col = (long long)threadIdx.x * V; col < P.C; col += 1024 * V) {
             Vec<TX, V> v;
@@ -261,25 +497,34 @@ constexpr int kBwdThreads = 512;
 
 // One row per team, the next row's loads in flight while this one is worked on; sums over the rows of a block stay in the
 // registers of the threads that own the columns, and its teams join them in shared memory at the end.  C <= T * E.
-template <typename TD, typename TX, typename TO, int V, int E>
+template <typename TD, typename TX, typename TO, int V, int E, int TT>
 __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_constant__ BwdParams P)
 {
-    constexpr int NV = E / V;
+    constexpr int NV = E / V, P2 = E / 2;
     extern __shared__ float cols[];          // [2][C], when a block has several teams (of a warp or more)
-    __shared__ float red[2][32][2];
+    __shared__ __align__(16) float red[2][32][2];
     unsigned int turn = 0;
-    const int T = P.T, t = threadIdx.x & (T - 1);
-    const int teams = kBwdThreads / T, team = threadIdx.x / T;
-    const float inv = 1.0f / (float)P.C;
+    const int T = TT ? TT : P.T, t = threadIdx.x & (T - 1), C = (int)P.C;
+    const int teams = blockDim.x / T, team = threadIdx.x / T;
+    const int barrier = teams > 1 ? team + 1 : 0;
+    const float inv = 1.0f / (float)C;
     const long long step = (long long)gridDim.x * teams;
+    const Columns<V, TT> col{T, t, C};
     pdl_begin();
-    float ga[NV][V], a_g[NV][V], a_b[NV][V];
+    two_f32 ga[P2], a_g[P2], a_b[P2];
+    {
+        float f[E];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const long long col = (long long)(j * T + t) * V;
+        for (int j = 0; j < NV; ++j) {
+            float g[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) a_g[j][i] = a_b[j][i] = ga[j][i] = 0.0f;
-        if (col < P.C) load_param(ga[j], P.gamma, col, 1.0f);
+            for (int i = 0; i < V; ++i) g[i] = 0.0f;
+            if (col(j) < C) load_param(g, P.gamma, col(j), 1.0f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[j * V + i] = g[i];
+        }
+#pragma unroll
+        for (int i = 0; i < P2; ++i) { ga[i] = two(f[2 * i], f[2 * i + 1]); a_g[i] = a_b[i] = 0; }
     }
     Vec<TD, V> nd[NV];
     Vec<TX, V> nx[NV];
@@ -290,88 +535,218 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
         const TX *x = static_cast<const TX *>(P.X) + (live ? r : 0) * P.ldx;
         n_mean = live ? P.mean[r] : 0.0f;
         n_rstd = live ? P.rstd[r] : 0.0f;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const long long col = (long long)(j * T + t) * V;
-            if (live && col < P.C) { nd[j].load(d + col); nx[j].load(x + col); }
-            else { nd[j].zero(); nx[j].zero(); }
-        }
+        load_vectors(nd, d, col, live);
+        load_vectors(nx, x, col, live);
     };
     long long r0 = (long long)blockIdx.x * teams;
     if (r0 < P.M) fetch(r0 + team);
     for (; r0 < P.M; r0 += step) {
         const long long r = r0 + team;
         const bool live = r < P.M;
-        Vec<TD, V> cd[NV];
-        Vec<TX, V> cx[NV];
+        two_f32 dy[P2], xh[P2];
+        {
+            float fd[E], fx[E];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) { cd[j] = nd[j]; cx[j] = nx[j]; }
+            for (int j = 0; j < NV; ++j) {
+                nd[j].get(*reinterpret_cast<float(*)[V]>(fd + j * V));
+                nx[j].get(*reinterpret_cast<float(*)[V]>(fx + j * V));
+            }
+#pragma unroll
+            for (int i = 0; i < P2; ++i) {
+                dy[i] = two(fd[2 * i], fd[2 * i + 1]);
+                xh[i] = two(fx[2 * i], fx[2 * i + 1]);
+            }
+        }
         const float mean = n_mean, rstd = n_rstd;
         if (r0 + step < P.M) fetch(r + step);
-        float s[2] = {0.0f, 0.0f};
+        // past the row's end dy and gamma are zero
+        const two_f32 minus = two(-mean, -mean), scale = two(rstd, rstd);
+        two_f32 s0 = 0, s1 = 0;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if (!live || (long long)(j * T + t) * V >= P.C) continue;
-            float d[V], x[V];
-            cd[j].get(d);
-            cx[j].get(x);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float xh = (x[i] - mean) * rstd, g = d[i] * ga[j][i];
-                s[0] += g;
-                s[1] = fmaf(g, xh, s[1]);
-                a_g[j][i] = fmaf(d[i], xh, a_g[j][i]);
-                a_b[j][i] += d[i];
-            }
+        for (int i = 0; i < P2; ++i) {
+            xh[i] = mul2(add2(xh[i], minus), scale);
+            a_g[i] = fma2(dy[i], xh[i], a_g[i]);
+            a_b[i] = add2(a_b[i], dy[i]);
+            dy[i] = mul2(dy[i], ga[i]);
+            s0 = add2(s0, dy[i]);
+            s1 = fma2(dy[i], xh[i], s1);
         }
         if (P.dX == nullptr) continue;
-        team_sum(s, T, red, turn);
+        float s[2] = {sum2(s0), sum2(s1)};
+        team_sum(s, T, red, turn, barrier);
         if (!live) continue;
-        const float c0 = s[0] * inv, c1 = s[1] * inv;
+        const float c0 = -s[0] * inv, c1 = -s[1] * inv;
+        const two_f32 k0 = two(c0, c0), k1 = two(c1, c1);
         TO *o = static_cast<TO *>(P.dX) + r * P.lddx;
+        float f[E];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const long long col = (long long)(j * T + t) * V;
-            if (col >= P.C) continue;
-            float d[V], x[V];
-            cd[j].get(d);
-            cx[j].get(x);
+        for (int i = 0; i < P2; ++i) each(mul2(fma2(xh[i], k1, add2(dy[i], k0)), scale), f[2 * i], f[2 * i + 1]);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float xh = (x[i] - mean) * rstd;
-                d[i] = (fmaf(d[i], ga[j][i], -c0) - xh * c1) * rstd;
-            }
-            store(o + col, d);
-        }
+        for (int j = 0; j < NV; ++j)
+            if (col.whole(j) || col(j) < C) store(o + col(j), *reinterpret_cast<const float(*)[V]>(f + j * V));
     }
     if (P.part == nullptr) return;
-    float *out = P.part + (long long)blockIdx.x * 2 * P.C;
+    float *out = P.part + (long long)blockIdx.x * 2 * C;
+    float g[E], b[E];
+#pragma unroll
+    for (int i = 0; i < P2; ++i) { each(a_g[i], g[2 * i], g[2 * i + 1]); each(a_b[i], b[2 * i], b[2 * i + 1]); }
     // the teams of a warp by shuffles, then the warps in turn: a fixed order
     for (int o = T; o < 32; o <<= 1)
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                a_g[j][i] += __shfl_xor_sync(0xffffffffu, a_g[j][i], o);
-                a_b[j][i] += __shfl_xor_sync(0xffffffffu, a_b[j][i], o);
-            }
-    const int span = max(T, 32), turns = kBwdThreads / span;
+        for (int e = 0; e < E; ++e) {
+            g[e] += __shfl_xor_sync(0xffffffffu, g[e], o);
+            b[e] += __shfl_xor_sync(0xffffffffu, b[e], o);
+        }
+    const int span = max(T, 32), turns = blockDim.x / span;
     for (int k = 0; k < turns; ++k) {
         if ((int)threadIdx.x / span == k && (int)threadIdx.x % span < T)
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                const long long col = (long long)(j * T + t) * V;
-                if (col >= P.C) continue;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float g = a_g[j][i], b = a_b[j][i];
-                    if (k > 0) { g += cols[col + i]; b += cols[P.C + col + i]; }
-                    float *to = k == turns - 1 ? out : cols;
-                    to[col + i] = g;
-                    to[P.C + col + i] = b;
-                }
+            for (int e = 0; e < E; ++e) {
+                const int c = col(e / V) + e % V;
+                if (c >= C) continue;
+                if (k > 0) { g[e] += cols[c]; b[e] += cols[C + c]; }
+                float *to = k == turns - 1 ? out : cols;
+                to[c] = g[e];
+                to[C + c] = b[e];
             }
         if (turns > 1) __syncthreads();
+    }
+}
+
+// The same with rows through shared memory (see norm_fwd_ring_kernel).  The sums over the rows fill the registers, so a row is read
+// twice from its stage, for its two sums and for its gradient; the stage is refilled after the next row's sums, when the whole team has
+// left it.
+template <typename TD, typename TX, typename TO, int V, int E>
+__global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __grid_constant__ BwdParams P, const __grid_constant__ Ring R)
+{
+    constexpr int P2 = E / 2, W = V;         // elements worked on at a time
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ unsigned long long full[kMaxTeams][kMaxRing];
+    __shared__ __align__(16) float red[2][32][2];
+    __shared__ volatile int gave_up;
+    unsigned int turn = 0;
+    const int T = P.T, team = threadIdx.x / T, t = threadIdx.x - team * T, C = (int)P.C;
+    const int teams = blockDim.x / T, barrier = teams > 1 ? team + 1 : 0;
+    const float inv = 1.0f / (float)C;
+    const Columns<V, 0> col{T, t, C};
+    if (t == 0)
+        for (int s = 0; s < R.stages; ++s) mbar_init(&full[team][s], 1);
+    if (threadIdx.x == 0) gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncthreads();
+    pdl_begin();
+    uint8_t *const mine = ring + R.params + (size_t)team * R.stages * R.stage_bytes;
+    const long long first = (long long)blockIdx.x * teams + team, step = (long long)gridDim.x * teams;
+    auto issue = [&](long long r, int s) {
+        if (r >= P.M) return;
+        uint8_t *const st = mine + (size_t)s * R.stage_bytes;
+        mbar_expect_tx(&full[team][s], C * (uint32_t)(sizeof(TD) + sizeof(TX)));
+        bulk_load(st, static_cast<const TD *>(P.dY) + r * P.lddy, C * (uint32_t)sizeof(TD), &full[team][s]);
+        bulk_load(st + R.second, static_cast<const TX *>(P.X) + r * P.ldx, C * (uint32_t)sizeof(TX), &full[team][s]);
+    };
+    if (t == 0)
+        for (int s = 0; s < R.stages; ++s) issue(first + s * step, s);
+    float *const gammas = R.params ? reinterpret_cast<float *>(ring) : nullptr;
+    if (R.params) {
+        for (int c = threadIdx.x; c < C; c += blockDim.x) gammas[param_at<V>(c, C)] = P.gamma ? P.gamma[c] : 1.0f;
+        __syncthreads();
+    }
+    two_f32 a_g[P2], a_b[P2];
+#pragma unroll
+    for (int i = 0; i < P2; ++i) a_g[i] = a_b[i] = 0;
+    int s = 0;
+    uint32_t ph = 0;
+    float n_mean = first < P.M ? P.mean[first] : 0.0f, n_rstd = first < P.M ? P.rstd[first] : 0.0f;
+    for (long long r = first; r < P.M; r += step) {
+        const float mean = n_mean, rstd = n_rstd;
+        if (r + step < P.M) { n_mean = P.mean[r + step]; n_rstd = P.rstd[r + step]; }
+        const bool ok = mbar_wait(&full[team][s], ph, &gave_up, nullptr, 0);
+        const uint8_t *const st = mine + (size_t)s * R.stage_bytes;
+        const TX *const x = reinterpret_cast<const TX *>(st + R.second);
+        const TD *const dy = reinterpret_cast<const TD *>(st);
+        const two_f32 minus = two(-mean, -mean), scale = two(rstd, rstd);
+        // W elements from e on: xh, dy, and g = dy gamma (past the row's end dy and gamma are zero)
+        auto load = [&](int e, two_f32 (&xh)[W / 2], two_f32 (&d)[W / 2], two_f32 (&g)[W / 2]) {
+            float fx[W], fd[W], fg[W];
+#pragma unroll
+            for (int h = 0; h < W; h += V) {
+                const int j = (e + h) / V;
+                read_vector(x, col, j, *reinterpret_cast<float(*)[V]>(fx + h));
+                read_vector(dy, col, j, *reinterpret_cast<float(*)[V]>(fd + h));
+                float(&gv)[V] = *reinterpret_cast<float(*)[V]>(fg + h);
+                if (col.whole(j) || col(j) < C) {
+                    read_param<V>(gammas, P.gamma, col(j), C, 1.0f, gv);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) gv[i] = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) {
+                xh[i] = mul2(add2(two(fx[2 * i], fx[2 * i + 1]), minus), scale);
+                d[i] = two(fd[2 * i], fd[2 * i + 1]);
+                g[i] = mul2(d[i], two(fg[2 * i], fg[2 * i + 1]));
+            }
+        };
+        two_f32 s0 = 0, s1 = 0;
+#pragma unroll
+        for (int e = 0; e < E; e += W) {
+            two_f32 xh[W / 2], d[W / 2], g[W / 2];
+            load(e, xh, d, g);
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) {
+                a_g[e / 2 + i] = fma2(d[i], xh[i], a_g[e / 2 + i]);
+                a_b[e / 2 + i] = add2(a_b[e / 2 + i], d[i]);
+                s0 = add2(s0, g[i]);
+                s1 = fma2(g[i], xh[i], s1);
+            }
+        }
+        float sums[2] = {sum2(s0), ok ? sum2(s1) : __uint_as_float(0x7FC00000u)};
+        team_sum(sums, T, red, turn, barrier);
+        // the whole team has left the row before this one: its stage is free
+        if (T == 32) __syncwarp();
+        if (t == 0 && r != first) issue(r + (R.stages - 1) * step, s == 0 ? R.stages - 1 : s - 1);
+        if (P.dX) {
+            const float c0 = -sums[0] * inv, c1 = -sums[1] * inv;
+            const two_f32 k0 = two(c0, c0), k1 = two(c1, c1);
+            TO *o = static_cast<TO *>(P.dX) + r * P.lddx;
+#pragma unroll
+            for (int e = 0; e < E; e += W) {
+                two_f32 xh[W / 2], d[W / 2], g[W / 2];
+                load(e, xh, d, g);
+                float f[W];
+#pragma unroll
+                for (int i = 0; i < W / 2; ++i) each(mul2(fma2(xh[i], k1, add2(g[i], k0)), scale), f[2 * i], f[2 * i + 1]);
+#pragma unroll
+                for (int h = 0; h < W; h += V) {
+                    const int j = (e + h) / V;
+                    if (col.whole(j) || col(j) < C) store(o + col(j), *reinterpret_cast<const float(*)[V]>(f + h));
+                }
+            }
+        }
+        if (++s == R.stages) { s = 0; ph ^= 1u; }
+    }
+    if (P.part == nullptr) return;
+    __syncthreads();                         // no copy is on its way: the ring takes the sums, the teams in turn
+    float *const cols = reinterpret_cast<float *>(ring), *const out = P.part + (long long)blockIdx.x * 2 * C;
+    for (int k = 0; k < teams; ++k) {
+        if (team == k)
+#pragma unroll
+            for (int i = 0; i < P2; ++i) {
+                float g[2], b[2];
+                each(a_g[i], g[0], g[1]);
+                each(a_b[i], b[0], b[1]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int e = 2 * i + h, c = col(e / V) + e % V;
+                    if (c >= C) continue;
+                    if (k > 0) { g[h] += cols[c]; b[h] += cols[C + c]; }
+                    float *const to = k == teams - 1 ? out : cols;
+                    to[c] = g[h];
+                    to[C + c] = b[h];
+                }
+            }
+        __syncthreads();
     }
 }
 
@@ -379,7 +754,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
 template <typename TD, typename TX, int V>
 __global__ void __launch_bounds__(kBwdThreads) norm_bwd_sums_kernel(const __grid_constant__ BwdParams P)
 {
-    __shared__ float red[2][32][2];
+    __shared__ __align__(16) float red[2][32][2];
     unsigned int turn = 0;
     const float inv = 1.0f / (float)P.C;
     pdl_begin();
@@ -404,7 +779,7 @@ __global__ void __launch_bounds__(kBwdThreads) norm_bwd_sums_kernel(const __grid
                 s[1] = fmaf(g, (x[i] - mean) * rstd, s[1]);
             }
         }
-        team_sum(s, kBwdThreads, red, turn);
+        team_sum(s, kBwdThreads, red, turn, 0);
         if (threadIdx.x == 0) {
             P.row_sums[2 * r] = s[0] * inv;
             P.row_sums[2 * r + 1] = s[1] * inv;
@@ -451,20 +826,29 @@ __global__ void __launch_bounds__(kStripeThreads) norm_bwd_stripe_kernel(const _
     }
 }
 
-// dgamma and dbeta: the parts of each column in a fixed order, eight runs of them at a time.
-__global__ void __launch_bounds__(256) norm_fold_kernel(const float *part, int parts, long long C, float *dgamma, float *dbeta)
+// dgamma and dbeta: a column's parts in 32 runs, all of a run's loads at once (with eight runs, one load after the other, the fold of 148
+// parts took longer than what it folds), and the runs in order.
+constexpr int kPartBlocks = 148, kRuns = 32, kPerRun = (kPartBlocks + kRuns - 1) / kRuns;
+__global__ void __launch_bounds__(32 * kRuns) norm_fold_kernel(const float *part, int parts, long long C, float *dgamma, float *dbeta)
 {
-    __shared__ float s[8][33];
+    __shared__ float s[kRuns][32];
     pdl_begin();
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
     const long long c = (long long)blockIdx.x * 32 + lane;
-    float v = 0.0f;
-    if (c < 2 * C)
-        for (int p = run; p < parts; p += 8) v += part[(long long)p * 2 * C + c];
+    float w[kPerRun], v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kPerRun; ++k) {
+        const int p = run + kRuns * k;
+        w[k] = p < parts && c < 2 * C ? __ldg(part + (long long)p * 2 * C + c) : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < kPerRun; ++k) v += w[k];
     s[run][lane] = v;
     __syncthreads();
     if (run == 0 && c < 2 * C) {
-        v = ((s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane])) + ((s[4][lane] + s[5][lane]) + (s[6][lane] + s[7][lane]));
+        v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kRuns; ++k) v += s[k][lane];
         float *out = c < C ? dgamma : dbeta;
         if (out) out[c < C ? c : c - C] = v;
     }
@@ -482,10 +866,15 @@ int check_matrix(const void *p, int dtype, long long ld, long long M, long long 
     TWN_REQUIRE(M == 0 || ld <= (1ll << 58) / M, TWN_ERR_TOO_LARGE);
     return TWN_OK;
 }
-bool vector_rows(const void *p, int dtype, long long ld) { return twn_aligned(p, 16) && ld * (long long)size_of(dtype) % 16 == 0; }
+// Rows whose runs of V elements are aligned to their loads (of 16 bytes at most).
+bool vector_rows(const void *p, int dtype, long long ld, int V)
+{
+    const long long unit = std::min<long long>(16, V * (long long)size_of(dtype));
+    return twn_aligned(p, (size_t)unit) && ld * (long long)size_of(dtype) % unit == 0;
+}
 
 constexpr long long kMaxC = 1ll << 31;       // channels: partial sums and columns stay far inside 64 bits
-constexpr int kPartBlocks = 148;
+constexpr long long kRingElements = 1 << 20;  // below, the launch itself is what counts
 
 int team_for(long long C, int E, int least, int most)
 {
@@ -494,40 +883,135 @@ int team_for(long long C, int E, int least, int most)
     return T;
 }
 
-template <typename TX, typename TY, int V, int E> int launch_fwd(FwdParams &P, int T, cudaStream_t s)
+template <typename TX, typename TY, int V, int E, int TT> int launch_fwd(FwdParams &P, int T, cudaStream_t s)
 {
     P.T = T;
-    const int block = std::max(T, 128), teams = block / T;
+    const int block = T > 32 ? T : 128, teams = block / T;
     const long long grid = std::min<long long>((P.M + teams - 1) / teams, 148ll * 64);
-    TWN_CUDA_OK(twn_launch_small(norm_fwd_kernel<TX, TY, V, E>, (int)grid, block, 0, s, P));
+    TWN_CUDA_OK(twn_launch_small(norm_fwd_kernel<TX, TY, V, E, TT>, (int)grid, block, 0, s, P));
     return TWN_OK;
 }
-template <typename TX, typename TY, int V> int fwd(FwdParams &P, cudaStream_t s)
+// Threads of a row (whole warps), rows that a block has at once, and their rings behind what holds gamma and beta.
+struct RingShape {
+    int T, teams;
+    Ring ring;
+    size_t smem;
+};
+bool ring_shape(RingShape &r, long long C, int E, int threads, size_t stage, size_t second, size_t params)
 {
-    if (P.C <= 32 * 8) return launch_fwd<TX, TY, V, 8>(P, team_for(P.C, 8, 4, 32), s);
-    if (P.C <= (V == 1 ? 16 : 8) * 1024) return launch_fwd<TX, TY, V, 16>(P, team_for(P.C, 16, 32, 1024), s);
-    if constexpr (V > 1) {                   // 32 elements of one load each do not fit the registers of 1024 threads
-        if (P.C <= 32 * 1024) return launch_fwd<TX, TY, V, 32>(P, team_for(P.C, 32, 512, 1024), s);
+    r.T = (int)((C + 32 * E - 1) / (32 * E)) * 32;
+    if (r.T > threads) return false;
+    r.teams = std::min(threads / r.T, r.T > 32 ? 15 : kMaxTeams);          // a block has fifteen named barriers beside its own
+    params = (params + 127) / 128 * 128;
+    if (params > kRingBytes / 2) params = 0;
+    while (r.teams > 1 && 2 * r.teams * stage > kRingBytes - params) --r.teams;
+    const int stages = (int)std::min<size_t>(kMaxRing, (kRingBytes - params) / (r.teams * stage));
+    r.ring = {stages, (int)stage, (int)second, (int)params};
+    r.smem = params + r.teams * stages * stage;
+    return stages >= 2 && r.teams * r.T >= 256 + 32;
+}
+template <typename Kernel> int allow_ring(Kernel kernel, int device, bool (&done)[64])
+{
+    if (!done[device]) TWN_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes));
+    done[device] = true;
+    return TWN_OK;
+}
+template <typename TX, typename TY, int V, int E> bool fwd_ring(FwdParams &P, const twn_device_info &dev, cudaStream_t s, int &rc)
+{
+    static bool done[64] = {false};
+    RingShape r;
+    if (!ring_shape(r, P.C, E, fwd_ring_threads<E>(), P.C * sizeof(TX), 0, 2 * sizeof(float) * P.C)) return false;
+    rc = allow_ring(norm_fwd_ring_kernel<TX, TY, V, E>, dev.ordinal, done);
+    if (rc != TWN_OK) return true;
+    P.T = r.T;
+    const int grid = (int)std::min<long long>((P.M + r.teams - 1) / r.teams, dev.sm_count);
+    if (twn_launch_small(norm_fwd_ring_kernel<TX, TY, V, E>, grid, r.T * r.teams, r.smem, s, P, r.ring) != cudaSuccess) rc = TWN_ERR_CUDA;
+    return true;
+}
+template <typename TD, typename TX, typename TO, int V, int E> bool bwd_ring(BwdParams &P, const twn_device_info &dev, cudaStream_t s, int &rc)
+{
+    static bool done[64] = {false};
+    RingShape r;
+    const size_t second = P.C * sizeof(TD);
+    if (!ring_shape(r, P.C, E, kBwdThreads, second + P.C * sizeof(TX), second, sizeof(float) * P.C)) return false;
+    rc = allow_ring(norm_bwd_ring_kernel<TD, TX, TO, V, E>, dev.ordinal, done);
+    if (rc != TWN_OK) return true;
+    P.T = r.T;
+    P.parts = (int)std::min<long long>((P.M + r.teams - 1) / r.teams, std::min(dev.sm_count, kPartBlocks));
+    const size_t smem = std::max<size_t>(r.smem, r.teams > 1 ? 2 * sizeof(float) * P.C : 0);
+    if (twn_launch_small(norm_bwd_ring_kernel<TD, TX, TO, V, E>, P.parts, r.T * r.teams, smem, s, P, r.ring) != cudaSuccess) rc = TWN_ERR_CUDA;
+    return true;
+}
+
+template <typename TX, typename TY, int V> int fwd(FwdParams &P, const twn_device_info &dev, cudaStream_t s)
+{
+    if constexpr (V > 1) {
+        int rc = TWN_OK;
+        if (P.C > 256 && P.M * P.C >= kRingElements &&
+            (P.C <= 512 ? fwd_ring<TX, TY, V, 16>(P, dev, s, rc) : P.C <= 1024 ? fwd_ring<TX, TY, V, 32>(P, dev, s, rc) : fwd_ring<TX, TY, V, 64>(P, dev, s, rc)))
+            return rc;
+    }
+    if (P.C <= 32 * 8) return launch_fwd<TX, TY, V, 8, 0>(P, team_for(P.C, 8, 4, 32), s);
+    if constexpr (V > 1) {
+        if (P.C <= 8 * 1024) return launch_fwd<TX, TY, V, 16, 0>(P, team_for(P.C, 16, 32, 512), s);
+        if (P.C <= 32 * 1024) return launch_fwd<TX, TY, V, 32, 0>(P, team_for(P.C, 32, 512, 1024), s);
+    } else {
+        if (P.C <= 512) return launch_fwd<TX, TY, 1, 16, 32>(P, 32, s);
+        if (P.C <= 1024) return launch_fwd<TX, TY, 1, 16, 64>(P, 64, s);
+        if (P.C <= 2048) return launch_fwd<TX, TY, 1, 16, 128>(P, 128, s);
+        if (P.C <= 4096) return launch_fwd<TX, TY, 1, 16, 256>(P, 256, s);
+        if (P.C <= 8192) return launch_fwd<TX, TY, 1, 16, 512>(P, 512, s);
+        if (P.C <= 16384) return launch_fwd<TX, TY, 1, 16, 1024>(P, 1024, s);
     }
     const int grid = (int)std::min<long long>(P.M, 148 * 2);
     TWN_CUDA_OK(twn_launch_small(norm_fwd_long_kernel<TX, TY, V>, grid, 1024, 0, s, P));
     return TWN_OK;
 }
-template <typename TX, typename TY> int fwd_any(FwdParams &P, bool vec, cudaStream_t s)
+template <typename TX, typename TY> int fwd_any(FwdParams &P, bool vec, const twn_device_info &dev, cudaStream_t s)
 {
     constexpr int V = sizeof(TX) == 2 ? 8 : 4;
-    return vec ? fwd<TX, TY, V>(P, s) : fwd<TX, TY, 1>(P, s);
+    return vec ? fwd<TX, TY, V>(P, dev, s) : fwd<TX, TY, 1>(P, dev, s);
 }
 
-template <typename TD, typename TX, typename TO, int V> int bwd(BwdParams &P, float *dgamma, float *dbeta, int sms, cudaStream_t s)
+template <typename TD, typename TX, typename TO, int V, int E> int bwd_rows(BwdParams &P, const twn_device_info &dev, cudaStream_t s)
+{
+    P.T = team_for(P.C, E, 4, kBwdThreads);
+    // few rows: blocks of fewer teams, so that there are more of them
+    int threads = kBwdThreads;
+    while (threads > std::max(P.T, 128) && (P.M * P.T + threads - 1) / threads < dev.sm_count) threads /= 2;
+    const int teams = threads / P.T;
+    P.parts = (int)std::max<long long>(1, std::min<long long>((P.M + teams - 1) / teams, std::min(dev.sm_count, kPartBlocks)));
+    const size_t smem = teams > 1 && P.part ? 2 * sizeof(float) * P.C : 0;
+    auto launch = [&](auto kernel) { return twn_launch_small(kernel, P.parts, threads, smem, s, P); };
+    cudaError_t e = cudaSuccess;
+    if constexpr (V > 1) e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 0>);
+    else
+        switch (P.T) {
+            case 32: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 32>); break;
+            case 64: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 64>); break;
+            case 128: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 128>); break;
+            case 256: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 256>); break;
+            case 512: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 512>); break;
+            default: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 0>);
+        }
+    TWN_CUDA_OK(e);
+    return TWN_OK;
+}
+template <typename TD, typename TX, typename TO, int V> int bwd(BwdParams &P, float *dgamma, float *dbeta, const twn_device_info &dev, cudaStream_t s)
 {
     constexpr int E = V == 8 && sizeof(TD) == 2 && sizeof(TX) == 2 ? 16 : 8;
-    if (P.C <= kBwdThreads * E) {
-        P.T = team_for(P.C, E, 4, kBwdThreads);
-        const int teams = kBwdThreads / P.T;
-        P.parts = (int)std::max<long long>(1, std::min<long long>((P.M + teams - 1) / teams, std::min(sms, kPartBlocks)));
-        const size_t smem = teams > 1 && P.part ? 2 * sizeof(float) * P.C : 0;
-        TWN_CUDA_OK(twn_launch_small(norm_bwd_kernel<TD, TX, TO, V, E>, P.parts, kBwdThreads, smem, s, P));
+    int rc = TWN_OK;
+    bool served = false;
+    if constexpr (V > 1) served = P.C > kBwdThreads * E && P.M * P.C >= kRingElements && bwd_ring<TD, TX, TO, V, 32>(P, dev, s, rc);
+    if (served) {
+        if (rc != TWN_OK) return rc;
+    } else if (V == 1 && P.C <= kBwdThreads * 16 && (P.C > kBwdThreads * E || P.M * P.C >= 1 << 23)) {
+        // single elements of large tensors: 60000 x 1001 144 us with eight a thread, 90 with sixteen (2999 x 1001 10.6 and 13.6)
+        rc = bwd_rows<TD, TX, TO, V, V == 1 ? 16 : E>(P, dev, s);
+        if (rc != TWN_OK) return rc;
+    } else if (P.C <= kBwdThreads * E) {
+        rc = bwd_rows<TD, TX, TO, V, E>(P, dev, s);
+        if (rc != TWN_OK) return rc;
     } else {
         if (P.dX && P.M > 0)
             TWN_CUDA_OK(twn_launch_small(norm_bwd_sums_kernel<TD, TX, V>, (int)std::min<long long>(P.M, 148 * 4), kBwdThreads, 0, s, P));
@@ -540,14 +1024,14 @@ template <typename TD, typename TX, typename TO, int V> int bwd(BwdParams &P, fl
         TWN_CUDA_OK(cudaLaunchKernelEx(&cfg, norm_bwd_stripe_kernel<TD, TX, TO, V>, P));
     }
     if (P.part)
-        TWN_CUDA_OK(twn_launch_small(norm_fold_kernel, (int)((2 * P.C + 31) / 32), 256, 0, s, P.part, P.parts, P.C, dgamma, dbeta));
+        TWN_CUDA_OK(twn_launch_small(norm_fold_kernel, (int)((2 * P.C + 31) / 32), 32 * kRuns, 0, s, P.part, P.parts, P.C, dgamma, dbeta));
     return TWN_OK;
 }
 template <typename TD, typename TX, typename TO>
-int bwd_any(BwdParams &P, bool vec, float *dgamma, float *dbeta, int sms, cudaStream_t s)
+int bwd_any(BwdParams &P, bool vec, float *dgamma, float *dbeta, const twn_device_info &dev, cudaStream_t s)
 {
     constexpr int V = sizeof(TD) == 4 && sizeof(TX) == 4 ? 4 : 8;
-    return vec ? bwd<TD, TX, TO, V>(P, dgamma, dbeta, sms, s) : bwd<TD, TX, TO, 1>(P, dgamma, dbeta, sms, s);
+    return vec ? bwd<TD, TX, TO, V>(P, dgamma, dbeta, dev, s) : bwd<TD, TX, TO, 1>(P, dgamma, dbeta, dev, s);
 }
 
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
@@ -570,11 +1054,12 @@ extern "C" int twn_layer_norm_fwd(const void *X, int32_t x_dtype, int64_t ldx, i
     rc = twn_current_device(&dev);
     if (rc != TWN_OK) return rc;
     FwdParams P = {X, Y, gamma, beta, mean, rstd, ldx, ldy, M, C, (float)eps, 0};
-    const bool vec = vector_rows(X, x_dtype, ldx) && vector_rows(Y, y_dtype, ldy) && C % 8 == 0 && twn_aligned(gamma, 16) &&
+    const int V = x_dtype == TWN_BF16 ? 8 : 4;
+    const bool vec = vector_rows(X, x_dtype, ldx, V) && vector_rows(Y, y_dtype, ldy, V) && C % V == 0 && twn_aligned(gamma, 16) &&
                      twn_aligned(beta, 16);
     cudaStream_t s = twn_cu(stream);
-    if (x_dtype == TWN_BF16) return y_dtype == TWN_BF16 ? fwd_any<bf16, bf16>(P, vec, s) : fwd_any<bf16, float>(P, vec, s);
-    return y_dtype == TWN_BF16 ? fwd_any<float, bf16>(P, vec, s) : fwd_any<float, float>(P, vec, s);
+    if (x_dtype == TWN_BF16) return y_dtype == TWN_BF16 ? fwd_any<bf16, bf16>(P, vec, dev, s) : fwd_any<bf16, float>(P, vec, dev, s);
+    return y_dtype == TWN_BF16 ? fwd_any<float, bf16>(P, vec, dev, s) : fwd_any<float, float>(P, vec, dev, s);
 }
 
 extern "C" size_t twn_layer_norm_bwd_workspace_bytes(int64_t M, int64_t C)
@@ -610,18 +1095,19 @@ extern "C" int twn_layer_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy
     P.part = sums ? static_cast<float *>(workspace) : nullptr;
     P.row_sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(C));
     P.lddy = lddy; P.ldx = ldx; P.lddx = lddx; P.M = M; P.C = C;
-    const bool vec = vector_rows(dY, dy_dtype, lddy) && vector_rows(X, x_dtype, ldx) && (!dX || vector_rows(dX, dx_dtype, lddx)) &&
-                     C % 8 == 0 && twn_aligned(gamma, 16);
+    const int V = dy_dtype == TWN_F32 && x_dtype == TWN_F32 ? 4 : 8;
+    const bool vec = vector_rows(dY, dy_dtype, lddy, V) && vector_rows(X, x_dtype, ldx, V) && (!dX || vector_rows(dX, dx_dtype, lddx, V)) &&
+                     C % V == 0 && twn_aligned(gamma, 16);
     cudaStream_t s = twn_cu(stream);
     const int key = (dy_dtype == TWN_BF16) * 4 + (x_dtype == TWN_BF16) * 2 + (dX && dx_dtype == TWN_BF16);
     switch (key) {
-        case 0: return bwd_any<float, float, float>(P, vec, dgamma, dbeta, dev.sm_count, s);
-        case 1: return bwd_any<float, float, bf16>(P, vec, dgamma, dbeta, dev.sm_count, s);
-        case 2: return bwd_any<float, bf16, float>(P, vec, dgamma, dbeta, dev.sm_count, s);
-        case 3: return bwd_any<float, bf16, bf16>(P, vec, dgamma, dbeta, dev.sm_count, s);
-        case 4: return bwd_any<bf16, float, float>(P, vec, dgamma, dbeta, dev.sm_count, s);
-        case 5: return bwd_any<bf16, float, bf16>(P, vec, dgamma, dbeta, dev.sm_count, s);
-        case 6: return bwd_any<bf16, bf16, float>(P, vec, dgamma, dbeta, dev.sm_count, s);
-        default: return bwd_any<bf16, bf16, bf16>(P, vec, dgamma, dbeta, dev.sm_count, s);
+        case 0: return bwd_any<float, float, float>(P, vec, dgamma, dbeta, dev, s);
+        case 1: return bwd_any<float, float, bf16>(P, vec, dgamma, dbeta, dev, s);
+        case 2: return bwd_any<float, bf16, float>(P, vec, dgamma, dbeta, dev, s);
+        case 3: return bwd_any<float, bf16, bf16>(P, vec, dgamma, dbeta, dev, s);
+        case 4: return bwd_any<bf16, float, float>(P, vec, dgamma, dbeta, dev, s);
+        case 5: return bwd_any<bf16, float, bf16>(P, vec, dgamma, dbeta, dev, s);
+        case 6: return bwd_any<bf16, bf16, float>(P, vec, dgamma, dbeta, dev, s);
+        default: return bwd_any<bf16, bf16, bf16>(P, vec, dgamma, dbeta, dev, s);
     }
 }

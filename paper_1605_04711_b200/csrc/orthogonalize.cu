@@ -292,11 +292,6 @@ __global__ void __launch_bounds__(kSweepBlock) ns_start_kernel(const __grid_cons
 }
 
 // ---- PTX of the products ---------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, void *bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
-}
 // Rows of 128 bytes from row `row` of a matrix of blocks on, by either block of a pair; the barrier is at this address in the
 // first of them.
 __device__ __forceinline__ void pair_load(void *dst, const CUtensorMap *map, uint32_t bar, int row)

@@ -21,6 +21,11 @@ SHAPES = [(1, 1), (1, 7), (3, 2), (5, 31), (4, 32), (9, 33), (64, 64), (130, 256
           (3, 4104), (3, 8192), (2, 8200), (3, 16384), (2, 16385), (2, 32768), (2, 32776), (1, 50001)]
 
 
+# a million elements and more, where rows go through shared memory, and the sizes about them
+LARGE = [(4100, 260), (2100, 512), (2047, 516), (1100, 1024), (1050, 1004), (1100, 1001), (600, 2048), (300, 4096), (131, 8192), (130, 8200), (70, 16384), (64, 16392),
+         (40, 32768), (9000, 1001), (1100, 8191)]
+
+
 def _normal(seed, *shape):
     return torch.from_numpy(np.random.default_rng(seed).standard_normal(shape).astype(np.float32)).cuda()
 
@@ -84,6 +89,12 @@ def test_forward(M, C, xt, yt):
     _check_fwd(M, C, xt, yt, C, C)
 
 
+@pytest.mark.parametrize("M,C", LARGE)
+@pytest.mark.parametrize("xt,yt", [(F, F), (B, B), (F, B), (B, F)])
+def test_forward_large(M, C, xt, yt):
+    _check_fwd(M, C, xt, yt, C, C + 24, gamma=C % 3 > 0, beta=C % 5 > 0)
+
+
 @pytest.mark.parametrize("ldx,ldy,offset", [(1008, 1024, 0), (1001, 1000, 0), (1000, 1000, 1), (1000, 1003, 8), (1024, 1024, 0)])
 @pytest.mark.parametrize("xt,yt", [(F, F), (B, B), (F, B), (B, F)])
 def test_forward_pitches_and_offsets(ldx, ldy, offset, xt, yt):
@@ -115,7 +126,7 @@ def test_forward_nonfinite_rows_stay_alone():
         assert bool(y[r].isnan().all()) if r in (2, 5, 7) else torch.equal(y[r], clean[r])
 
 
-@pytest.mark.parametrize("C,dtype", [(96, B), (1001, F), (4096, B), (32768, F), (33000, B)])
+@pytest.mark.parametrize("C,dtype", [(96, B), (1001, F), (4096, B), (32768, F), (33000, B), (60000, F)])
 def test_forward_in_place_gives_the_same_bits(C, dtype):
     x, buf = _rows(7, 21, C, C, dtype)
     y = torch.empty(21, C, dtype=dtype, device="cuda")
@@ -124,14 +135,14 @@ def test_forward_in_place_gives_the_same_bits(C, dtype):
     assert torch.equal(buf.view(21, C), y)
 
 
-def test_a_row_has_the_same_bits_in_every_batch_and_call():
-    for C in (64, 1000, 4096, 40000):
-        x = _normal(8, 600, C).to(B)
-        y, one, again = (torch.empty_like(x) for _ in range(3))
-        twn.layer_norm_fwd(x, C, 600, C, None, None, EPS, y, C)
-        twn.layer_norm_fwd(x, C, 600, C, None, None, EPS, again, C)
-        twn.layer_norm_fwd(x[599:], C, 1, C, None, None, EPS, one[:1], C)
-        assert torch.equal(y, again) and torch.equal(one[0], y[599])
+def test_a_row_has_the_same_bits_at_every_place_and_in_every_call():
+    for M, C in ((600, 64), (600, 1000), (600, 4096), (3, 4096), (600, 1001), (30, 40000)):
+        x = _normal(8, M, C).to(B)
+        x[M - 1] = x[M // 2] = x[0]
+        y, again = torch.empty_like(x), torch.empty_like(x)
+        twn.layer_norm_fwd(x, C, M, C, None, None, EPS, y, C)
+        twn.layer_norm_fwd(x, C, M, C, None, None, EPS, again, C)
+        assert torch.equal(y, again) and torch.equal(y[0], y[M - 1]) and torch.equal(y[0], y[M // 2])
 
 
 def _bwd_reference(dy, x, gamma, mean, rstd):
@@ -177,6 +188,12 @@ def _check_bwd(M, C, dt, xt, ot, lddy, ldx, lddx, gamma=True, offset=0, seed=11,
 @pytest.mark.parametrize("dt,xt,ot", [(F, F, F), (B, B, B), (B, F, F), (F, B, B)])
 def test_backward(M, C, dt, xt, ot):
     _check_bwd(M, C, dt, xt, ot, C, C, C)
+
+
+@pytest.mark.parametrize("M,C", LARGE)
+@pytest.mark.parametrize("dt,xt,ot", [(F, F, F), (B, B, B), (B, F, B), (F, B, F)])
+def test_backward_large(M, C, dt, xt, ot):
+    _check_bwd(M, C, dt, xt, ot, C, C + 8, C + 24, gamma=C % 3 > 0)
 
 
 @pytest.mark.parametrize("lddy,ldx,lddx,offset", [(1008, 1024, 1000, 0), (1001, 1000, 1000, 0), (1000, 1000, 1003, 0), (1000, 1000, 1000, 1)])
