@@ -272,7 +272,10 @@ int twn_ternarize_codes_batch(const twn_ternarize_item_t *items, int count, void
  * fp16 products, fp32 sums; X is carried in 22 bits and the diagonals of A and of b A + c A^2 in fp32, so five steps are within
  * 1e-3 (2-norm, relative) of 64-bit arithmetic for matrices of independent elements, and within 4e-3 for low rank (one included)
  * and for singular values that fall off.  Where blocks of equal elements make the roundings of the products align it can be
- * more (up to 1e-2 seen in 150 such matrices, 1.3e-3 in the middle).  Deterministic, and a matrix has the same bits alone and in a batch.
+ * more (up to 1e-2 seen in 150 such matrices, 1.3e-3 in the middle).  A call of small matrices alone (sides of at most 128 and
+ * 8192, five steps at most) takes its polynomial from the m x m matrix A in 22 bits: within 1e-4 for independent elements, and
+ * within 4e-3 where singular values fall off over orders of magnitude (up to 1.1e-3 seen).
+ * Deterministic; among the matrices of one call the others do not change a matrix's bits, but whether all are small does.
  */
 typedef struct {
     const void *G;

@@ -38,15 +38,15 @@
 
 #include <cuda_fp16.h>
 
-#include "common.cuh"
+#include "orthogonalize.cuh"
 #include "tc_ptx.cuh"
 #include "tconv_host.cuh"
 
 namespace {
 
-constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr float kA = twn_detail::kNsA, kB = twn_detail::kNsB, kC = twn_detail::kNsC;
 constexpr float kStart = 256.0f;             // X of the first step is this much larger
-constexpr int kMaxItems = 32;
+constexpr int kMaxItems = twn_detail::kNsMaxItems;
 constexpr int kBlockBytes = 8192, kBlockHalves = kBlockBytes / 2;
 constexpr int kOpBytes = 2 * kBlockBytes, kStageBytes = 2 * kOpBytes;     // 128 rows (or columns) of each operand by 64
 constexpr int kPairStages = 5, kTileStages = 3;
@@ -1148,9 +1148,35 @@ int make_maps(CUtensorMap (&map)[2], void *base, size_t bytes)
     return TWN_OK;
 }
 
+// Where every matrix of the call is small: one launch for all of it (64 x 576 113 us as fifteen products, see orthogonalize_small.cu).
+// In a call with larger ones they ride along in the launches of those.
+bool all_small(const NsParams &P, int steps)
+{
+    for (int t = 0; t < P.count; ++t)
+        if (P.item[t].m > twn_detail::kNsSmallM || P.item[t].n > twn_detail::kNsSmallN) return false;
+    return steps <= twn_detail::kNsSmallSteps;
+}
+int run_small(const NsParams &P, int steps, cudaStream_t s)
+{
+    twn_detail::NsSmallParams S = {};
+    S.count = P.count;
+    S.steps = steps;
+    S.look_ahead = P.look_ahead;
+    S.momentum = P.momentum;
+    S.eps = P.eps;
+    S.status = P.status;
+    for (int t = 0; t < P.count; ++t) {
+        const NsItem &it = P.item[t];
+        static_assert(2 * 4 * kBlockBytes >= twn_detail::kNsSmallScratch, "A and B, one after the other, hold the small path's scratch");
+        S.item[t] = {{it.G, it.dW, it.V, it.O, it.m, it.n, it.out_scale, it.g_bf16, it.o_bf16, it.tall, it.vec_in, it.vec_out}, it.A};
+    }
+    return twn_detail::ns_small(S, s);
+}
+
 // The items of P are placed from `base` on, within `bytes`.
 int run_steps(NsParams &P, int steps, char *base, size_t bytes, cudaStream_t s)
 {
+    if (all_small(P, steps)) return run_small(P, steps, s);
     P.base = reinterpret_cast<const uint16_t *>(base);
     enum { kNorm, kStartList, kSymPair, kGramTile, kSquareTile, kApplyPair, kApplyTile, kLists };
     NsParams list[kLists];

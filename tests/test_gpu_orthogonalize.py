@@ -120,13 +120,105 @@ def test_scales():
     assert bool((_run([torch.zeros(70, 90, device="cuda")])[0] == 0).all())
 
 
-def test_a_batch_gives_the_bits_of_single_calls_and_repeats_them():
-    shapes = [(64, 576), (512, 64), (1, 1), (300, 300), (129, 127), (1000, 512), (5, 2000), (256, 2304)] * 4
+@pytest.mark.parametrize("shapes", [[(64, 576), (512, 64), (1, 1), (100, 128), (128, 128), (128, 8192), (5, 2000), (8192, 3)] * 4,
+                                    [(300, 300), (129, 131), (1000, 512), (256, 2304), (1500, 2700), (7000, 200)] * 3])
+def test_a_batch_gives_the_bits_of_single_calls_and_repeats_them(shapes):
     Gs = [_normal(40 + i, r, c).to(B if i % 3 == 0 else F) for i, (r, c) in enumerate(shapes)]
     types = [B if i % 2 else F for i in range(len(Gs))]
     many, again = _run(Gs, types), _run(Gs, types)
     for G, t, O, O2 in zip(Gs, types, many, again):
         assert torch.equal(O, O2) and torch.equal(_run([G], t)[0], O)
+
+
+@pytest.mark.parametrize("gt,ot", [(F, F), (B, B)])
+def test_small_matrices_among_larger_ones(gt, ot):
+    shapes = [s for s in SHAPES if min(s) <= 128] + [(150, 200)]
+    Gs = [(0.01 * _normal(sum(s), *s)).to(gt) for s in shapes]
+    for G, O in zip(Gs, _run(Gs, ot)):
+        _check(G, O, 1e-3 if min(G.shape) >= 64 else 4e-3)
+
+
+SMALL = [(1, 1), (1, 8192), (8192, 1), (3, 5), (31, 33), (64, 64), (64, 147), (147, 64), (100, 1000), (999, 101), (127, 129), (128, 128), (128, 8192), (8192, 128), (128, 8193), (129, 700)]
+
+
+@pytest.mark.parametrize("rows,cols", SMALL)
+@pytest.mark.parametrize("gt,ot", [(F, F), (B, B), (F, B), (B, F)])
+@pytest.mark.parametrize("steps", [1, 2, 5, 6])
+def test_small_matrices(rows, cols, gt, ot, steps):
+    G = (0.01 * _normal(rows + cols, rows, cols)).to(gt)
+    # one launch of its own: 1e-3 for any of them
+    _check(G, _run([G], ot, steps=steps)[0], 1e-3 if max(rows, cols) <= 8192 and min(rows, cols) in range(2, 129) and steps <= 5 else 4e-3, steps)
+
+
+@pytest.mark.parametrize("rows,cols", [(96, 700), (700, 96), (128, 128), (40, 3000)])
+@pytest.mark.parametrize("kind", ["rank1", "rank4", "rank32", "power1", "power2", "power3", "identity", "ones", "blocks"])
+def test_spectra_of_small_matrices(rows, cols, kind):
+    m = min(rows, cols)
+    if kind == "identity":
+        G = torch.eye(rows, cols, device="cuda")
+    elif kind == "ones":
+        G = torch.ones(rows, cols, device="cuda")
+    elif kind == "blocks":
+        G = torch.zeros(rows, cols, device="cuda")
+        G.view(-1)[::cols + 1] = 1.0
+        G = G[:rows // 4, :cols // 4].repeat_interleave(4, 0).repeat_interleave(4, 1).contiguous()
+    elif kind.startswith("rank"):
+        k = int(kind[4:])
+        G = _normal(3, rows, k) @ _normal(4, k, cols)
+    else:
+        u, _ = torch.linalg.qr(_normal(5, rows, m).double())
+        v, _ = torch.linalg.qr(_normal(6, cols, m).double())
+        G = ((u * torch.arange(1, m + 1, device="cuda").double() ** -int(kind[5:])) @ v.T).float()
+    O = _run([G])[0]
+    # Elements of A = X X^T are off by 2^-22 of their value (its two fp16 parts), so its eigenvalues s^2 by 2^-22 of the trace, 1, at most.
+    # The result for s is s times a product of a + b t + c t^2 over t = s^2, 11.9 s^2, ...; for s = 2e-3, the least that five steps bring to
+    # about 1, t is off by 6 % and reaches 0.08 in the last factor, which changes by 4.775 * 0.08 / 3.06 * 6 % = 0.75 %.  Larger s are off
+    # by less (the shift is the same, and t stops growing), smaller ones come out as 485 s, with a smaller share of t.  A spectrum that falls off
+    # has less than a quarter of its result (in squares) there: 0.75 % / 2 = 3.8e-3.  Rank one, equal elements and the identity have
+    # singular values 1 and 0 alone.
+    assert float((O.double() - _exact(G)).norm()) <= (4e-3 if kind.startswith("power") else 1e-3) * float(_exact(G).norm())
+
+
+def test_scales_of_small_matrices():
+    G = _normal(9, 60, 300)
+    want = _run([G])[0]
+    for scale in (2.0 ** -60, 2.0 ** 60, 2.0 ** 120, 2.0 ** -100):
+        assert float((_run([G * scale], eps=1e-30)[0] - want).norm()) <= 1e-5 * float(want.norm())
+    for scale in (2.0 ** -60, 2.0 ** 100):
+        assert float((_run([(G * scale).to(B)], eps=1e-30)[0] - _run([G.to(B)])[0]).norm()) <= 1e-5 * float(want.norm())
+    tiny = G * (1e-9 / float(G.norm()))
+    O = _run([tiny], steps=1, eps=1e-7)[0]
+    assert float((O.double() - NS[0] * 0.01 * G.double() / float(G.norm())).norm()) <= 1e-3 * NS[0] * 0.01
+    assert bool((_run([torch.zeros(70, 90, device="cuda")])[0] == 0).all())
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_nonfinite_small_matrices(bad):
+    Gs = [_normal(60 + i, r, c) for i, (r, c) in enumerate([(70, 300), (300, 70), (128, 128)])]
+    clean = _run(Gs)
+    Gs[1][299, 3] = bad
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    Os = _run(Gs, status=status)
+    assert twn.read_status(status) == -4 and bool(Os[1].isnan().all())
+    assert torch.equal(Os[0], clean[0]) and torch.equal(Os[2], clean[2])
+
+
+def test_small_matrices_in_place_unaligned_and_on_streams():
+    for r, c in ((100, 333), (333, 100)):
+        G = _normal(51, r, c)
+        want = _run([G])[0]
+        buf = torch.empty(r * c + 1, device="cuda")[1:].view(r, c)
+        buf.copy_(G)
+        ws = [workspace(twn.orthogonalize_workspace_bytes([(r, c)])) for _ in range(3)]
+        twn.orthogonalize_batch([(buf, r, c, buf)], 5, 1e-7, ws[0])
+        assert torch.equal(buf, want)
+        outs, streams = [torch.empty_like(G) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for O, w, st in zip(outs, ws[1:], streams):
+                twn.orthogonalize_batch([(G, r, c, O)], 5, 1e-7, w, stream=st)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
 
 
 def test_empty_matrices_are_skipped_and_output_may_be_the_input():
@@ -190,7 +282,7 @@ def _f32(a, b, c):
 
 
 @pytest.mark.parametrize("look", [False, True])
-@pytest.mark.parametrize("shapes", [[(64, 576)], [(10, 1024), (512, 64), (300, 300), (1, 33), (1000, 512)]])
+@pytest.mark.parametrize("shapes", [[(64, 576)], [(64, 147), (300, 64), (1, 33), (128, 1152)], [(10, 1024), (512, 64), (300, 300), (1, 33), (1000, 512)]])
 def test_muon_steps(look, shapes):
     lr, mu, wd = (float(np.float32(v)) for v in (0.02, 0.95, 0.1))
     W = [0.05 * _normal(90 + i, r, c) for i, (r, c) in enumerate(shapes)]
