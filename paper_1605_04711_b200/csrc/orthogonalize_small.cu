@@ -33,7 +33,8 @@ namespace {
 
 using namespace twn_detail;
 
-constexpr int kThreads = 256;                // eight warps: two per lane quadrant of tensor memory
+constexpr int kThreads = 512;                // sixteen warps: each has 32 rows and 32 columns of a matrix
+constexpr int kQuads = 128 * 64 / 4 / kThreads;
 constexpr int kCluster = 8;
 constexpr uint32_t kHalfMatrix = 32 * 1024, kMatrix = 2 * kHalfMatrix;      // 128 x 128 fp16; its upper and lower parts
 constexpr float kScaleA = 4096.0f, kScaleB = 1024.0f, kScaleT = 4096.0f, kScaleQ = 64.0f, kScaleX = 256.0f;
@@ -106,15 +107,13 @@ __device__ __forceinline__ void two_parts(float a, float b, uint32_t &hi, uint32
 
 // Four elements of G from row `row` (of its own shape) and column `col` on, zeros past its end; with UPDATE the momentum is
 // updated on the way.
-template <bool UPDATE> __device__ __forceinline__ float4 four(const NsSource &it, const NsSmallParams &P, int row, int col)
+enum { kF32, kBf16, kMuon };
+template <int KIND, bool UPDATE> __device__ __forceinline__ float4 four(const NsSource &it, const NsSmallParams &P, int row, int col, int rows, int cols, bool vec)
 {
-    const int rows = it.tall ? it.n : it.m, cols = it.tall ? it.m : it.n;
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (row < rows && col < cols) {
-        const long long i = (long long)row * cols + col;
-        const bool vec = it.vec_in && (cols & 3) == 0;
-        const int left = min(4, cols - col);
-        if (it.V) {
+        const int i = row * cols + col, left = cols - col;
+        if (KIND == kMuon) {
             float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             if (vec) {
                 const float4 a = *reinterpret_cast<const float4 *>(it.V + i), b = *reinterpret_cast<const float4 *>(it.dW + i);
@@ -139,7 +138,7 @@ template <bool UPDATE> __device__ __forceinline__ float4 four(const NsSource &it
             if (P.look_ahead)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = __fadd_rn(d[j], __fmul_rn(P.momentum, v[j]));
-        } else if (it.g_bf16) {
+        } else if (KIND == kBf16) {
             const uint16_t *g = static_cast<const uint16_t *>(it.G) + i;
             if (vec) {
                 const uint2 w = *reinterpret_cast<const uint2 *>(g);
@@ -175,12 +174,12 @@ __device__ __forceinline__ Quad quad_of(bool tall, int b, int i)
     const int tid = threadIdx.x;
     Quad q;
     if (tall) {
-        const int c = 4 * (tid & 31), r = (tid >> 5) + 8 * i;
+        const int c = 4 * (tid & 31), r = (tid >> 5) + (kThreads / 32) * i;
         q.row = 64 * b + r;
         q.col = c;
         q.at = (uint32_t)(c >> 6) * 8192 + swizzled(r, c & 63);
     } else {
-        const int c = 4 * (tid & 15), r = (tid >> 4) + 16 * i;
+        const int c = 4 * (tid & 15), r = (tid >> 4) + (kThreads / 16) * i;
         q.row = r;
         q.col = 64 * b + c;
         q.at = swizzled(r, c);
@@ -188,16 +187,15 @@ __device__ __forceinline__ Quad quad_of(bool tall, int b, int i)
     return q;
 }
 
-// D = P R^T (three products of two parts each, the small ones first) of two matrices of 128 x 128 in shared memory, by the calling
+// D = P R^T (three products of two parts each, the small ones first) of two matrices of mm x mm in shared memory, by the calling
 // thread.
-__device__ __forceinline__ void product(uint32_t d, uint32_t p, uint32_t r)
+__device__ __forceinline__ void product(uint32_t d, uint32_t p, uint32_t r, int mm)
 {
-    constexpr uint32_t idesc = idesc_f16(128, false);
+    const uint32_t idesc = idesc_f16(mm, false);
 #pragma unroll
     for (int combo = 0; combo < 3; ++combo) {
         const uint64_t a = smem_desc_sw128(p + (combo == 1 ? kHalfMatrix : 0)), b = smem_desc_sw128(r + (combo == 0 ? kHalfMatrix : 0));
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < mm / 16; ++k) {
             const uint64_t off = (uint64_t)((k >> 2) * (16384 >> 4) + 2 * (k & 3));
             mma(d, a + off, b + off, idesc, combo + k > 0);
         }
@@ -239,7 +237,22 @@ __device__ __forceinline__ void tmem_row32(uint32_t taddr, float (&v)[32])
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(w[j]);
 }
 
-__global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_constant__ NsSmallParams P)
+__device__ __forceinline__ void tmem_row16(uint32_t taddr, float (&v)[16])
+{
+    uint32_t w[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]), "=r"(w[8]), "=r"(w[9]),
+                   "=r"(w[10]), "=r"(w[11]), "=r"(w[12]), "=r"(w[13]), "=r"(w[14]), "=r"(w[15])
+                 : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]), "+r"(w[4]), "+r"(w[5]), "+r"(w[6]), "+r"(w[7]), "+r"(w[8]), "+r"(w[9]),
+                   "+r"(w[10]), "+r"(w[11]), "+r"(w[12]), "+r"(w[13]), "+r"(w[14]), "+r"(w[15])
+                 :: "memory");
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(w[j]);
+}
+
+template <int KIND> __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_constant__ NsSmallParams P)
 {
     extern __shared__ uint8_t smem_raw[];
     SmallSmem *sm = reinterpret_cast<SmallSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -280,35 +293,37 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
     const bool tall = it.tall != 0;
     const int blocks = (it.n + 63) >> 6;                 // of 64 columns of X; this block has every eighth
     const int mine = rank < blocks ? (blocks - rank + kCluster - 1) / kCluster : 0;
-    const int q = warp & 3, half = warp >> 2, row = 32 * q + lane;
+    const int rows = tall ? it.n : it.m, cols = tall ? it.m : it.n;      // of G
+    const bool vec = it.vec_in && (cols & 3) == 0;
+    // rows and columns that are worked on (of the others nothing that is used depends), this thread's row and columns
+    const int mm = (it.m + 15) & ~15, q = warp & 3, row = 32 * q + lane, c = 32 * (warp >> 2);
+    const bool in = 32 * q < mm && c < mm;
     const uint32_t t_row = tmem + ((uint32_t)(32 * q) << 16);
 
     // ---- Gram matrix, its trace ------------------------------------------------------------------------------------------
     float pre = 1.0f, factor = 0.0f;
-    const int planes = it.g_bf16 && !it.V ? 1 : 3;
+    constexpr int planes = KIND == kBf16 ? 1 : 3;
 #pragma unroll 1
     for (int attempt = 0; attempt < 2; ++attempt) {
-        float4 next[8];
+        float4 next[kQuads];
         auto fetch = [&](int b) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < kQuads; ++i) {
                 const Quad at = quad_of(tall, b, i);
-                next[i] = attempt == 0 ? four<true>(it, P, at.row, at.col) : four<false>(it, P, at.row, at.col);
+                next[i] = attempt == 0 ? four<KIND, true>(it, P, at.row, at.col, rows, cols, vec) : four<KIND, false>(it, P, at.row, at.col, rows, cols, vec);
             }
         };
-        float total[64];
+        float total[32];
 #pragma unroll
-        for (int j = 0; j < 64; ++j) total[j] = 0.0f;
+        for (int j = 0; j < 32; ++j) total[j] = 0.0f;
         // the sums of a tile, of 64 columns of X, when its products are done
         auto take = [&](int s) {
             wait(s);
+            if (!in) return;
+            float v[32];
+            tmem_row32(t_row + (s ? kColQ : kColS) + c, v);
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                float v[32];
-                tmem_row32(t_row + (s ? kColQ : kColS) + 64 * half + 32 * g, v);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) total[32 * g + j] += v[j];
-            }
+            for (int j = 0; j < 32; ++j) total[j] += v[j];
         };
         if (mine > 0) fetch(rank);
 #pragma unroll 1
@@ -317,10 +332,12 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
             uint8_t *const tile = sm->mat[0] + s * 3 * 16384;      // planes of 16 KB
             if (k >= 2) take(s);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < kQuads; ++i) {
                 const Quad at = quad_of(tall, 0, i);
+                if ((tall ? at.col : at.row) >= mm) continue;
                 const float f[4] = {next[i].x * pre, next[i].y * pre, next[i].z * pre, next[i].w * pre};
                 float rest[4] = {f[0], f[1], f[2], f[3]};
+#pragma unroll
                 for (int p = 0; p < planes; ++p) {
                     const uint2 w = make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
                     *reinterpret_cast<uint2 *>(tile + p * 16384 + at.at) = w;
@@ -332,14 +349,14 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
             ready();
             if (warp == 0 && elect_one()) {
                 const uint32_t base = smem_u32(tile);
-                const uint32_t idesc = tall ? make_idesc_mn(128, 128) : make_idesc(128, 128);
+                const uint32_t idesc = tall ? make_idesc_mn(128, mm) : make_idesc(128, mm);
                 // the product of the upper parts, and apart from it, in sums of their own, those with a lower one
-                for (int c = 0; c < (planes == 1 ? 1 : 6); ++c) {
-                    const int pa = c == 2 || c == 5 ? 1 : c == 4 ? 2 : 0, pb = c == 1 || c == 5 ? 1 : c == 3 ? 2 : 0;
+                for (int o = 0; o < (planes == 1 ? 1 : 6); ++o) {
+                    const int pa = o == 2 || o == 5 ? 1 : o == 4 ? 2 : 0, pb = o == 1 || o == 5 ? 1 : o == 3 ? 2 : 0;
                     const uint32_t a = base + pa * 16384, b = base + pb * 16384;
                     const uint64_t da = tall ? smem_desc_mn_sw128(a, 8192) : smem_desc_sw128(a), db = tall ? smem_desc_mn_sw128(b, 8192) : smem_desc_sw128(b);
                     const uint64_t step = tall ? 128 : 2;
-                    for (int j = 0; j < 4; ++j) mma(tmem + (c ? kColT : s ? kColQ : kColS), da + j * step, db + j * step, idesc, c ? k + c + j > 1 : j > 0);
+                    for (int j = 0; j < 4; ++j) mma(tmem + (o ? kColT : s ? kColQ : kColS), da + j * step, db + j * step, idesc, o ? k + o + j > 1 : j > 0);
                 }
                 tc_commit(&sm->bar[s]);
             }
@@ -348,29 +365,24 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
         for (int k = max(0, mine - 2); k < mine; ++k) take(k & 1);
         // this block's sums to shared memory (behind the tiles), row by row
         float *const sums = reinterpret_cast<float *>(sm->mat[2]);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const int c = 64 * half + 32 * g;
+        if (in) {
             float v[32];
             if (mine > 0 && planes > 1) {
                 tmem_row32(t_row + kColT + c, v);
-            } else {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+                for (int j = 0; j < 32; ++j) total[j] += v[j];
             }
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] += total[32 * g + j];
             // 16-byte pieces exchanged by the row, so that a warp's writes spread over the banks
 #pragma unroll
             for (int p = 0; p < 8; ++p)
-                *reinterpret_cast<float4 *>(sums + row * 128 + ((((c >> 2) + p) ^ lane) & 31) * 4) = make_float4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
+                *reinterpret_cast<float4 *>(sums + row * 128 + ((((c >> 2) + p) ^ lane) & 31) * 4) = make_float4(total[4 * p], total[4 * p + 1], total[4 * p + 2], total[4 * p + 3]);
         }
         tc_fence_before();
         whole_cluster();
-        // sixteen rows each, the blocks' sums in their order, to block 0
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int i = tid + e * kThreads, r = 16 * rank + (i >> 5);
+        // an eighth of the rows each, the blocks' sums in their order, to block 0
+        for (int i = tid; i < mm / kCluster * 32; i += kThreads) {
+            const int r = mm / kCluster * rank + (i >> 5);
+            if (4 * (i & 31) >= mm) continue;
             const uint32_t at = (uint32_t)(r * 512 + (((i & 31) ^ r) & 31) * 16);
             float4 part[kCluster];
 #pragma unroll
@@ -384,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
         if (rank == 0) {
             const float *const gram = reinterpret_cast<const float *>(sm->mat[1]);
             double d = 0.0;
-            if (tid < 128) d = gram[tid * 128 + (((tid >> 2) ^ tid) & 31) * 4 + (tid & 3)];
+            if (tid < mm) d = gram[tid * 128 + (((tid >> 2) ^ tid) & 31) * 4 + (tid & 3)];
             for (int o = 16; o > 0; o >>= 1) d += __shfl_down_sync(0xffffffffu, d, o);
             if (lane == 0) sm->red[warp] = d;
             __syncthreads();
@@ -411,9 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
     if (rank == 0) {
         {
             const float *const gram = reinterpret_cast<const float *>(sm->mat[1]);
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int c = 64 * half + 32 * g;
+            if (in) {
                 float v[32], w[32];
 #pragma unroll
                 for (int p = 0; p < 8; ++p) {
@@ -436,15 +446,13 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
             const bool last = step + 1 == P.steps;
             ready();
             if (warp == 0 && elect_one()) {
-                product(tmem + kColS, smem_u32(sm->mat[0]), smem_u32(sm->mat[0]));
+                product(tmem + kColS, smem_u32(sm->mat[0]), smem_u32(sm->mat[0]), mm);
                 tc_commit(&sm->bar[0]);
             }
             __syncwarp();
             wait(0);
             // B' = b A + c A A; of Q' what it has beside the product
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int c = 64 * half + 32 * g;
+            if (in) {
                 float a[32], v[32];
                 tmem_row32(t_row + kColA + c, a);
                 tmem_row32(t_row + kColS + c, v);
@@ -468,16 +476,14 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
             if (last && step == 0) break;
             ready();
             if (warp == 0 && elect_one()) {
-                if (!last) product(tmem + kColT, smem_u32(sm->mat[1]), smem_u32(sm->mat[0]));
-                if (step > 0) product(tmem + kColS, smem_u32(sm->mat[1]), smem_u32(sm->mat[2]));
+                if (!last) product(tmem + kColT, smem_u32(sm->mat[1]), smem_u32(sm->mat[0]), mm);
+                if (step > 0) product(tmem + kColS, smem_u32(sm->mat[1]), smem_u32(sm->mat[2]), mm);
                 tc_commit(&sm->bar[0]);
             }
             __syncwarp();
             wait(0);
             // T = a A + B' A, Q'
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int c = 64 * half + 32 * g;
+            if (in) {
                 float a[32], v[32];
                 if (!last) {
                     tmem_row32(t_row + kColA + c, a);
@@ -503,15 +509,13 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
             if (last) break;
             ready();
             if (warp == 0 && elect_one()) {
-                product(tmem + kColS, smem_u32(sm->mat[0]), smem_u32(sm->mat[1]));
+                product(tmem + kColS, smem_u32(sm->mat[0]), smem_u32(sm->mat[1]), mm);
                 tc_commit(&sm->bar[0]);
             }
             __syncwarp();
             wait(0);
             // A = a T + T B'
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int c = 64 * half + 32 * g;
+            if (in) {
                 float a[32], v[32];
                 tmem_row32(t_row + kColA + c, a);
                 tmem_row32(t_row + kColS + c, v);
@@ -530,18 +534,21 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
 
     // ---- O = Q X0 ----------------------------------------------------------------------------------------------------------
     if (rank != 0)
-        for (int i = tid; i < (int)(kMatrix / 16); i += kThreads)
-            reinterpret_cast<uint4 *>(sm->mat[2])[i] = __ldcg(reinterpret_cast<const uint4 *>(scratch) + i);
+        for (int i = tid; i < 2 * mm * (mm / 8); i += kThreads) {
+            const int piece = i % (mm / 8), r = i / (mm / 8) % mm, part = i / (mm / 8) / mm;
+            const uint32_t at = (uint32_t)part * kHalfMatrix + (uint32_t)(piece >> 3) * 16384 + swizzled(r, 8 * (piece & 7));
+            *reinterpret_cast<uint4 *>(sm->mat[2] + at) = __ldcg(reinterpret_cast<const uint4 *>(scratch + at));
+        }
     const float x_scale = factor * kScaleX, unscale = 1.0f / (kScaleQ * kScaleX);
     float power = kScaleQ;                               // a^steps, beside the product
     for (int k = 0; k < P.steps; ++k) power *= kNsA;
     {
-        float4 next[8];
+        float4 next[kQuads];
         auto fetch = [&](int b) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < kQuads; ++i) {
                 const Quad at = quad_of(tall, b, i);
-                next[i] = four<false>(it, P, at.row, at.col);
+                next[i] = four<KIND, false>(it, P, at.row, at.col, rows, cols, vec);
             }
         };
         if (mine > 0) fetch(rank);
@@ -551,8 +558,9 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
             if (k < mine) {
                 uint8_t *const tile = sm->mat[0] + (k & 1) * 32768;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < kQuads; ++i) {
                     const Quad at = quad_of(tall, 0, i);
+                    if ((tall ? at.col : at.row) >= mm) continue;
                     uint32_t h[2], l[2];
                     two_parts(next[i].x * pre * x_scale, next[i].y * pre * x_scale, h[0], l[0]);
                     two_parts(next[i].z * pre * x_scale, next[i].w * pre * x_scale, h[1], l[1]);
@@ -568,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
                         const uint64_t a = smem_desc_sw128(qa + (combo == 1 ? kHalfMatrix : 0));
                         const uint32_t x = xb + (combo == 0 ? 16384 : 0);
                         const uint64_t b = tall ? smem_desc_sw128(x) : smem_desc_mn_sw128(x, 8192);
-                        for (int j = 0; j < 8; ++j) {
+                        for (int j = 0; j < mm / 16; ++j) {
                             const uint64_t a_off = (uint64_t)((j >> 2) * (16384 >> 4) + 2 * (j & 3));
                             const uint64_t b_off = tall ? (uint64_t)((j >> 2) * (8192 >> 4) + 2 * (j & 3)) : (uint64_t)(128 * j);
                             mma(tmem + 64 * (k & 1), a + a_off, b + b_off, idesc, combo + j > 0);
@@ -581,39 +589,41 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
             if (k == 0) continue;
             const int done = k - 1, b = rank + done * kCluster;
             wait(done & 1);
-            float v[32];
-            const int c0 = 64 * b + 32 * half;
-            tmem_row32(t_row + 64 * (done & 1) + 32 * half, v);
+            // a thread has 16 of the tile's 64 columns
+            const int part = 16 * (warp >> 2), c0 = 64 * b + part;
+            float d[16];
+            tmem_row16(t_row + 64 * (done & 1) + part, d);
             tc_fence_before();
-            {
-                const uint8_t *const tile = sm->mat[0] + (done & 1) * 32768;
-                if (tall) {
+            if (row < it.m) {
+                float v[16];
+                {
+                    const uint8_t *const tile = sm->mat[0] + (done & 1) * 32768;
+                    if (tall) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const uint32_t at = (uint32_t)(row >> 6) * 8192 + swizzled(32 * half + j, row & 63);
-                        v[j] = fmaf(power, __half2float(*reinterpret_cast<const __half *>(tile + at)) + __half2float(*reinterpret_cast<const __half *>(tile + 16384 + at)), v[j]);
-                    }
-                } else {
+                        for (int j = 0; j < 16; ++j) {
+                            const uint32_t at = (uint32_t)(row >> 6) * 8192 + swizzled(part + j, row & 63);
+                            v[j] = __half2float(*reinterpret_cast<const __half *>(tile + at)) + __half2float(*reinterpret_cast<const __half *>(tile + 16384 + at));
+                        }
+                    } else {
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        const uint32_t at = swizzled(row, 32 * half + 8 * p);
-                        const uint4 h = *reinterpret_cast<const uint4 *>(tile + at), l = *reinterpret_cast<const uint4 *>(tile + 16384 + at);
-                        const uint32_t hs[4] = {h.x, h.y, h.z, h.w}, ls[4] = {l.x, l.y, l.z, l.w};
+                        for (int p = 0; p < 2; ++p) {
+                            const uint32_t at = swizzled(row, part + 8 * p);
+                            const uint4 h = *reinterpret_cast<const uint4 *>(tile + at), l = *reinterpret_cast<const uint4 *>(tile + 16384 + at);
+                            const uint32_t hs[4] = {h.x, h.y, h.z, h.w}, ls[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float2 a = from_half_pair(hs[j]), b2 = from_half_pair(ls[j]);
-                            v[8 * p + 2 * j] = fmaf(power, a.x + b2.x, v[8 * p + 2 * j]);
-                            v[8 * p + 2 * j + 1] = fmaf(power, a.y + b2.y, v[8 * p + 2 * j + 1]);
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 x = from_half_pair(hs[j]), y = from_half_pair(ls[j]);
+                                v[8 * p + 2 * j] = x.x + y.x;
+                                v[8 * p + 2 * j + 1] = x.y + y.y;
+                            }
                         }
                     }
                 }
-            }
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = v[j] * unscale * it.out_scale;
-            if (row < it.m) {
+                for (int j = 0; j < 16; ++j) v[j] = fmaf(power, v[j], d[j]) * unscale * it.out_scale;
                 if (!tall && it.vec_out) {
 #pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
+                    for (int j = 0; j < 16; j += 8) {
                         if (c0 + j >= it.n) break;
                         const long long at = (long long)row * it.n + c0 + j;
                         if (it.o_bf16) {
@@ -627,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
                     }
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
+                    for (int j = 0; j < 16; ++j) {
                         if (c0 + j >= it.n) break;
                         const long long at = tall ? (long long)(c0 + j) * it.m + row : (long long)row * it.n + c0 + j;
                         if (it.o_bf16) static_cast<__nv_bfloat16 *>(it.O)[at] = __float2bfloat16_rn(v[j]);
@@ -654,15 +664,19 @@ __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_cons
 
 }  // namespace
 
-int twn_detail::ns_small(const NsSmallParams &P, cudaStream_t s)
+template <int KIND> static int launch(const NsSmallParams &all, const twn_device_info &dev, cudaStream_t s)
 {
-    twn_device_info dev;
-    const int rc = twn_current_device(&dev);
-    if (rc != TWN_OK) return rc;
+    NsSmallParams P = all;
+    P.count = 0;
+    for (int t = 0; t < all.count; ++t) {
+        const NsSource &it = all.item[t].src;
+        if ((it.V ? kMuon : it.g_bf16 ? kBf16 : kF32) == KIND) P.item[P.count++] = all.item[t];
+    }
+    if (P.count == 0) return TWN_OK;
     static bool done[64] = {false};
     const int smem = (int)sizeof(SmallSmem) + 1024;
     if (!done[dev.ordinal]) {
-        TWN_CUDA_OK(cudaFuncSetAttribute(ns_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        TWN_CUDA_OK(cudaFuncSetAttribute(ns_small_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
         done[dev.ordinal] = true;
     }
     cudaLaunchAttribute attr[2];
@@ -678,6 +692,16 @@ int twn_detail::ns_small(const NsSmallParams &P, cudaStream_t s)
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    TWN_CUDA_OK(cudaLaunchKernelEx(&cfg, ns_small_kernel, P));
+    TWN_CUDA_OK(cudaLaunchKernelEx(&cfg, ns_small_kernel<KIND>, P));
     return TWN_OK;
+}
+
+int twn_detail::ns_small(const NsSmallParams &P, cudaStream_t s)
+{
+    twn_device_info dev;
+    int rc = twn_current_device(&dev);
+    if (rc == TWN_OK) rc = launch<kF32>(P, dev, s);
+    if (rc == TWN_OK) rc = launch<kBf16>(P, dev, s);
+    if (rc == TWN_OK) rc = launch<kMuon>(P, dev, s);
+    return rc;
 }
