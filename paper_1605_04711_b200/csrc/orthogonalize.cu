@@ -49,7 +49,7 @@ constexpr float kStart = 256.0f;             // X of the first step is this much
 constexpr int kMaxItems = twn_detail::kNsMaxItems;
 constexpr int kBlockBytes = 8192, kBlockHalves = kBlockBytes / 2;
 constexpr int kOpBytes = 2 * kBlockBytes, kStageBytes = 2 * kOpBytes;     // 128 rows (or columns) of each operand by 64
-constexpr int kPairStages = 5, kTileStages = 3;
+constexpr int kPairStages = 5;
 constexpr int kEpiWarps = 8, kWarpTile = 32 * 64;
 constexpr int kNsThreads = 32 * (2 + kEpiWarps);
 constexpr int kMaxSplit = 4;                 // blocks that share a tile's reduction: a cluster
@@ -259,12 +259,17 @@ __global__ void __launch_bounds__(kSweepBlock) ns_start_kernel(const __grid_cons
         if (!direct) {
             // rows of G along the threads of a warp
             __syncthreads();
-            for (int e = threadIdx.x; e < 4096; e += kSweepBlock) {
-                const int i = e >> 6, j = e & 63;
-                const int r = r0 + (it.tall ? j : i), c = c0 + (it.tall ? i : j);
-                float v = 0.0f;
-                if (r < it.m && c < it.n) v = element(it, P, it.tall ? (long long)c * it.m + r : (long long)r * it.n + c);
-                tile[it.tall ? j : i][it.tall ? i : j] = v;
+            const int rows = it.tall ? it.n : it.m, cols = it.tall ? it.m : it.n;
+            const int j = threadIdx.x & 63, i0 = threadIdx.x >> 6, col = (it.tall ? r0 : c0) + j, row = (it.tall ? c0 : r0) + i0;
+            float v[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = row + 4 * k < rows && col < cols ? element(it, P, (long long)(row + 4 * k) * cols + col) : 0.0f;
+            if (it.tall) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) tile[j][i0 + 4 * k] = v[k];
+            } else {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) tile[i0 + 4 * k][j] = v[k];
             }
             __syncthreads();
         }
@@ -617,22 +622,25 @@ __device__ __forceinline__ void store_out8(const NsItem &it, long long at, const
     }
 }
 
-// X of the next step, or the result.
-__device__ __forceinline__ void finish_apply(const NsItem &it, const NsParams &P, Ahead<kApply> &ahead, float *buf, int r0, int c0)
+// X of the next step, or the result.  DEEP: the second half of the operands is on its way while the first is worked on (32 registers).
+template <bool DEEP> __device__ __forceinline__ void finish_apply(const NsItem &it, const NsParams &P, Ahead<kApply> &ahead, float *buf, int r0, int c0)
 {
     const int lane = threadIdx.x & 31, p = lane & 7, cur = P.step & 1;
     const float unscale = P.step == 0 ? 1.0f / kStart : 1.0f;
     uint16_t *const next = it.x[cur ^ 1], *const rest = it.lo;
     const Pieces at(it, r0, c0);
+    Ahead<kApply> second;
+    if (DEEP) second.load4(it, P, r0, c0, 4);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-        if (u == 4) ahead.load4(it, P, r0, c0, 4);
+        if (!DEEP && u == 4) ahead.load4(it, P, r0, c0, 4);
+        const Ahead<kApply> &now = DEEP && u >= 4 ? second : ahead;
         const int r = 4 * u + (lane >> 3);
         const float k = kA + ahead.row[u];
         float v[8], h[8], l[8];
         row_sums8(buf, r, p, v);
-        unpack_half8(ahead.hi[u & 3], h);
-        unpack_half8(ahead.lo[u & 3], l);
+        unpack_half8(now.hi[u & 3], h);
+        unpack_half8(now.lo[u & 3], l);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = (k * (h[j] + l[j]) + v[j]) * unscale;
         if (P.last) {
@@ -837,7 +845,7 @@ ns_pair_kernel(const __grid_constant__ CUtensorMap rows128, const __grid_constan
                     __syncwarp();
                     if (lane == 0) arrive_at(of_block(smem_u32(&sm->acc_empty[lu & 1]), 0));
                 }
-                if constexpr (PHASE == kApply) finish_apply(it, P, ahead, buf, r0, c0);
+                if constexpr (PHASE == kApply) finish_apply<true>(it, P, ahead, buf, r0, c0);
                 else finish_symmetric<PHASE>(it, P, ahead, buf, r0, c0, J < I);
                 __syncwarp();
             }
@@ -861,24 +869,26 @@ ns_pair_kernel(const __grid_constant__ CUtensorMap rows128, const __grid_constan
 }
 
 // ---- small products ------------------------------------------------------------------------------------------------------
-// A 128x128 tile a block, two blocks on an SM.  `split` blocks of a cluster share a tile's reduction; each leaves its sums in
+// A 128x128 tile a block, two blocks on an SM with rings of three stages, or one with six where there are no more blocks than SMs (a
+// block's reduction of 64 took 0.46 us with three, 1.5 times what the feed from L2 needs).  `split` blocks of a cluster share a tile's reduction; each leaves its sums in
 // the shared memory that was its ring, and finishes every split-th unit of the whole tile.
-struct __align__(1024) TileSmem {
+template <int STAGES> struct __align__(1024) TileSmem {
     union {
-        uint8_t ring[kTileStages][kStageBytes];
+        uint8_t ring[STAGES][kStageBytes];
         float sums[kEpiWarps][kWarpTile];
     };
-    unsigned long long full[kTileStages], empty[kTileStages], acc_full;
+    unsigned long long full[STAGES], empty[STAGES], acc_full;
     uint32_t tmem_base;
     volatile int abort_flag;
 };
 
-template <int PHASE>
-__global__ void __launch_bounds__(kNsThreads, 2) ns_tile_kernel(const __grid_constant__ NsParams P, bool clustered)
+template <int PHASE, int kTileStages>
+__global__ void __launch_bounds__(kNsThreads, kTileStages > 3 ? 1 : 2) ns_tile_kernel(const __grid_constant__ NsParams P, bool clustered)
 {
     pdl_launch_dependents();
     extern __shared__ uint8_t smem_raw[];
-    TileSmem *sm = reinterpret_cast<TileSmem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    using Smem = TileSmem<kTileStages>;
+    Smem *sm = reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     volatile int *abort_flag = &sm->abort_flag;
     const int warp = threadIdx.x >> 5;
 
@@ -972,7 +982,7 @@ __global__ void __launch_bounds__(kNsThreads, 2) ns_tile_kernel(const __grid_con
             tc_fence_before();
             __syncwarp();
             if (split == 1) {
-                if constexpr (PHASE == kApply) finish_apply(it, P, ahead, sm->sums[w], r0, c0);
+                if constexpr (PHASE == kApply) finish_apply<(kTileStages > 3)>(it, P, ahead, sm->sums[w], r0, c0);
                 else finish_symmetric<PHASE>(it, P, ahead, sm->sums[w], r0, c0, j < i);
             }
         }
@@ -1119,17 +1129,22 @@ template <int PHASE> int launch_pair(const NsParams &P, const CUtensorMap (&map)
     TWN_CUDA_OK(launch_clusters(ns_pair_kernel<PHASE>, 2 * std::min(P.units, dev.sm_count / 2), 2, smem, s, map[0], map[1], P));
     return TWN_OK;
 }
-template <int PHASE> int launch_tile(const NsParams &P, const twn_device_info &dev, cudaStream_t s)
+template <int PHASE, int STAGES> int launch_tile(const NsParams &P, int grid, int cluster, const twn_device_info &dev, cudaStream_t s)
 {
     static bool done[64] = {false};
-    const size_t smem = sizeof(TileSmem) + 1024;
-    const int rc = allow_smem(ns_tile_kernel<PHASE>, smem, done[dev.ordinal]);
+    const size_t smem = sizeof(TileSmem<STAGES>) + 1024;
+    const int rc = allow_smem(ns_tile_kernel<PHASE, STAGES>, smem, done[dev.ordinal]);
     if (rc != TWN_OK) return rc;
+    TWN_CUDA_OK(launch_clusters(ns_tile_kernel<PHASE, STAGES>, grid, cluster, smem, s, P, cluster > 1));
+    return TWN_OK;
+}
+template <int PHASE> int launch_tile(const NsParams &P, const twn_device_info &dev, cudaStream_t s)
+{
     int cluster = 1;
     if (PHASE != kApply)
         for (int t = 0; t < P.count; ++t) cluster = std::max(cluster, P.item[t].split);
-    TWN_CUDA_OK(launch_clusters(ns_tile_kernel<PHASE>, (P.units + cluster - 1) / cluster * cluster, cluster, smem, s, P, cluster > 1));
-    return TWN_OK;
+    const int grid = (P.units + cluster - 1) / cluster * cluster;
+    return grid <= dev.sm_count ? launch_tile<PHASE, 6>(P, grid, cluster, dev, s) : launch_tile<PHASE, 3>(P, grid, cluster, dev, s);
 }
 
 // All blocks of the workspace as one matrix of 128-byte rows, in copies of 128 and of 64 of them.
