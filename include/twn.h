@@ -637,10 +637,12 @@ int twn_layer_norm_fwd(const void *X, int32_t x_dtype, int64_t ldx, int64_t M, i
 
 /*
  * Its backward pass.  With xh = (X - mean) * rstd and g = dY * gamma:
- *   dX[m,c]   = rstd * (g - sum_c g / C - xh * sum_c (g * xh) / C)
+ *   dX[m,c]   = rstd * (g - sum_c g / C - xh * sum_c (g * xh) / C)  (+ residual[m,c])
  *   dgamma[c] = sum_m dY[m,c] * xh[m,c],   dbeta[c] = sum_m dY[m,c]
  *   dY, X, dX  each TWN_F32 or TWN_BF16 with its own pitch, as above; dX may be dY or X itself (same type and pitch).
  *   gamma      fp32 [C] or NULL (1);  mean, rstd  fp32 [M], what twn_layer_norm_fwd wrote.
+ *   residual   type and pitch of dX, or NULL: a second branch of the gradient (the shortcut around a block that begins
+ *              with the norm), added before the rounding; may be dX itself.
  *   dX, dgamma, dbeta (fp32 [C]) are overwritten; each may be NULL.  M = 0 gives zero gradients.
  *   workspace  at least twn_layer_norm_bwd_workspace_bytes(M, C) bytes, 256-byte aligned; contents need not be
  *              preserved or initialised.  Two calls that overlap on the device must not share it.
@@ -649,8 +651,8 @@ int twn_layer_norm_fwd(const void *X, int32_t x_dtype, int64_t ldx, int64_t M, i
 size_t twn_layer_norm_bwd_workspace_bytes(int64_t M, int64_t C);
 int twn_layer_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy, const void *X, int32_t x_dtype, int64_t ldx,
                        int64_t M, int64_t C, const float *gamma, const float *mean, const float *rstd, void *dX,
-                       int32_t dx_dtype, int64_t lddx, float *dgamma, float *dbeta, void *workspace,
-                       size_t workspace_bytes, twn_stream_t stream);
+                       int32_t dx_dtype, int64_t lddx, const void *residual, float *dgamma, float *dbeta,
+                       void *workspace, size_t workspace_bytes, twn_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -198,7 +198,7 @@ PyObject *layer_norm_fwd(Args &a)
     return finish(twn_layer_norm_fwd, std::make_tuple(X.p, X.dtype, ldx, M, C, gamma, beta, eps, Y.p, Y.dtype, ldy, mean, rstd, stream));
 }
 
-// (dY, lddy, X, ldx, M, C, gamma, mean, rstd, dX, lddx, dgamma, dbeta, workspace, stream)
+// (dY, lddy, X, ldx, M, C, gamma, mean, rstd, dX, lddx, residual, dgamma, dbeta, workspace, stream)
 PyObject *layer_norm_bwd(Args &a)
 {
     const Typed dY = typed_tensor(a);
@@ -211,12 +211,15 @@ PyObject *layer_norm_bwd(Args &a)
     const Typed dX = typed_tensor(a);
     const int64_t lddx = integer_of(a.take());
     has_rows(dX, lddx, M, C);
+    const Typed residual = typed_tensor(a);
+    if (residual.p && residual.dtype != dX.dtype) type_error("the residual has the type of dX");
+    has_rows(residual, lddx, M, C);
     float *const dgamma = float_vector(a, C), *const dbeta = float_vector(a, C);
     void *const ws = get<void *>(a);
     const size_t ws_bytes = a.last_bytes;
     const twn_stream_t stream = get<twn_stream_t>(a);
     no_more(a);
-    return finish(twn_layer_norm_bwd, std::make_tuple(dY.p, dY.dtype, lddy, X.p, X.dtype, ldx, M, C, gamma, mean, rstd, dX.p, dX.dtype, lddx,
+    return finish(twn_layer_norm_bwd, std::make_tuple(dY.p, dY.dtype, lddy, X.p, X.dtype, ldx, M, C, gamma, mean, rstd, dX.p, dX.dtype, lddx, residual.p,
                                                       dgamma, dbeta, ws, ws_bytes, stream));
 }
 

@@ -36,6 +36,16 @@ template <> struct Vec<bf16, 8> {
         }
     }
 };
+template <> struct Vec<bf16, 4> {
+    uint2 r;
+    __device__ void load(const bf16 *p) { r = *reinterpret_cast<const uint2 *>(p); }
+    __device__ void zero() { r = make_uint2(0u, 0u); }
+    __device__ void get(float (&f)[4]) const
+    {
+        f[0] = __uint_as_float(r.x << 16); f[1] = __uint_as_float(r.x & 0xFFFF0000u);
+        f[2] = __uint_as_float(r.y << 16); f[3] = __uint_as_float(r.y & 0xFFFF0000u);
+    }
+};
 template <> struct Vec<float, 4> {
     float4 r;
     __device__ void load(const float *p) { r = *reinterpret_cast<const float4 *>(p); }
@@ -199,6 +209,14 @@ template <typename T, int V, int TT> __device__ __forceinline__ void read_vector
         v.zero();
     }
     v.get(f);
+}
+
+template <typename T, int V, int TT> __device__ __forceinline__ void add_vector(float (&f)[V], const T *row, const Columns<V, TT> &col, int j)
+{
+    float e[V];
+    read_vector(row, col, j, e);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] += e[i];
 }
 
 struct FwdParams {
@@ -486,6 +504,7 @@ __global__ void __launch_bounds__(1024) norm_fwd_long_kernel(const __grid_consta
 struct BwdParams {
     const void *dY, *X;
     void *dX;
+    const void *add;             // added to dX
     const float *gamma, *mean, *rstd;
     float *part;                 // [parts][2][C]: sums of dy xh, sums of dy; NULL where the caller wants neither
     float *row_sums;             // long rows: [M][2]
@@ -581,6 +600,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
         float f[E];
 #pragma unroll
         for (int i = 0; i < P2; ++i) each(mul2(fma2(xh[i], k1, add2(dy[i], k0)), scale), f[2 * i], f[2 * i + 1]);
+        if (P.add)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) add_vector(*reinterpret_cast<float(*)[V]>(f + j * V), static_cast<const TO *>(P.add) + r * P.lddx, col, j);
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (col.whole(j) || col(j) < C) store(o + col(j), *reinterpret_cast<const float(*)[V]>(f + j * V));
@@ -710,6 +732,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
             const float c0 = -sums[0] * inv, c1 = -sums[1] * inv;
             const two_f32 k0 = two(c0, c0), k1 = two(c1, c1);
             TO *o = static_cast<TO *>(P.dX) + r * P.lddx;
+            const TO *const add = P.add ? static_cast<const TO *>(P.add) + r * P.lddx : nullptr;
 #pragma unroll
             for (int e = 0; e < E; e += W) {
                 two_f32 xh[W / 2], d[W / 2], g[W / 2];
@@ -720,6 +743,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
 #pragma unroll
                 for (int h = 0; h < W; h += V) {
                     const int j = (e + h) / V;
+                    if (add) add_vector(*reinterpret_cast<float(*)[V]>(f + h), add, col, j);
                     if (col.whole(j) || col(j) < C) store(o + col(j), *reinterpret_cast<const float(*)[V]>(f + h));
                 }
             }
@@ -817,7 +841,17 @@ __global__ void __launch_bounds__(kStripeThreads) norm_bwd_stripe_kernel(const _
             a_b[i] += d[i];
             d[i] = (fmaf(d[i], ga[i], -c0) - xh * c1) * rstd;
         }
-        if (P.dX) store(static_cast<TO *>(P.dX) + r * P.lddx + col, d);
+        if (P.dX) {
+            if (P.add) {
+                Vec<TO, V> w;
+                float e[V];
+                w.load(static_cast<const TO *>(P.add) + r * P.lddx + col);
+                w.get(e);
+#pragma unroll
+                for (int i = 0; i < V; ++i) d[i] += e[i];
+            }
+            store(static_cast<TO *>(P.dX) + r * P.lddx + col, d);
+        }
     }
     if (P.part) {
         float *out = P.part + (long long)part * 2 * P.C + col;
@@ -1070,13 +1104,14 @@ extern "C" size_t twn_layer_norm_bwd_workspace_bytes(int64_t M, int64_t C)
 
 extern "C" int twn_layer_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy, const void *X, int32_t x_dtype, int64_t ldx,
                                   int64_t M, int64_t C, const float *gamma, const float *mean, const float *rstd, void *dX,
-                                  int32_t dx_dtype, int64_t lddx, float *dgamma, float *dbeta, void *workspace,
-                                  size_t workspace_bytes, twn_stream_t stream)
+                                  int32_t dx_dtype, int64_t lddx, const void *residual, float *dgamma, float *dbeta,
+                                  void *workspace, size_t workspace_bytes, twn_stream_t stream)
 {
     TWN_REQUIRE(M >= 0 && C >= 1 && C <= kMaxC, TWN_ERR_INVALID_ARG);
     int rc = check_matrix(dY, dy_dtype, lddy, M, C);
     if (rc == TWN_OK) rc = check_matrix(X, x_dtype, ldx, M, C);
     if (rc == TWN_OK && dX) rc = check_matrix(dX, dx_dtype, lddx, M, C);
+    if (rc == TWN_OK && residual) rc = dX ? check_matrix(residual, dx_dtype, lddx, M, C) : TWN_ERR_INVALID_ARG;
     if (rc != TWN_OK) return rc;
     TWN_REQUIRE(M == 0 || (mean != nullptr && rstd != nullptr), TWN_ERR_INVALID_ARG);
     for (const void *p : {(const void *)gamma, (const void *)mean, (const void *)rstd, (const void *)dgamma, (const void *)dbeta})
@@ -1090,13 +1125,13 @@ extern "C" int twn_layer_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy
     rc = twn_current_device(&dev);
     if (rc != TWN_OK) return rc;
     BwdParams P = {};
-    P.dY = dY; P.X = X; P.dX = dX;
+    P.dY = dY; P.X = X; P.dX = dX; P.add = residual;
     P.gamma = gamma; P.mean = mean; P.rstd = rstd;
     P.part = sums ? static_cast<float *>(workspace) : nullptr;
     P.row_sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(C));
     P.lddy = lddy; P.ldx = ldx; P.lddx = lddx; P.M = M; P.C = C;
     const int V = dy_dtype == TWN_F32 && x_dtype == TWN_F32 ? 4 : 8;
-    const bool vec = vector_rows(dY, dy_dtype, lddy, V) && vector_rows(X, x_dtype, ldx, V) && (!dX || vector_rows(dX, dx_dtype, lddx, V)) &&
+    const bool vec = vector_rows(dY, dy_dtype, lddy, V) && vector_rows(X, x_dtype, ldx, V) && (!dX || vector_rows(dX, dx_dtype, lddx, V)) && (!residual || vector_rows(residual, dx_dtype, lddx, V)) &&
                      C % V == 0 && twn_aligned(gamma, 16);
     cudaStream_t s = twn_cu(stream);
     const int key = (dy_dtype == TWN_BF16) * 4 + (x_dtype == TWN_BF16) * 2 + (dX && dx_dtype == TWN_BF16);

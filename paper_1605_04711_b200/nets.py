@@ -126,6 +126,7 @@ class Layer(_Counted):
 class TernaryNet(_Counted):
     """A chain of ternary conv / FC layers with pooling glue, all buffers preallocated.  A buffer or parameter may be
     replaced between two passes (act, aux, grad, a layer's extra, ...); the next pass uses the new one."""
+    norm_eps = 1e-5
     # what a pass itself assigns, and what its list of calls does not hold
     _uncounted = frozenset(["_changes", "_made", "_built", "_fwd", "_bwd", "_delta_ready", "_pending_join", "_dz_ready", "last_grads", "timed",
                             "side_streams", "dw_stream"])
@@ -134,7 +135,12 @@ class TernaryNet(_Counted):
                  train: bool = False, optimizer: dict | None = None):
         """optimizer: None (the step ends with the weight gradients) or dict(lr, momentum, weight_decay):
         the step then ends with the SGD update of the master weights (Algorithm 1, UpdateParameters), which
-        also leaves the next iteration's thresholds behind, so that later steps run only the coding sweep."""
+        also leaves the next iteration's thresholds behind, so that later steps run only the coding sweep.
+        With rule="muon" in it (and, if wanted, look_ahead, steps and eps) the update is that of twn_muon_update_batch,
+        every layer's filters as the rows of a matrix.
+
+        An operation ("layernorm", name, src) normalises every pixel of src over its channels.  Its gamma and beta, and
+        after a backward pass their gradients, are norm[name + ".gamma"], ".beta", ".dgamma" and ".dbeta"."""
         self._changes = _Changes()
         self.name, self.B, self.in_shape, self.ops = name, batch, in_shape, ops
         self.seed, self.delta_factor, self.train = seed, delta_factor, train
@@ -147,6 +153,7 @@ class TernaryNet(_Counted):
         self.act: dict[str, torch.Tensor] = {}
         self.aux: dict[str, torch.Tensor] = {}
         self.grad: dict[str, torch.Tensor] = {}
+        self.norm: dict[str, torch.Tensor] = {}
         self._made: dict[str, object] = {}       # epilogues and views as this class made them, by layer or activation
         self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
         # the code re-layouts for the backward pass run on a side stream beside the forward pass
@@ -232,9 +239,25 @@ class TernaryNet(_Counted):
                 _, name, src = op
                 Bx, H, W, C = self.act[src].shape
                 self.act[name] = torch.zeros((Bx, 1, 1, C), dtype=torch.bfloat16, device="cuda")
+            elif kind == "layernorm":
+                _, name, src = op
+                x = self.act[src]
+                C, M = x.shape[-1], x.numel() // x.shape[-1]
+                self.act[name] = torch.zeros_like(x, dtype=torch.bfloat16)
+                new = {"gamma": torch.ones(C, device="cuda"), "beta": torch.zeros(C, device="cuda")}
+                if self.train:
+                    new |= {k: torch.zeros(M, device="cuda") for k in ("mean", "rstd")}
+                    new |= {k: torch.zeros(C, device="cuda") for k in ("dgamma", "dbeta")}
+                    new["ws"] = torch.empty(twn.layer_norm_bwd_workspace_bytes(M, C), dtype=torch.uint8, device="cuda")
+                self.norm.update({f"{name}.{k}": t for k, t in new.items()})
             elif kind == "flatten":
                 _, name, src = op
                 self._make_view(name, src)
+        self.ws_muon = None
+        if self.optimizer and self._rule() == "muon":
+            layers = list(self.layers.values())
+            most = max(twn.muon_workspace_bytes([(L.Cout, L.K) for L in layers[i:i + 32]]) for i in range(0, len(layers), 32))
+            self.ws_muon = torch.empty(most, dtype=torch.uint8, device="cuda")
         self.ws_tern = torch.empty(twn.ternarize_batch_workspace_bytes(min(len(self.layers), 32)),
                                    dtype=torch.uint8, device="cuda")
         if self.train:
@@ -243,6 +266,12 @@ class TernaryNet(_Counted):
                     self.grad[name] = torch.zeros_like(a)
             self.ws_dw = torch.empty(max(ws_dw, 16), dtype=torch.uint8, device="cuda")
         self._built = self._changes.n
+
+    def _rule(self):
+        rule = self.optimizer.get("rule", "sgd")
+        if rule not in ("sgd", "muon"):
+            raise ValueError(f"no update rule {rule!r}")
+        return rule
 
     def _make_epilogue(self, L):
         """The layer's epilogue, which holds the addresses of its affine and its residual; after the first time, the one
@@ -367,6 +396,12 @@ class TernaryNet(_Counted):
                 x = self.act[src]
                 Bx, H, W, C = x.shape
                 calls.append((None, "", 0, "avgpool_fwd", (x, Bx, H * W, C, self.act[name])))
+            elif kind == "layernorm":
+                _, name, src = op
+                x, p = self.act[src], lambda k: self.norm.get(f"{name}.{k}")
+                C = x.shape[-1]
+                calls.append((None, "", 0, "layer_norm_fwd", (x, C, x.numel() // C, C, p("gamma"), p("beta"), self.norm_eps, self.act[name], C,
+                                                              p("mean"), p("rstd"))))
         return calls, depends
 
     def _from_image(self, L, pool, depends):
@@ -421,7 +456,7 @@ class TernaryNet(_Counted):
                 consumers.setdefault(op[1].src, []).append(op[1])
                 if op[1].residual:
                     consumers.setdefault(op[1].residual, []).append(None)
-            elif op[0] in ("maxpool", "avgpool", "flatten"):
+            elif op[0] in ("maxpool", "avgpool", "flatten", "layernorm"):
                 consumers.setdefault(op[2], []).append(op[1])
         FUSED = object()
 
@@ -505,6 +540,17 @@ class TernaryNet(_Counted):
                 if src != "input":
                     emit_tensor(src, self.grad[src])
                     steps.append(("call", "avgpool_bwd", (acc[name], Bx, H * W, C, self.grad[src])))
+            elif kind == "layernorm":
+                _, name, src = op
+                x, p = self.act[src], lambda k: self.norm[f"{name}.{k}"]
+                C, M = x.shape[-1], x.numel() // x.shape[-1]
+                # the shortcut around a block that begins with the norm has left its part of the gradient
+                shortcut = acc.get(src)
+                out = None
+                if src != "input":
+                    out = acc[src] = self.grad[src]
+                steps.append(("call", "layer_norm_bwd", (acc[name], C, x, C, M, C, p("gamma"), p("mean"), p("rstd"), out, C, p("dgamma"), p("dbeta"),
+                                                         p("ws"), shortcut)))
             elif kind == "flatten":
                 _, name, src = op
                 emit_tensor(src, acc[name].view(self.act[src].shape))
@@ -566,13 +612,23 @@ class TernaryNet(_Counted):
             twn.sgd_update_batch(items, o["lr"], o["momentum"], o["weight_decay"], self.delta_factor, self.ws_tern)
         self._delta_ready = True
 
+    def muon_step(self):
+        """The same with orthogonalised momentum (twn_muon_update_batch)."""
+        o = self.optimizer
+        layers = list(self.layers.values())
+        for i in range(0, len(layers), 32):
+            items = [(L.extra["W"], L.extra["dW"], L.extra["V"], L.Cout, L.K, L.extra["stats"]) for L in layers[i:i + 32]]
+            twn.muon_update_batch(items, o["lr"], o["momentum"], o["weight_decay"], o.get("look_ahead", True), o.get("steps", 5),
+                                  o.get("eps", 1e-7), self.delta_factor, self.ws_muon, self.status)
+        self._delta_ready = True
+
     def train_step(self, dlogits):
         self.ternarize_all(join=False)
         self.forward()
         self.backward(dlogits)
         self.join_side_streams()
         if self.optimizer:
-            self.sgd_step()
+            self.muon_step() if self._rule() == "muon" else self.sgd_step()
 
     def check_status(self):
         s = twn.read_status(self.status)

@@ -450,9 +450,10 @@ def layer_norm_bwd_workspace_bytes(M: int, Cc: int) -> int:
     return int(lib().twn_layer_norm_bwd_workspace_bytes(C.c_int64(M), C.c_int64(Cc)))
 
 
-def layer_norm_bwd(dY, lddy, X, ldx, M, Cc, gamma, mean, rstd, dX, lddx, dgamma, dbeta, workspace, stream=None) -> None:
-    """twn_layer_norm_bwd.  dY, X and dX are fp32 or bf16, the type that each tensor has; dX, dgamma and dbeta may be None."""
-    _check(_C.layer_norm_bwd(dY, lddy, X, ldx, M, Cc, gamma, mean, rstd, dX, lddx, dgamma, dbeta, workspace, stream),
+def layer_norm_bwd(dY, lddy, X, ldx, M, Cc, gamma, mean, rstd, dX, lddx, dgamma, dbeta, workspace, residual=None, stream=None) -> None:
+    """twn_layer_norm_bwd.  dY, X and dX are fp32 or bf16, the type that each tensor has; dX, dgamma and dbeta may be None.
+    residual has the type and the pitch of dX and is added to it."""
+    _check(_C.layer_norm_bwd(dY, lddy, X, ldx, M, Cc, gamma, mean, rstd, dX, lddx, residual, dgamma, dbeta, workspace, stream),
            "twn_layer_norm_bwd")
 
 

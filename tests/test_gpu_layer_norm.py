@@ -153,7 +153,7 @@ def _bwd_reference(dy, x, gamma, mean, rstd):
     return xh, g, (g - c0 - xh * c1) * rstd.double()[:, None], (dy * xh).sum(0), dy.sum(0)
 
 
-def _check_bwd(M, C, dt, xt, ot, lddy, ldx, lddx, gamma=True, offset=0, seed=11, sums=True, data=True, in_place=None):
+def _check_bwd(M, C, dt, xt, ot, lddy, ldx, lddx, gamma=True, offset=0, seed=11, sums=True, data=True, in_place=None, residual=None):
     x, xbuf = _rows(seed, M, C, ldx, xt, offset)
     dy, dbuf = _rows(seed + 5, M, C, lddy, dt, offset)
     ga = 1 + 0.3 * _normal(seed + 2, C) if gamma else None
@@ -162,18 +162,23 @@ def _check_bwd(M, C, dt, xt, ot, lddy, ldx, lddx, gamma=True, offset=0, seed=11,
     xh, g, rdx, rdg, rdb = _bwd_reference(dy, x, ga, mean, rstd)
     ady = dy.double().abs()
     obuf = {"dY": dbuf, "X": xbuf, None: torch.full((offset + M * lddx,), 5.0, dtype=ot, device="cuda")[offset:]}[in_place]
+    rbuf = None
+    if residual:                             # "apart", or "in place": dX itself
+        rbuf = obuf if residual == "in place" else torch.empty_like(obuf)
+        rbuf.copy_(_normal(seed + 9, 1, rbuf.numel()).flatten())
+        rdx = rdx + rbuf.view(M, lddx)[:, :C].double()
     keep = obuf.view(M, lddx)[:, C:].clone()
     dg, db = (torch.full((C,), 9.0, device="cuda") for _ in range(2))
     ws = workspace(twn.layer_norm_bwd_workspace_bytes(M, C))
     ws.fill_(255)                            # NaNs: nothing of it may be read before it is written
-    twn.layer_norm_bwd(dbuf, lddy, xbuf, ldx, M, C, ga, mean, rstd, obuf if data else None, lddx, dg if sums else None, db if sums else None, ws)
+    twn.layer_norm_bwd(dbuf, lddy, xbuf, ldx, M, C, ga, mean, rstd, obuf if data else None, lddx, dg if sums else None, db if sums else None, ws, rbuf)
     k = _depth(C)
     # xh: two roundings of a difference (u of |x|, |mean| counted in it) and a product
     e_xh = 2 * U * xh.abs() + U * (x.double().abs() + m.abs()) * r
     if data:
         size = g.abs() + g.abs().mean(1, keepdim=True) + xh.abs() * (g * xh).abs().mean(1, keepdim=True)
         spread = e_xh * (g * xh).abs().mean(1, keepdim=True) + xh.abs() * (g.abs() * e_xh).mean(1, keepdim=True)
-        e = r * (k * U * size + 2 * spread)
+        e = r * (k * U * size + 2 * spread) + U * rdx.abs()
         dx = obuf.view(M, lddx)
         assert bool(((dx[:, :C].double() - rdx).abs() <= e + HALF[ot] * (rdx.abs() + e)).all())
         assert torch.equal(dx[:, C:], keep)
@@ -194,6 +199,13 @@ def test_backward(M, C, dt, xt, ot):
 @pytest.mark.parametrize("dt,xt,ot", [(F, F, F), (B, B, B), (B, F, B), (F, B, F)])
 def test_backward_large(M, C, dt, xt, ot):
     _check_bwd(M, C, dt, xt, ot, C, C + 8, C + 24, gamma=C % 3 > 0)
+
+
+@pytest.mark.parametrize("M,C", [(3, 20), (50, 1000), (41, 1001), (300, 4096), (70, 16384), (9000, 1001), (20, 20000), (30, 9001)])
+@pytest.mark.parametrize("residual", ["apart", "in place"])
+@pytest.mark.parametrize("dt,xt,ot", [(F, F, F), (B, B, B), (B, F, F), (F, F, B)])
+def test_backward_with_a_residual(M, C, residual, dt, xt, ot):
+    _check_bwd(M, C, dt, xt, ot, C, C, C + 8, residual=residual)
 
 
 @pytest.mark.parametrize("lddy,ldx,lddx,offset", [(1008, 1024, 1000, 0), (1001, 1000, 1000, 0), (1000, 1000, 1003, 0), (1000, 1000, 1000, 1)])

@@ -27,13 +27,13 @@ def fwd(lib, X=FAKE, xt=F32, ldx=64, M=4, Cc=64, gamma=FAKE, beta=FAKE, eps=1e-5
                                   _ptr(mean), _ptr(rstd), None)
 
 
-def bwd(lib, dY=FAKE, dt=F32, lddy=64, X=FAKE, xt=F32, ldx=64, M=4, Cc=64, gamma=FAKE, mean=FAKE, rstd=FAKE, dX=FAKE, ot=F32, lddx=64,
+def bwd(lib, dY=FAKE, dt=F32, lddy=64, X=FAKE, xt=F32, ldx=64, M=4, Cc=64, gamma=FAKE, mean=FAKE, rstd=FAKE, dX=FAKE, ot=F32, lddx=64, residual=0,
         dgamma=FAKE, dbeta=FAKE, ws=FAKE, bytes_=None):
     i = C.c_int64
     if bytes_ is None:
         bytes_ = lib.twn_layer_norm_bwd_workspace_bytes(i(4), i(64))
     return lib.twn_layer_norm_bwd(_ptr(dY), dt, i(lddy), _ptr(X), xt, i(ldx), i(M), i(Cc), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dX), ot,
-                                  i(lddx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), C.c_size_t(bytes_), None)
+                                  i(lddx), _ptr(residual), _ptr(dgamma), _ptr(dbeta), _ptr(ws), C.c_size_t(bytes_), None)
 
 
 @pytest.mark.parametrize("args,code", [
@@ -51,7 +51,7 @@ def test_forward(lib, args, code):
     ({"X": 0}, INVALID), ({"mean": 0}, INVALID), ({"rstd": 0}, INVALID), ({"dt": 2}, INVALID), ({"xt": 3}, INVALID), ({"ot": 5}, INVALID),
     ({"dY": ODD}, MISALIGNED), ({"dX": ODD}, MISALIGNED), ({"dgamma": ODD}, MISALIGNED), ({"ws": 0}, WORKSPACE), ({"bytes_": 16}, WORKSPACE),
     ({"ws": FAKE + 16}, MISALIGNED), ({"lddx": 1 << 60}, TOO_LARGE), ({"dX": 0, "dgamma": 0, "dbeta": 0, "ws": 0}, 0),
-    ({"M": 0, "dgamma": 0, "dbeta": 0}, 0)])
+    ({"M": 0, "dgamma": 0, "dbeta": 0}, 0), ({"residual": ODD}, MISALIGNED), ({"residual": FAKE, "dX": 0}, INVALID)])
 def test_backward(lib, args, code):
     assert bwd(lib, **args) == code
 
