@@ -1028,8 +1028,11 @@ Shape shape_of(int64_t rows, int64_t cols)
     s.fits = s.m <= kMaxShort && s.n <= kMaxLong;
     if (!s.fits || s.m == 0) return s;
     const int64_t m256 = (s.m + 255) / 256, n256 = (s.n + 255) / 256, m128 = (s.m + 127) / 128;
-    s.sym_pair = m256 > 8;
-    s.apply_pair = m256 * n256 >= 32;
+    // Pairs need tiles for most of the 74 of them.  Triangles: 36 tiles (2048 rows) 344 us with pairs, 239 without, 55 (2560 rows) 450 and 439,
+    // 136 (4096 rows) two rounds of pairs for 3.6 of single blocks.  B X: 36 tiles (512 x 4608) 167 and 145, 64 (4096 x 1024) 200 and 189,
+    // 81 (2300 x 2300) 438 and 462, 96 (3000 x 2000) 311 and 343.
+    s.sym_pair = m256 > 10;
+    s.apply_pair = m256 * n256 > 64;
     const bool wide = s.sym_pair || s.apply_pair;
     s.rb = wide ? 4 * m256 : 2 * m128;
     s.cb = wide ? 4 * n256 : (s.n + 127) / 128 * 2;

@@ -17,7 +17,7 @@ pytestmark = pytest.mark.gpu
 NS = (3.4445, -4.7750, 2.0315)
 F, B = torch.float32, torch.bfloat16
 SHAPES = [(1, 1), (1, 7), (7, 1), (2, 3), (63, 65), (64, 64), (65, 63), (64, 576), (128, 128), (129, 300), (300, 129), (255, 257), (256, 1000),
-          (1000, 512), (513, 511), (640, 640), (1024, 2048), (2047, 1111), (1, 5000), (130, 10000), (768, 6912), (1500, 2700), (2560, 2304), (2309, 2701)]
+          (1000, 512), (513, 511), (640, 640), (1024, 2048), (2047, 1111), (1, 5000), (130, 10000), (768, 6912), (1500, 2700), (2560, 2304), (2309, 2701), (2817, 2900), (3100, 2820)]
 
 
 def _normal(seed, rows, cols):
