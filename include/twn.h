@@ -263,6 +263,7 @@ int twn_ternarize_codes_batch(const twn_ternarize_item_t *items, int count, void
  *   items      HOST array of up to 32 matrices, read during the call only; their tiles share the launches.
  *     G        TWN_F32 or TWN_BF16 [rows, cols], contiguous;  O likewise, its own type; both aligned to their element.
  *              O may be G (same type).  An empty matrix is skipped.  min(rows, cols) <= 32768, max <= 2^24.
+ *              The matrices are worked on at the same time: an O that overlaps anything else is refused (TWN_ERR_INVALID_ARG).
  *   steps      1 .. 32;  eps  1e-30 .. 1e30 (1e-7 is usual).
  *   workspace  at least twn_orthogonalize_workspace_bytes(items, count) bytes (only rows and cols are read; 0 for shapes that
  *              the call refuses), 256-byte aligned; contents need not be preserved or initialised.  Two calls that overlap on
@@ -293,7 +294,7 @@ int twn_orthogonalize_batch(const twn_orthogonalize_item_t *items, int count, in
  *   V = momentum * V + dW;   U = dW + momentum * V (look_ahead = 1) or V (0);   O = the orthogonalised U, as above;
  *   W = W - lr * (s * O + weight_decay * W),   s = sqrt(max(1, rows / cols))
  * V and U are separately rounded fp32 operations, defined to the bit, and so is W as a function of O (which is fp32).
- *   W, dW, V   fp32 [rows, cols], 16-byte aligned;  stats_next as in twn_sgd_update (optional): sum_abs, delta and status
+ *   W, dW, V   fp32 [rows, cols], 16-byte aligned, each W and V apart from all others (else TWN_ERR_INVALID_ARG);  stats_next as in twn_sgd_update (optional): sum_abs, delta and status
  *              of the updated weights, for twn_ternarize_codes.
  *   look_ahead 0 or 1; steps, eps, dev_status as above; workspace at least twn_muon_workspace_bytes(items, count).
  */

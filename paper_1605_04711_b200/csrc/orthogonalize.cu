@@ -1191,10 +1191,35 @@ int run_small(const NsParams &P, int steps, cudaStream_t s)
     return twn_detail::ns_small(S, s);
 }
 
+// What a call writes lies apart from all else that it reads or writes: the matrices of a call are worked on at the same time.
+struct Extent {
+    const char *begin, *end;
+    bool written;
+};
+struct Extents {
+    Extent e[3 * kMaxItems];
+    int n = 0;
+    void add(const void *p, size_t bytes, bool written) { e[n++] = {static_cast<const char *>(p), static_cast<const char *>(p) + bytes, written}; }
+    bool apart()
+    {
+        std::sort(e, e + n, [](const Extent &a, const Extent &b) { return a.begin < b.begin; });
+        const char *any = nullptr, *written = nullptr;       // ends of what begins before
+        for (int i = 0; i < n; ++i) {
+            if (e[i].begin < (e[i].written ? any : written)) return false;
+            any = std::max(any, e[i].end);
+            if (e[i].written) written = std::max(written, e[i].end);
+        }
+        return true;
+    }
+};
+
 // The items of P are placed from `base` on, within `bytes`.
-int run_steps(NsParams &P, int steps, char *base, size_t bytes, cudaStream_t s)
+int run_steps(NsParams &P, int steps, char *base, size_t bytes, Extents &extents, cudaStream_t s)
 {
-    if (all_small(P, steps)) return run_small(P, steps, s);
+    if (all_small(P, steps)) {
+        TWN_REQUIRE(extents.apart(), TWN_ERR_INVALID_ARG);
+        return run_small(P, steps, s);
+    }
     P.base = reinterpret_cast<const uint16_t *>(base);
     enum { kNorm, kStartList, kSymPair, kGramTile, kSquareTile, kApplyPair, kApplyTile, kLists };
     NsParams list[kLists];
@@ -1212,6 +1237,7 @@ int run_steps(NsParams &P, int steps, char *base, size_t bytes, cudaStream_t s)
         select(P, list[kApplyPair], [](const NsItem &it) { return it.apply_pair != 0; }, one, [](const NsItem &it) { return (int64_t)(it.rb / 4) * (it.cb / 4); }) &&
         select(P, list[kApplyTile], [](const NsItem &it) { return it.apply_pair == 0; }, one, [](const NsItem &it) { return (int64_t)(it.rb / 2) * (it.cb / 2); });
     TWN_REQUIRE(fits && bytes / 128 < (1ull << 31), TWN_ERR_TOO_LARGE);
+    TWN_REQUIRE(extents.apart(), TWN_ERR_INVALID_ARG);
     twn_device_info dev;
     int rc = twn_current_device(&dev);
     if (rc != TWN_OK) return rc;
@@ -1268,6 +1294,7 @@ extern "C" int twn_orthogonalize_batch(const twn_orthogonalize_item_t *items, in
     if (count == 0) return TWN_OK;
     TWN_REQUIRE(items != nullptr && workspace != nullptr, TWN_ERR_INVALID_ARG);
     NsParams P = {};
+    Extents extents;
     char *p = static_cast<char *>(workspace);
     for (int t = 0; t < count; ++t) {
         const twn_orthogonalize_item_t &in = items[t];
@@ -1285,6 +1312,9 @@ extern "C" int twn_orthogonalize_batch(const twn_orthogonalize_item_t *items, in
         it.vec_in = twn_aligned(in.G, 16);
         it.vec_out = twn_aligned(in.O, 16) && in.cols % 8 == 0;      // rows of O on 16-byte boundaries, in runs of eight
         it.out_scale = 1.0f;
+        // in place, or else apart
+        if (in.G != in.O || it.g_bf16 != it.o_bf16) extents.add(in.G, it.count * (it.g_bf16 ? 2 : 4), false);
+        extents.add(in.O, it.count * (it.o_bf16 ? 2 : 4), true);
     }
     const size_t need = twn_orthogonalize_workspace_bytes(items, count);
     TWN_REQUIRE(workspace_bytes >= need, TWN_ERR_WORKSPACE);
@@ -1292,7 +1322,7 @@ extern "C" int twn_orthogonalize_batch(const twn_orthogonalize_item_t *items, in
     if (P.count == 0) return TWN_OK;
     P.eps = (float)eps;
     P.status = dev_status;
-    return run_steps(P, steps, static_cast<char *>(workspace), need, twn_cu(stream));
+    return run_steps(P, steps, static_cast<char *>(workspace), need, extents, twn_cu(stream));
 }
 
 extern "C" size_t twn_muon_workspace_bytes(const twn_muon_item_t *items, int count)
@@ -1312,6 +1342,7 @@ extern "C" int twn_muon_update_batch(const twn_muon_item_t *items, int count, fl
     if (count == 0) return TWN_OK;
     TWN_REQUIRE(items != nullptr && workspace != nullptr, TWN_ERR_INVALID_ARG);
     NsParams P = {};
+    Extents extents;
     twn_sgd_item_t apply[kMaxItems];
     char *p = static_cast<char *>(workspace);
     void *const sweep_ws = p;
@@ -1329,6 +1360,9 @@ extern "C" int twn_muon_update_batch(const twn_muon_item_t *items, int count, fl
         const Shape s = shape_of(in.rows, in.cols);
         p = place(it, s, p);
         it.dW = in.dW; it.V = in.V; it.O = p;
+        extents.add(in.W, it.count * sizeof(float), true);
+        extents.add(in.dW, it.count * sizeof(float), false);
+        extents.add(in.V, it.count * sizeof(float), true);
         p += align256((size_t)(s.m * s.n) * sizeof(float));
         it.tall = in.rows > in.cols;
         it.vec_in = 1;
@@ -1347,7 +1381,7 @@ extern "C" int twn_muon_update_batch(const twn_muon_item_t *items, int count, fl
     P.look_ahead = look_ahead;
     P.status = dev_status;
     if (P.count > 0) {
-        const int rc = run_steps(P, steps, static_cast<char *>(workspace), need, twn_cu(stream));
+        const int rc = run_steps(P, steps, static_cast<char *>(workspace), need, extents, twn_cu(stream));
         if (rc != TWN_OK) return rc;
     }
     return twn_sgd_update_batch(apply, count, lr, 0.0f, weight_decay, delta_factor, sweep_ws, sweep_bytes, stream);

@@ -54,6 +54,51 @@ def test_muon(lib, args, code):
     assert muon(lib, **args) == code
 
 
+@pytest.mark.parametrize("big", [0, 100])
+def test_matrices_that_overlap_are_refused(lib, big):
+    """An output over another matrix's input or output, over a part of its own input, or over it in another type."""
+    def call(*items):
+        its = (twn._OrthogonalizeItem * len(items))(*[twn._OrthogonalizeItem(g, o, 8 + 50 * big, 8 + big, gt, ot) for g, o, gt, ot in items])
+        size = lib.twn_orthogonalize_workspace_bytes(its, len(items))
+        return lib.twn_orthogonalize_batch(its, len(items), 5, C.c_double(1e-7), C.c_void_p(FAKE), C.c_size_t(size), None, None)
+
+    n = (8 + 50 * big) * (8 + big) * 4
+    x = [(1 << 30) + i * n for i in range(4)]
+    refused = [[(x[0], x[1], 0, 0), (x[1], x[2], 0, 0)], [(x[1], x[2], 0, 0), (x[0], x[1], 0, 0)], [(x[0], x[2], 0, 0), (x[1], x[2], 0, 0)],
+               [(x[0], x[0], 0, 0)] * 2, [(x[0], x[0] + 4, 0, 0)], [(x[0] + n - 4, x[0], 0, 0)], [(x[0], x[0], 0, 1)], [(x[0], x[0], 1, 0)]]
+    for items in refused:
+        assert call(*items) == INVALID
+    # one input for two outputs, in place, side by side: what stops these is that there is no device
+    for items in [[(x[0], x[1], 0, 0), (x[0], x[2], 0, 0)], [(x[0], x[0], 0, 0), (x[1], x[1], 1, 1)], [(x[1], x[0], 0, 0), (x[1], x[2], 0, 0)]]:
+        assert _no_device() and call(*items) not in (INVALID, MISALIGNED, WORKSPACE, TOO_LARGE)
+
+
+def _no_device():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are made up")
+    return True
+
+
+def test_muon_matrices_that_overlap_are_refused(lib):
+    n = 64 * 64 * 4
+    x = [(1 << 30) + i * n for i in range(8)]
+
+    def call(*items):
+        its = (twn._MuonItem * len(items))(*[twn._MuonItem(w, d, v, 64, 64, 0) for w, d, v in items])
+        size = lib.twn_muon_workspace_bytes(its, len(items))
+        f = C.c_float
+        return lib.twn_muon_update_batch(its, len(items), f(0.1), f(0.9), f(0.0), 1, 5, C.c_double(1e-7), C.c_double(0.7), C.c_void_p(FAKE),
+                                         C.c_size_t(size), None, None)
+
+    for items in [[(x[0], x[0], x[1])], [(x[0], x[1], x[0])], [(x[0], x[1], x[1])], [(x[0], x[1], x[2])] * 2, [(x[0], x[1], x[2]), (x[3], x[4], x[2])],
+                  [(x[0], x[1], x[2]), (x[1], x[4], x[5])], [(x[0], x[1], x[2]), (x[3], x[0] + n - 16, x[5])]]:
+        assert call(*items) == INVALID
+    for items in [[(x[0], x[1], x[2]), (x[3], x[1], x[4])], [(x[0], x[1], x[2]), (x[3], x[4], x[5])]]:
+        assert _no_device() and call(*items) not in (INVALID, MISALIGNED, WORKSPACE, TOO_LARGE)
+
+
+
 def test_workspace():
     one, two = twn.orthogonalize_workspace_bytes([(64, 576)]), twn.orthogonalize_workspace_bytes([(64, 576), (576, 64)])
     assert 0 < one < two and one % 256 == 0
