@@ -544,10 +544,10 @@ class TernaryNet(_Counted):
                 _, name, src = op
                 x, p = self.act[src], lambda k: self.norm[f"{name}.{k}"]
                 C, M = x.shape[-1], x.numel() // x.shape[-1]
-                # the shortcut around a block that begins with the norm has left its part of the gradient
-                shortcut = acc.get(src)
-                out = None
+                out = shortcut = None
                 if src != "input":
+                    # the shortcut around a block that begins with the norm has left its part of the gradient
+                    shortcut = acc.get(src)
                     out = acc[src] = self.grad[src]
                 steps.append(("call", "layer_norm_bwd", (acc[name], C, x, C, M, C, p("gamma"), p("mean"), p("rstd"), out, C, p("dgamma"), p("dbeta"),
                                                          p("ws"), shortcut)))

@@ -89,6 +89,28 @@ def test_a_step_is_that_of_64_bits():
             _near(net.norm[f"{name}.d{k}"], dn[f"{name}.{k}"], 22 * 2.0 ** -8)
 
 
+def test_a_block_around_the_input():
+    """The shortcut of the first block leaves a gradient at the input, which nobody asks for."""
+    H = W = 4
+    ops = [("layernorm", "n0", "input"), ("layer", nets.Layer("up", 64, 128, H=H, W=W, src="n0")),
+           ("layer", nets.Layer("down", 128, 64, H=H, W=W, relu=False, residual="input", src="up")),
+           ("layernorm", "last", "down"), ("avgpool", "gap", "last"), ("layer", nets.Layer("fc", 64, 16, relu=False, src="gap", out_f32=True))]
+    net = nets.TernaryNet("first", 24, (H, W, 64), ops, seed=3, train=True)
+    net.set_input(dg.draw_bf16(7, "x", 24 * H * W * 64, "normal"))
+    dlogits = torch.from_numpy(dg.draw(9, "dl", 24 * 16, "normal")).cuda().view(24, 16).to(torch.bfloat16)
+    net.train_step(dlogits)
+    torch.cuda.synchronize()
+    net.check_status()
+    y, dT, dn = _reference(net, net.act["input"], _weights(net), net.norm, dlogits)
+    # fewer roundings on the way than in the step above
+    _near(net.act["fc"], y, 10 * 2.0 ** -8)
+    for name, L in net.layers.items():
+        _near(L.extra["dW"], dT[name], 22 * 2.0 ** -8)
+    for name in ("n0", "last"):
+        for k in ("gamma", "beta"):
+            _near(net.norm[f"{name}.d{k}"], dn[f"{name}.{k}"], 22 * 2.0 ** -8)
+
+
 def test_steps_with_muon_update_every_weight_as_the_call_alone_does():
     net = _net()
     dlogits = torch.from_numpy(dg.draw(9, "dl", 24 * 16, "normal")).cuda().view(24, 16).to(torch.bfloat16)
