@@ -172,6 +172,53 @@ template <int N> __device__ __forceinline__ void team_sum(float (&v)[N], int T, 
     }
 }
 
+// The same for a team whose size is known at compile time.  Two sums share their shuffles: of a pair of lanes each goes on with one.
+template <int TT, int N> __device__ __forceinline__ void team_sum(float (&v)[N], float (*red)[32][2], unsigned int &turn, int barrier)
+{
+    constexpr int kSpan = TT < 32 ? TT : 32, kWarps = TT / 32;
+    const int lane = threadIdx.x & 31;
+    float own = v[0];
+    if (N == 2) {
+        const bool odd = lane & 1;
+        own = (odd ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, odd ? v[0] : v[1], 1);
+    }
+#pragma unroll
+    for (int o = N; o < kSpan; o <<= 1) own += __shfl_xor_sync(0xffffffffu, own, o);
+    if (TT <= 32) {
+        if (N == 1) {
+            v[0] = own;
+        } else {
+            const float other = __shfl_xor_sync(0xffffffffu, own, 1);
+            v[0] = lane & 1 ? other : own;
+            v[N - 1] = lane & 1 ? own : other;
+        }
+    } else {
+        // a warp's sums, its one or two floats next to the next warp's
+        float *const buf = &red[turn & 1][0][0];
+        ++turn;
+        const int warp = threadIdx.x >> 5, first = warp / (kWarps ? kWarps : 1) * kWarps;
+        if (lane < N) buf[warp * N + lane] = own;
+        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "n"(TT) : "memory");
+        if (N == 2) {
+            two_f32 s = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; w += 2) {
+                const float4 a = *reinterpret_cast<const float4 *>(buf + (first + w) * 2);
+                s = add2(add2(s, two(a.x, a.y)), two(a.z, a.w));
+            }
+            each(s, v[0], v[N - 1]);
+        } else {
+            float s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; w += 2) {
+                const float2 a = *reinterpret_cast<const float2 *>(buf + first + w);
+                s += a.x + a.y;
+            }
+            v[0] = s;
+        }
+    }
+}
+
 // Column of a thread's vector j, and whether the vectors j of the whole team lie inside the row (the same for all threads).  TT: the
 // team's size where it is known at compile time, so that single elements (V = 1) lie at constant offsets of one address; with
 // the offsets worked out for each, a row of 1001 took 85 instructions an element.
@@ -231,7 +278,7 @@ struct FwdParams {
 
 // One row per team, in registers.  C <= T * E.  A team of more than a warp is a block.
 template <typename TX, typename TY, int V, int E, int TT>
-__global__ void __launch_bounds__(TT > 32 ? TT : TT == 32 || E < 16 ? 128 : 1024) norm_fwd_kernel(const __grid_constant__ FwdParams P)
+__global__ void __launch_bounds__(TT > 32 ? TT : TT == 32 || E < 16 ? 128 : 1024, TT <= 32 || V == 1 ? 1 : 1024 / (TT ? TT : 1)) norm_fwd_kernel(const __grid_constant__ FwdParams P)
 {
     constexpr int NV = E / V, P2 = E / 2;
     __shared__ __align__(16) float red[2][32][2];
@@ -259,7 +306,8 @@ __global__ void __launch_bounds__(TT > 32 ? TT : TT == 32 || E < 16 ? 128 : 1024
             }
         }
         float s[1] = {sum2(s2)};
-        team_sum(s, T, red, turn, 0);
+        if constexpr (TT > 0) team_sum<TT>(s, red, turn, 0);
+        else team_sum(s, T, red, turn, 0);
         const float mean = s[0] * inv;
         const two_f32 minus = two(-mean, -mean);
 #pragma unroll
@@ -282,7 +330,8 @@ __global__ void __launch_bounds__(TT > 32 ? TT : TT == 32 || E < 16 ? 128 : 1024
 #pragma unroll
         for (int i = 0; i < P2; ++i) q2 = fma2(d[i], d[i], q2);
         float q[1] = {sum2(q2)};
-        team_sum(q, T, red, turn, 0);
+        if constexpr (TT > 0) team_sum<TT>(q, red, turn, 0);
+        else team_sum(q, T, red, turn, 0);
         const float rstd = rsqrtf(fmaf(q[0], inv, P.eps));
         if (!live) continue;
         const two_f32 scale = two(rstd, rstd);
@@ -361,7 +410,8 @@ template <int V> __device__ __forceinline__ void read_param(const float *sm, con
 
 template <int E> constexpr int fwd_ring_threads() { return E >= 64 ? 512 : E >= 32 ? 768 : 1024; }
 
-template <typename TX, typename TY, int V, int E>
+// TT > 0: teams of TT threads whose elements the row fills, C = TT E, so that addresses are constants and nothing is checked.
+template <typename TX, typename TY, int V, int E, int TT>
 __global__ void __launch_bounds__(fwd_ring_threads<E>(), 1) norm_fwd_ring_kernel(const __grid_constant__ FwdParams P, const __grid_constant__ Ring R)
 {
     constexpr int NV = E / V, P2 = E / 2;
@@ -370,10 +420,10 @@ __global__ void __launch_bounds__(fwd_ring_threads<E>(), 1) norm_fwd_ring_kernel
     __shared__ __align__(16) float red[2][32][2];
     __shared__ volatile int gave_up;
     unsigned int turn = 0;
-    const int T = P.T, team = threadIdx.x / T, t = threadIdx.x - team * T, C = (int)P.C;
+    const int T = TT ? TT : P.T, team = threadIdx.x / T, t = threadIdx.x - team * T, C = TT ? TT * E : (int)P.C;
     const int teams = blockDim.x / T, barrier = teams > 1 ? team + 1 : 0;
     const float inv = 1.0f / (float)C;
-    const Columns<V, 0> col{T, t, C};
+    const Columns<V, TT> col{T, t, C};
     if (t == 0)
         for (int s = 0; s < R.stages; ++s) mbar_init(&full[team][s], 1);
     if (threadIdx.x == 0) gave_up = 0;
@@ -415,7 +465,8 @@ __global__ void __launch_bounds__(fwd_ring_threads<E>(), 1) norm_fwd_ring_kernel
             }
         }
         float sum[1] = {ok ? sum2(s2) : __uint_as_float(0x7FC00000u)};
-        team_sum(sum, T, red, turn, barrier);
+        if constexpr (TT > 0) team_sum<TT>(sum, red, turn, barrier);
+        else team_sum(sum, T, red, turn, barrier);
         // the whole team has its elements: the stage is free
         if (T == 32) __syncwarp();
         if (t == 0) issue(r + R.stages * step, s);
@@ -429,7 +480,8 @@ __global__ void __launch_bounds__(fwd_ring_threads<E>(), 1) norm_fwd_ring_kernel
             q2 = fma2(d[i], d[i], q2);
         }
         float q[1] = {sum2(q2)};
-        team_sum(q, T, red, turn, barrier);
+        if constexpr (TT > 0) team_sum<TT>(q, red, turn, barrier);
+        else team_sum(q, T, red, turn, barrier);
         const float rstd = rsqrtf(fmaf(q[0], inv, P.eps));
         const two_f32 scale = two(rstd, rstd);
         TY *y = static_cast<TY *>(P.Y) + r * P.ldy;
@@ -514,13 +566,59 @@ struct BwdParams {
 
 constexpr int kBwdThreads = 512;
 
-// One row per team, the next row's loads in flight while this one is worked on; sums over the rows of a block stay in the
-// registers of the threads that own the columns, and its teams join them in shared memory at the end.  C <= T * E.
+// The column sums of a block's `parties` (teams, or warps of several teams), of which this thread belongs to number `me`, to `out`, [2][C]; they are added in
+// their order.  cols: [parties][2][C] in shared memory where there are several (with one after the other adding to one [2][C], the sixteen
+// warps of a block took 5 of 29 us for rows of 64).
+template <int V, int E, typename Col>
+__device__ __forceinline__ void join_sums(const float (&g)[E], const float (&b)[E], const Col &col, bool mine, int me, int parties, float *cols, float *out)
+{
+    const int C = col.C;
+    float *const to = parties > 1 ? cols + (size_t)me * 2 * C : out;
+    if (mine)
+#pragma unroll
+        for (int j = 0; j < E / V; ++j) {
+            if (col(j) >= C) continue;
+            float v[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = g[j * V + i];
+            store(to + col(j), v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = b[j * V + i];
+            store(to + C + col(j), v);
+        }
+    if (parties == 1) return;
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * C; c += blockDim.x) {
+        float v = 0.0f;
+#pragma unroll 4
+        for (int k = 0; k < parties; ++k) v += cols[(size_t)k * 2 * C + c];
+        out[c] = v;
+    }
+}
+
+// 16 bytes (or 4) to shared memory on their own way; zeros where `there` is false.
+__device__ __forceinline__ void copy_piece(uint32_t dst, const void *src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_float(uint32_t dst, const float *src, bool there)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
+// Bytes of a thread's part of a row in a stage: dY, X, mean and rstd.
+template <typename TD, typename TX, int E> __host__ __device__ constexpr int bwd_stage_bytes() { return E * (int)(sizeof(TD) + sizeof(TX)) + 8; }
+constexpr int kBwdStages = 5;
+
+// One row per team; sums over the rows of a block stay in the registers of the threads that own the columns, and its teams join them in
+// shared memory at the end.  C <= T * E.  Vectors come through shared memory, every thread's own elements by its own copies, so no
+// barrier guards them: four rows of every team are on their way (one, in registers, was 32 KB an SM and took SHORT us for
+// 200704 x 64 and LONG for 16384 x 4096).  Single elements (V = 1) of the next row are in registers.
 template <typename TD, typename TX, typename TO, int V, int E, int TT>
 __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_constant__ BwdParams P)
 {
     constexpr int NV = E / V, P2 = E / 2;
-    extern __shared__ float cols[];          // [2][C], when a block has several teams (of a warp or more)
+    constexpr bool kRing = V > 1;
+    extern __shared__ __align__(16) uint8_t bwd_smem[];      // the stages; [2][C] sums when a block has several teams (of a warp or more)
     __shared__ __align__(16) float red[2][32][2];
     unsigned int turn = 0;
     const int T = TT ? TT : P.T, t = threadIdx.x & (T - 1), C = (int)P.C;
@@ -557,12 +655,61 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
         load_vectors(nd, d, col, live);
         load_vectors(nx, x, col, live);
     };
+    // a stage: pieces of 16 bytes, piece p of all threads next to each other, then the means, then the 1/deviations
+    constexpr int kPD = V * (int)sizeof(TD) / 16, kPX = V * (int)sizeof(TX) / 16, kPieces = NV * (kPD + kPX);
+    const uint32_t threads = blockDim.x, stage = threads * bwd_stage_bytes<TD, TX, E>();
+    const uint32_t mine = smem_u32(bwd_smem) + 16 * threadIdx.x, floats = smem_u32(bwd_smem) + 16 * kPieces * threads + 4 * threadIdx.x;
+    auto issue = [&](long long r, uint32_t s) {
+        const bool live = r < P.M;
+        const long long row = live ? r : 0;
+        const TD *d = static_cast<const TD *>(P.dY) + row * P.lddy + t * V;
+        const TX *x = static_cast<const TX *>(P.X) + row * P.ldx + t * V;
+        const uint32_t to = mine + s * stage;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const bool there = live && col(j) < C;
+            const int c = there ? j * T * V : 0;             // an address inside the row, whatever is copied
+#pragma unroll
+            for (int p = 0; p < kPD; ++p) copy_piece(to + 16 * threads * (j * kPD + p), (there ? d : static_cast<const TD *>(P.dY)) + c + p * (16 / sizeof(TD)), there);
+#pragma unroll
+            for (int p = 0; p < kPX; ++p)
+                copy_piece(to + 16 * threads * (NV * kPD + j * kPX + p), (there ? x : static_cast<const TX *>(P.X)) + c + p * (16 / sizeof(TX)), there);
+        }
+        copy_float(floats + s * stage, P.mean + row, live);
+        copy_float(floats + s * stage + 4 * threads, P.rstd + row, live);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
     long long r0 = (long long)blockIdx.x * teams;
-    if (r0 < P.M) fetch(r0 + team);
+    uint32_t s_in = kBwdStages - 1, s_out = 0;
+    if constexpr (kRing) {
+        if (r0 < P.M)
+            for (uint32_t k = 0; k < kBwdStages - 1; ++k) issue(r0 + team + k * step, k);
+    } else {
+        if (r0 < P.M) fetch(r0 + team);
+    }
     for (; r0 < P.M; r0 += step) {
         const long long r = r0 + team;
         const bool live = r < P.M;
         two_f32 dy[P2], xh[P2];
+        float mean, rstd;
+        if constexpr (kRing) {
+            issue(r + (kBwdStages - 1) * step, s_in);
+            if (++s_in == kBwdStages) s_in = 0;
+            asm volatile("cp.async.wait_group %0;" ::"n"(kBwdStages - 1) : "memory");
+            const uint8_t *const from = bwd_smem + s_out * stage;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int p = 0; p < kPD; ++p)
+                    reinterpret_cast<uint4 *>(&nd[j])[p] = *reinterpret_cast<const uint4 *>(from + 16 * (threads * (j * kPD + p) + threadIdx.x));
+#pragma unroll
+                for (int p = 0; p < kPX; ++p)
+                    reinterpret_cast<uint4 *>(&nx[j])[p] = *reinterpret_cast<const uint4 *>(from + 16 * (threads * (NV * kPD + j * kPX + p) + threadIdx.x));
+            }
+            mean = *reinterpret_cast<const float *>(from + 16 * kPieces * threads + 4 * threadIdx.x);
+            rstd = *reinterpret_cast<const float *>(from + 16 * kPieces * threads + 4 * (threads + threadIdx.x));
+            if (++s_out == kBwdStages) s_out = 0;
+        }
         {
             float fd[E], fx[E];
 #pragma unroll
@@ -576,8 +723,11 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
                 xh[i] = two(fx[2 * i], fx[2 * i + 1]);
             }
         }
-        const float mean = n_mean, rstd = n_rstd;
-        if (r0 + step < P.M) fetch(r + step);
+        if constexpr (!kRing) {
+            mean = n_mean;
+            rstd = n_rstd;
+            if (r0 + step < P.M) fetch(r + step);
+        }
         // past the row's end dy and gamma are zero
         const two_f32 minus = two(-mean, -mean), scale = two(rstd, rstd);
         two_f32 s0 = 0, s1 = 0;
@@ -592,7 +742,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
         }
         if (P.dX == nullptr) continue;
         float s[2] = {sum2(s0), sum2(s1)};
-        team_sum(s, T, red, turn, barrier);
+        if constexpr (TT > 0) team_sum<TT>(s, red, turn, barrier);
+        else team_sum(s, T, red, turn, barrier);
         if (!live) continue;
         const float c0 = -s[0] * inv, c1 = -s[1] * inv;
         const two_f32 k0 = two(c0, c0), k1 = two(c1, c1);
@@ -605,8 +756,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
             for (int j = 0; j < NV; ++j) add_vector(*reinterpret_cast<float(*)[V]>(f + j * V), static_cast<const TO *>(P.add) + r * P.lddx, col, j);
 #pragma unroll
         for (int j = 0; j < NV; ++j)
-            if (col.whole(j) || col(j) < C) store(o + col(j), *reinterpret_cast<const float(*)[V]>(f + j * V));
+            if (col(j) < C) store(o + col(j), *reinterpret_cast<const float(*)[V]>(f + j * V));
     }
+    if constexpr (kRing) {
+        // the stages take the sums
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+    }
+    float *const cols = reinterpret_cast<float *>(bwd_smem);
     if (P.part == nullptr) return;
     float *out = P.part + (long long)blockIdx.x * 2 * C;
     float g[E], b[E];
@@ -619,26 +776,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
             g[e] += __shfl_xor_sync(0xffffffffu, g[e], o);
             b[e] += __shfl_xor_sync(0xffffffffu, b[e], o);
         }
-    const int span = max(T, 32), turns = blockDim.x / span;
-    for (int k = 0; k < turns; ++k) {
-        if ((int)threadIdx.x / span == k && (int)threadIdx.x % span < T)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int c = col(e / V) + e % V;
-                if (c >= C) continue;
-                if (k > 0) { g[e] += cols[c]; b[e] += cols[C + c]; }
-                float *to = k == turns - 1 ? out : cols;
-                to[c] = g[e];
-                to[C + c] = b[e];
-            }
-        if (turns > 1) __syncthreads();
-    }
+    const int span = max(T, 32);
+    join_sums<V>(g, b, col, (int)threadIdx.x % span < T, threadIdx.x / span, blockDim.x / span, cols, out);
 }
 
 // The same with rows through shared memory (see norm_fwd_ring_kernel).  The sums over the rows fill the registers, so a row is read
 // twice from its stage, for its two sums and for its gradient; the stage is refilled after the next row's sums, when the whole team has
 // left it.
-template <typename TD, typename TX, typename TO, int V, int E>
+template <typename TD, typename TX, typename TO, int V, int E, int TT>
 __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __grid_constant__ BwdParams P, const __grid_constant__ Ring R)
 {
     constexpr int P2 = E / 2, W = V;         // elements worked on at a time
@@ -647,10 +792,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
     __shared__ __align__(16) float red[2][32][2];
     __shared__ volatile int gave_up;
     unsigned int turn = 0;
-    const int T = P.T, team = threadIdx.x / T, t = threadIdx.x - team * T, C = (int)P.C;
+    const int T = TT ? TT : P.T, team = threadIdx.x / T, t = threadIdx.x - team * T, C = TT ? TT * E : (int)P.C;
     const int teams = blockDim.x / T, barrier = teams > 1 ? team + 1 : 0;
     const float inv = 1.0f / (float)C;
-    const Columns<V, 0> col{T, t, C};
+    const Columns<V, TT> col{T, t, C};
     if (t == 0)
         for (int s = 0; s < R.stages; ++s) mbar_init(&full[team][s], 1);
     if (threadIdx.x == 0) gave_up = 0;
@@ -724,7 +869,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
             }
         }
         float sums[2] = {sum2(s0), ok ? sum2(s1) : __uint_as_float(0x7FC00000u)};
-        team_sum(sums, T, red, turn, barrier);
+        if constexpr (TT > 0) team_sum<TT>(sums, red, turn, barrier);
+        else team_sum(sums, T, red, turn, barrier);
         // the whole team has left the row before this one: its stage is free
         if (T == 32) __syncwarp();
         if (t == 0 && r != first) issue(r + (R.stages - 1) * step, s == 0 ? R.stages - 1 : s - 1);
@@ -753,25 +899,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
     if (P.part == nullptr) return;
     __syncthreads();                         // no copy is on its way: the ring takes the sums, the teams in turn
     float *const cols = reinterpret_cast<float *>(ring), *const out = P.part + (long long)blockIdx.x * 2 * C;
-    for (int k = 0; k < teams; ++k) {
-        if (team == k)
+    float g[E], b[E];
 #pragma unroll
-            for (int i = 0; i < P2; ++i) {
-                float g[2], b[2];
-                each(a_g[i], g[0], g[1]);
-                each(a_b[i], b[0], b[1]);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int e = 2 * i + h, c = col(e / V) + e % V;
-                    if (c >= C) continue;
-                    if (k > 0) { g[h] += cols[c]; b[h] += cols[C + c]; }
-                    float *const to = k == teams - 1 ? out : cols;
-                    to[c] = g[h];
-                    to[C + c] = b[h];
-                }
-            }
-        __syncthreads();
-    }
+    for (int i = 0; i < P2; ++i) { each(a_g[i], g[2 * i], g[2 * i + 1]); each(a_b[i], b[2 * i], b[2 * i + 1]); }
+    join_sums<V>(g, b, col, true, team, teams, cols, out);
 }
 
 // Long rows, first pass: sum(g) / C and sum(g xh) / C of every row.
@@ -950,30 +1081,57 @@ template <typename Kernel> int allow_ring(Kernel kernel, int device, bool (&done
     done[device] = true;
     return TWN_OK;
 }
-template <typename TX, typename TY, int V, int E> bool fwd_ring(FwdParams &P, const twn_device_info &dev, cudaStream_t s, int &rc)
+template <typename TX, typename TY, int V, int E, int TT> int launch_fwd_ring(const FwdParams &P, const RingShape &r, const twn_device_info &dev, cudaStream_t s)
 {
     static bool done[64] = {false};
+    const int rc = allow_ring(norm_fwd_ring_kernel<TX, TY, V, E, TT>, dev.ordinal, done);
+    if (rc != TWN_OK) return rc;
+    const int grid = (int)std::min<long long>((P.M + r.teams - 1) / r.teams, dev.sm_count);
+    TWN_CUDA_OK(twn_launch_small(norm_fwd_ring_kernel<TX, TY, V, E, TT>, grid, r.T * r.teams, r.smem, s, P, r.ring));
+    return TWN_OK;
+}
+template <typename TX, typename TY, int V, int E> bool fwd_ring(FwdParams &P, const twn_device_info &dev, cudaStream_t s, int &rc)
+{
     RingShape r;
     if (!ring_shape(r, P.C, E, fwd_ring_threads<E>(), P.C * sizeof(TX), 0, 2 * sizeof(float) * P.C)) return false;
-    rc = allow_ring(norm_fwd_ring_kernel<TX, TY, V, E>, dev.ordinal, done);
-    if (rc != TWN_OK) return true;
     P.T = r.T;
-    const int grid = (int)std::min<long long>((P.M + r.teams - 1) / r.teams, dev.sm_count);
-    if (twn_launch_small(norm_fwd_ring_kernel<TX, TY, V, E>, grid, r.T * r.teams, r.smem, s, P, r.ring) != cudaSuccess) rc = TWN_ERR_CUDA;
+    const int filled = P.C == (long long)r.T * E ? r.T : 0;
+    if constexpr (E == 64) {
+        rc = filled == 32    ? launch_fwd_ring<TX, TY, V, E, 32>(P, r, dev, s)
+             : filled == 64  ? launch_fwd_ring<TX, TY, V, E, 64>(P, r, dev, s)
+             : filled == 128 ? launch_fwd_ring<TX, TY, V, E, 128>(P, r, dev, s)
+             : filled == 256 ? launch_fwd_ring<TX, TY, V, E, 256>(P, r, dev, s)
+             : filled == 512 ? launch_fwd_ring<TX, TY, V, E, 512>(P, r, dev, s)
+                             : launch_fwd_ring<TX, TY, V, E, 0>(P, r, dev, s);
+    } else {
+        rc = filled == 32 ? launch_fwd_ring<TX, TY, V, E, 32>(P, r, dev, s) : launch_fwd_ring<TX, TY, V, E, 0>(P, r, dev, s);
+    }
     return true;
+}
+template <typename TD, typename TX, typename TO, int V, int E, int TT>
+int launch_bwd_ring(const BwdParams &P, const RingShape &r, const twn_device_info &dev, cudaStream_t s)
+{
+    static bool done[64] = {false};
+    const int rc = allow_ring(norm_bwd_ring_kernel<TD, TX, TO, V, E, TT>, dev.ordinal, done);
+    if (rc != TWN_OK) return rc;
+    TWN_CUDA_OK(twn_launch_small(norm_bwd_ring_kernel<TD, TX, TO, V, E, TT>, P.parts, r.T * r.teams, r.smem, s, P, r.ring));
+    return TWN_OK;
 }
 template <typename TD, typename TX, typename TO, int V, int E> bool bwd_ring(BwdParams &P, const twn_device_info &dev, cudaStream_t s, int &rc)
 {
-    static bool done[64] = {false};
     RingShape r;
     const size_t second = P.C * sizeof(TD);
     if (!ring_shape(r, P.C, E, kBwdThreads, second + P.C * sizeof(TX), second, sizeof(float) * P.C)) return false;
-    rc = allow_ring(norm_bwd_ring_kernel<TD, TX, TO, V, E>, dev.ordinal, done);
-    if (rc != TWN_OK) return true;
     P.T = r.T;
     P.parts = (int)std::min<long long>((P.M + r.teams - 1) / r.teams, std::min(dev.sm_count, kPartBlocks));
-    const size_t smem = std::max<size_t>(r.smem, r.teams > 1 ? 2 * sizeof(float) * P.C : 0);
-    if (twn_launch_small(norm_bwd_ring_kernel<TD, TX, TO, V, E>, P.parts, r.T * r.teams, smem, s, P, r.ring) != cudaSuccess) rc = TWN_ERR_CUDA;
+    // at most 512 threads of 32 columns: 128 KB
+    r.smem = std::max<size_t>(r.smem, r.teams > 1 ? r.teams * 2 * sizeof(float) * P.C : 0);
+    const int filled = P.C == (long long)r.T * E ? r.T : 0;
+    rc = filled == 64    ? launch_bwd_ring<TD, TX, TO, V, E, 64>(P, r, dev, s)
+         : filled == 128 ? launch_bwd_ring<TD, TX, TO, V, E, 128>(P, r, dev, s)
+         : filled == 256 ? launch_bwd_ring<TD, TX, TO, V, E, 256>(P, r, dev, s)
+         : filled == 512 ? launch_bwd_ring<TD, TX, TO, V, E, 512>(P, r, dev, s)
+                         : launch_bwd_ring<TD, TX, TO, V, E, 0>(P, r, dev, s);
     return true;
 }
 
@@ -982,13 +1140,20 @@ template <typename TX, typename TY, int V> int fwd(FwdParams &P, const twn_devic
     if constexpr (V > 1) {
         int rc = TWN_OK;
         if (P.C > 256 && P.M * P.C >= kRingElements &&
-            (P.C <= 512 ? fwd_ring<TX, TY, V, 16>(P, dev, s, rc) : P.C <= 1024 ? fwd_ring<TX, TY, V, 32>(P, dev, s, rc) : fwd_ring<TX, TY, V, 64>(P, dev, s, rc)))
+            (P.C <= 512 ? fwd_ring<TX, TY, V, 16>(P, dev, s, rc)
+         : P.C <= 1024 ? fwd_ring<TX, TY, V, 32>(P, dev, s, rc)
+                       : fwd_ring<TX, TY, V, 64>(P, dev, s, rc)))
             return rc;
     }
     if (P.C <= 32 * 8) return launch_fwd<TX, TY, V, 8, 0>(P, team_for(P.C, 8, 4, 32), s);
     if constexpr (V > 1) {
-        if (P.C <= 8 * 1024) return launch_fwd<TX, TY, V, 16, 0>(P, team_for(P.C, 16, 32, 512), s);
-        if (P.C <= 32 * 1024) return launch_fwd<TX, TY, V, 32, 0>(P, team_for(P.C, 32, 512, 1024), s);
+        if (P.C <= 512) return launch_fwd<TX, TY, V, 16, 32>(P, 32, s);
+        if (P.C <= 1024) return launch_fwd<TX, TY, V, 16, 64>(P, 64, s);
+        if (P.C <= 2048) return launch_fwd<TX, TY, V, 16, 128>(P, 128, s);
+        if (P.C <= 4096) return launch_fwd<TX, TY, V, 16, 256>(P, 256, s);
+        if (P.C <= 8192) return launch_fwd<TX, TY, V, 16, 512>(P, 512, s);
+        if (P.C <= 16384) return launch_fwd<TX, TY, V, 32, 512>(P, 512, s);
+        if (P.C <= 32768) return launch_fwd<TX, TY, V, 32, 1024>(P, 1024, s);
     } else {
         if (P.C <= 512) return launch_fwd<TX, TY, 1, 16, 32>(P, 32, s);
         if (P.C <= 1024) return launch_fwd<TX, TY, 1, 16, 64>(P, 64, s);
@@ -1007,6 +1172,15 @@ template <typename TX, typename TY> int fwd_any(FwdParams &P, bool vec, const tw
     return vec ? fwd<TX, TY, V>(P, dev, s) : fwd<TX, TY, 1>(P, dev, s);
 }
 
+template <typename TD, typename TX, typename TO, int V, int E, int TT>
+int launch_bwd_rows(BwdParams &P, int threads, size_t smem, const twn_device_info &dev, cudaStream_t s)
+{
+    static bool done[64] = {false};
+    const int rc = allow_ring(norm_bwd_kernel<TD, TX, TO, V, E, TT>, dev.ordinal, done);
+    if (rc != TWN_OK) return rc;
+    TWN_CUDA_OK(twn_launch_small(norm_bwd_kernel<TD, TX, TO, V, E, TT>, P.parts, threads, smem, s, P));
+    return TWN_OK;
+}
 template <typename TD, typename TX, typename TO, int V, int E> int bwd_rows(BwdParams &P, const twn_device_info &dev, cudaStream_t s)
 {
     P.T = team_for(P.C, E, 4, kBwdThreads);
@@ -1015,28 +1189,26 @@ template <typename TD, typename TX, typename TO, int V, int E> int bwd_rows(BwdP
     while (threads > std::max(P.T, 128) && (P.M * P.T + threads - 1) / threads < dev.sm_count) threads /= 2;
     const int teams = threads / P.T;
     P.parts = (int)std::max<long long>(1, std::min<long long>((P.M + teams - 1) / teams, std::min(dev.sm_count, kPartBlocks)));
-    const size_t smem = teams > 1 && P.part ? 2 * sizeof(float) * P.C : 0;
-    auto launch = [&](auto kernel) { return twn_launch_small(kernel, P.parts, threads, smem, s, P); };
-    cudaError_t e = cudaSuccess;
-    if constexpr (V > 1) e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 0>);
-    else
-        switch (P.T) {
-            case 32: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 32>); break;
-            case 64: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 64>); break;
-            case 128: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 128>); break;
-            case 256: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 256>); break;
-            case 512: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 512>); break;
-            default: e = launch(norm_bwd_kernel<TD, TX, TO, V, E, 0>);
-        }
-    TWN_CUDA_OK(e);
-    return TWN_OK;
+    const int parties = threads / std::max(P.T, 32);
+    const size_t sums = parties > 1 && P.part ? parties * 2 * sizeof(float) * P.C : 0;
+    const size_t smem = V > 1 ? std::max<size_t>(sums, (size_t)kBwdStages * threads * bwd_stage_bytes<TD, TX, E>()) : sums;
+    switch (P.T) {
+        case 4: return launch_bwd_rows<TD, TX, TO, V, E, V == 1 ? 0 : 4>(P, threads, smem, dev, s);
+        case 8: return launch_bwd_rows<TD, TX, TO, V, E, V == 1 ? 0 : 8>(P, threads, smem, dev, s);
+        case 16: return launch_bwd_rows<TD, TX, TO, V, E, V == 1 ? 0 : 16>(P, threads, smem, dev, s);
+        case 32: return launch_bwd_rows<TD, TX, TO, V, E, 32>(P, threads, smem, dev, s);
+        case 64: return launch_bwd_rows<TD, TX, TO, V, E, 64>(P, threads, smem, dev, s);
+        case 128: return launch_bwd_rows<TD, TX, TO, V, E, 128>(P, threads, smem, dev, s);
+        case 256: return launch_bwd_rows<TD, TX, TO, V, E, 256>(P, threads, smem, dev, s);
+        default: return launch_bwd_rows<TD, TX, TO, V, E, 512>(P, threads, smem, dev, s);
+    }
 }
 template <typename TD, typename TX, typename TO, int V> int bwd(BwdParams &P, float *dgamma, float *dbeta, const twn_device_info &dev, cudaStream_t s)
 {
     constexpr int E = V == 8 && sizeof(TD) == 2 && sizeof(TX) == 2 ? 16 : 8;
     int rc = TWN_OK;
     bool served = false;
-    if constexpr (V > 1) served = P.C > kBwdThreads * E && P.M * P.C >= kRingElements && bwd_ring<TD, TX, TO, V, 32>(P, dev, s, rc);
+    if constexpr (V > 1) served = P.C > 2048 && P.M * P.C >= kRingElements && bwd_ring<TD, TX, TO, V, 32>(P, dev, s, rc);
     if (served) {
         if (rc != TWN_OK) return rc;
     } else if (V == 1 && P.C <= kBwdThreads * 16 && (P.C > kBwdThreads * E || P.M * P.C >= 1 << 23)) {
