@@ -3,6 +3,7 @@
 //   forward   mean = sum x / C,  var = sum (x - mean)^2 / C,  rstd = 1 / sqrt(var + eps),  y = (x - mean) rstd gamma + beta
 //   backward  xh = (x - mean) rstd,  g = dy gamma,  dx = rstd (g - sum(g) / C - xh sum(g xh) / C),
 //             dgamma = sum over the rows of dy xh,  dbeta = sum over the rows of dy
+//   computed with d = x - mean and h = rstd g, so that xh is never formed:  dx = h - sum(h) / C - d rstd^2 sum(h d) / C
 //
 // Both are bound by HBM: a row is read once and stays in registers until its result is written.  A team of T threads (4 to
 // 1024, a power of two) has a row, E elements a thread; its sums are shuffle trees, and one barrier where it is more than a
@@ -383,10 +384,12 @@ __global__ void __launch_bounds__(TT > 32 ? TT : TT == 32 || E < 16 ? 128 : 1024
 // ---- rows through shared memory ---------------------------------------------------------------------------------------------
 // Large tensors of aligned rows.  With 16 elements a thread, all of them in registers, a row of 4096 took 31 instructions an element,
 // most of them the fixed part of a row: two sums, the barriers, the root, the addresses; with more, few rows fit the registers, and
-// too little is on its way.  Here rows come by bulk copies into a ring in shared memory, up to 200 KB an SM on their way, for threads
+// too little is on its way.  Here rows come by bulk copies into a ring in shared memory, up to 192 KB an SM on their way, for threads
 // of up to 64 elements.
 constexpr int kMaxRing = 8, kMaxTeams = 32;
-constexpr size_t kRingBytes = 200 * 1024;
+// Of the 227 KB that a block may have; 2.6 KB are barriers and sums.  Forward with 200 KB, two stages at 16384 x 4096 instead of three, took 48.0 us for 46.6;
+// backward with 224 KB, three instead of two, 85.7 for 82.2.
+constexpr size_t kFwdRingBytes = 224 * 1024, kBwdRingBytes = 200 * 1024;
 struct Ring {
     int stages, stage_bytes, second;         // of a stage: where a second tensor's row begins
     int params;                              // bytes at the front that hold gamma (and beta), 0: they are read from global memory
@@ -439,8 +442,9 @@ __global__ void __launch_bounds__(fwd_ring_threads<E>(), 1) norm_fwd_ring_kernel
     };
     if (t == 0)
         for (int s = 0; s < R.stages; ++s) issue(first + s * step, s);
-    float *const gammas = R.params ? reinterpret_cast<float *>(ring) : nullptr, *const betas = R.params ? gammas + C : nullptr;
-    if (R.params) {
+    const bool in_ring = TT ? 2 * TT * E * sizeof(float) <= kFwdRingBytes / 2 : R.params > 0;
+    float *const gammas = in_ring ? reinterpret_cast<float *>(ring) : nullptr, *const betas = in_ring ? gammas + C : nullptr;
+    if (in_ring) {
         for (int c = threadIdx.x; c < C; c += blockDim.x) {
             gammas[param_at<V>(c, C)] = P.gamma ? P.gamma[c] : 1.0f;
             betas[param_at<V>(c, C)] = P.beta ? P.beta[c] : 0.0f;
@@ -562,6 +566,7 @@ struct BwdParams {
     float *row_sums;             // long rows: [M][2]
     long long lddy, ldx, lddx, M, C;
     int T, parts;
+    bool bulk;                   // rows of dY and X on 16-byte boundaries, a multiple of that long
 };
 
 constexpr int kBwdThreads = 512;
@@ -596,28 +601,27 @@ __device__ __forceinline__ void join_sums(const float (&g)[E], const float (&b)[
     }
 }
 
-// 16 bytes (or 4) to shared memory on their own way; zeros where `there` is false.
-__device__ __forceinline__ void copy_piece(uint32_t dst, const void *src, bool there)
+// 16, 8 or 4 bytes to shared memory on their own way; zeros where `there` is false.
+template <int BYTES> __device__ __forceinline__ void copy_piece(uint32_t dst, const void *src, bool there)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy_float(uint32_t dst, const float *src, bool there)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(there ? BYTES : 0) : "memory");
 }
 // Bytes of a thread's part of a row in a stage: dY, X, mean and rstd.
 template <typename TD, typename TX, int E> __host__ __device__ constexpr int bwd_stage_bytes() { return E * (int)(sizeof(TD) + sizeof(TX)) + 8; }
-constexpr int kBwdStages = 5;
+// A thread has sixteen elements of a row.  As many stages as fit 208 KB of shared memory for 512 threads: five where dY and X are bf16, three where both are fp32.
+template <typename TD, typename TX> __host__ __device__ constexpr int bwd_stages() { return sizeof(TD) + sizeof(TX) == 4 ? 5 : sizeof(TD) + sizeof(TX) == 6 ? 4 : 3; }
 
 // One row per team; sums over the rows of a block stay in the registers of the threads that own the columns, and its teams join them in
 // shared memory at the end.  C <= T * E.  Vectors come through shared memory, every thread's own elements by its own copies, so no
-// barrier guards them: four rows of every team are on their way (one, in registers, was 32 KB an SM and took SHORT us for
-// 200704 x 64 and LONG for 16384 x 4096).  Single elements (V = 1) of the next row are in registers.
+// barrier guards them: two to four rows of every team are on their way.  Single elements (V = 1) of the next row are in registers.
+// With sixteen elements a thread the fixed part of a row is half that of eight (32 M elements in rows of 2304, fp32: 83 us, 130 with eight).
 template <typename TD, typename TX, typename TO, int V, int E, int TT>
 __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_constant__ BwdParams P)
 {
     constexpr int NV = E / V, P2 = E / 2;
     constexpr bool kRing = V > 1;
+    constexpr uint32_t kStages = bwd_stages<TD, TX>();
     extern __shared__ __align__(16) uint8_t bwd_smem[];      // the stages; [2][C] sums when a block has several teams (of a warp or more)
     __shared__ __align__(16) float red[2][32][2];
     unsigned int turn = 0;
@@ -655,60 +659,52 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
         load_vectors(nd, d, col, live);
         load_vectors(nx, x, col, live);
     };
-    // a stage: pieces of 16 bytes, piece p of all threads next to each other, then the means, then the 1/deviations
-    constexpr int kPD = V * (int)sizeof(TD) / 16, kPX = V * (int)sizeof(TX) / 16, kPieces = NV * (kPD + kPX);
-    const uint32_t threads = blockDim.x, stage = threads * bwd_stage_bytes<TD, TX, E>();
-    const uint32_t mine = smem_u32(bwd_smem) + 16 * threadIdx.x, floats = smem_u32(bwd_smem) + 16 * kPieces * threads + 4 * threadIdx.x;
+    // a stage: vector j of dY of all threads, one next to the other, for every j; X likewise; the means, the 1/deviations
+    constexpr uint32_t kD = V * sizeof(TD), kX = V * sizeof(TX);
+    const uint32_t threads = blockDim.x, stage = threads * bwd_stage_bytes<TD, TX, E>(), x_at = NV * kD * threads, mean_at = x_at + NV * kX * threads;
     auto issue = [&](long long r, uint32_t s) {
         const bool live = r < P.M;
         const long long row = live ? r : 0;
-        const TD *d = static_cast<const TD *>(P.dY) + row * P.lddy + t * V;
+        const TD *dy = static_cast<const TD *>(P.dY) + row * P.lddy + t * V;
         const TX *x = static_cast<const TX *>(P.X) + row * P.ldx + t * V;
-        const uint32_t to = mine + s * stage;
+        const uint32_t to = smem_u32(bwd_smem) + s * stage;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            // what is not there is copied from the first elements, no byte of it
             const bool there = live && col(j) < C;
-            const int c = there ? j * T * V : 0;             // an address inside the row, whatever is copied
-#pragma unroll
-            for (int p = 0; p < kPD; ++p) copy_piece(to + 16 * threads * (j * kPD + p), (there ? d : static_cast<const TD *>(P.dY)) + c + p * (16 / sizeof(TD)), there);
-#pragma unroll
-            for (int p = 0; p < kPX; ++p)
-                copy_piece(to + 16 * threads * (NV * kPD + j * kPX + p), (there ? x : static_cast<const TX *>(P.X)) + c + p * (16 / sizeof(TX)), there);
+            copy_piece<kD>(to + kD * (j * threads + threadIdx.x), there ? dy + j * T * V : static_cast<const TD *>(P.dY), there);
+            copy_piece<kX>(to + x_at + kX * (j * threads + threadIdx.x), there ? x + j * T * V : static_cast<const TX *>(P.X), there);
         }
-        copy_float(floats + s * stage, P.mean + row, live);
-        copy_float(floats + s * stage + 4 * threads, P.rstd + row, live);
+        copy_piece<4>(to + mean_at + 4 * threadIdx.x, P.mean + row, live);
+        copy_piece<4>(to + mean_at + 4 * (threads + threadIdx.x), P.rstd + row, live);
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     long long r0 = (long long)blockIdx.x * teams;
-    uint32_t s_in = kBwdStages - 1, s_out = 0;
+    uint32_t s_in = kStages - 1, s_out = 0;
     if constexpr (kRing) {
         if (r0 < P.M)
-            for (uint32_t k = 0; k < kBwdStages - 1; ++k) issue(r0 + team + k * step, k);
+            for (uint32_t k = 0; k < kStages - 1; ++k) issue(r0 + team + k * step, k);
     } else {
         if (r0 < P.M) fetch(r0 + team);
     }
     for (; r0 < P.M; r0 += step) {
         const long long r = r0 + team;
         const bool live = r < P.M;
-        two_f32 dy[P2], xh[P2];
+        two_f32 g[P2], d[P2];                    // dY, then rstd g; X, then X - mean
         float mean, rstd;
         if constexpr (kRing) {
-            issue(r + (kBwdStages - 1) * step, s_in);
-            if (++s_in == kBwdStages) s_in = 0;
-            asm volatile("cp.async.wait_group %0;" ::"n"(kBwdStages - 1) : "memory");
+            issue(r + (kStages - 1) * step, s_in);
+            if (++s_in == kStages) s_in = 0;
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
             const uint8_t *const from = bwd_smem + s_out * stage;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-#pragma unroll
-                for (int p = 0; p < kPD; ++p)
-                    reinterpret_cast<uint4 *>(&nd[j])[p] = *reinterpret_cast<const uint4 *>(from + 16 * (threads * (j * kPD + p) + threadIdx.x));
-#pragma unroll
-                for (int p = 0; p < kPX; ++p)
-                    reinterpret_cast<uint4 *>(&nx[j])[p] = *reinterpret_cast<const uint4 *>(from + 16 * (threads * (NV * kPD + j * kPX + p) + threadIdx.x));
+                nd[j].load(reinterpret_cast<const TD *>(from + kD * (j * threads + threadIdx.x)));
+                nx[j].load(reinterpret_cast<const TX *>(from + x_at + kX * (j * threads + threadIdx.x)));
             }
-            mean = *reinterpret_cast<const float *>(from + 16 * kPieces * threads + 4 * threadIdx.x);
-            rstd = *reinterpret_cast<const float *>(from + 16 * kPieces * threads + 4 * (threads + threadIdx.x));
-            if (++s_out == kBwdStages) s_out = 0;
+            mean = *reinterpret_cast<const float *>(from + mean_at + 4 * threadIdx.x);
+            rstd = *reinterpret_cast<const float *>(from + mean_at + 4 * (threads + threadIdx.x));
+            if (++s_out == kStages) s_out = 0;
         }
         {
             float fd[E], fx[E];
@@ -719,8 +715,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
             }
 #pragma unroll
             for (int i = 0; i < P2; ++i) {
-                dy[i] = two(fd[2 * i], fd[2 * i + 1]);
-                xh[i] = two(fx[2 * i], fx[2 * i + 1]);
+                g[i] = two(fd[2 * i], fd[2 * i + 1]);
+                d[i] = two(fx[2 * i], fx[2 * i + 1]);
             }
         }
         if constexpr (!kRing) {
@@ -733,24 +729,25 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
         two_f32 s0 = 0, s1 = 0;
 #pragma unroll
         for (int i = 0; i < P2; ++i) {
-            xh[i] = mul2(add2(xh[i], minus), scale);
-            a_g[i] = fma2(dy[i], xh[i], a_g[i]);
-            a_b[i] = add2(a_b[i], dy[i]);
-            dy[i] = mul2(dy[i], ga[i]);
-            s0 = add2(s0, dy[i]);
-            s1 = fma2(dy[i], xh[i], s1);
+            d[i] = add2(d[i], minus);
+            a_b[i] = add2(a_b[i], g[i]);
+            g[i] = mul2(g[i], scale);
+            a_g[i] = fma2(g[i], d[i], a_g[i]);
+            g[i] = mul2(g[i], ga[i]);
+            s0 = add2(s0, g[i]);
+            s1 = fma2(g[i], d[i], s1);
         }
         if (P.dX == nullptr) continue;
         float s[2] = {sum2(s0), sum2(s1)};
         if constexpr (TT > 0) team_sum<TT>(s, red, turn, barrier);
         else team_sum(s, T, red, turn, barrier);
         if (!live) continue;
-        const float c0 = -s[0] * inv, c1 = -s[1] * inv;
+        const float c0 = -s[0] * inv, c1 = -s[1] * inv * rstd * rstd;
         const two_f32 k0 = two(c0, c0), k1 = two(c1, c1);
         TO *o = static_cast<TO *>(P.dX) + r * P.lddx;
         float f[E];
 #pragma unroll
-        for (int i = 0; i < P2; ++i) each(mul2(fma2(xh[i], k1, add2(dy[i], k0)), scale), f[2 * i], f[2 * i + 1]);
+        for (int i = 0; i < P2; ++i) each(fma2(d[i], k1, add2(g[i], k0)), f[2 * i], f[2 * i + 1]);
         if (P.add)
 #pragma unroll
             for (int j = 0; j < NV; ++j) add_vector(*reinterpret_cast<float(*)[V]>(f + j * V), static_cast<const TO *>(P.add) + r * P.lddx, col, j);
@@ -780,7 +777,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
     join_sums<V>(g, b, col, (int)threadIdx.x % span < T, threadIdx.x / span, blockDim.x / span, cols, out);
 }
 
-// The same with rows through shared memory (see norm_fwd_ring_kernel).  The sums over the rows fill the registers, so a row is read
+// Rows of more than 8192 elements, through shared memory by bulk copies (see norm_fwd_ring_kernel; up to 8192 it is behind the one above by up to 1.6 times).  The sums over the rows fill the registers, so a row is read
 // twice from its stage, for its two sums and for its gradient; the stage is refilled after the next row's sums, when the whole team has
 // left it.
 template <typename TD, typename TX, typename TO, int V, int E, int TT>
@@ -813,8 +810,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
     };
     if (t == 0)
         for (int s = 0; s < R.stages; ++s) issue(first + s * step, s);
-    float *const gammas = R.params ? reinterpret_cast<float *>(ring) : nullptr;
-    if (R.params) {
+    const bool in_ring = TT ? TT * E * sizeof(float) <= kBwdRingBytes / 2 : R.params > 0;
+    float *const gammas = in_ring ? reinterpret_cast<float *>(ring) : nullptr;
+    if (in_ring) {
         for (int c = threadIdx.x; c < C; c += blockDim.x) gammas[param_at<V>(c, C)] = P.gamma ? P.gamma[c] : 1.0f;
         __syncthreads();
     }
@@ -832,40 +830,38 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
         const TX *const x = reinterpret_cast<const TX *>(st + R.second);
         const TD *const dy = reinterpret_cast<const TD *>(st);
         const two_f32 minus = two(-mean, -mean), scale = two(rstd, rstd);
-        // W elements from e on: xh, dy, and g = dy gamma (past the row's end dy and gamma are zero)
-        auto load = [&](int e, two_f32 (&xh)[W / 2], two_f32 (&d)[W / 2], two_f32 (&g)[W / 2]) {
+        // W elements from e on: d = x - mean, dy, gamma (past the row's end dy and gamma are zero)
+        auto load = [&](int e, two_f32 (&d)[W / 2], two_f32 (&g)[W / 2], two_f32 (&ga)[W / 2]) {
             float fx[W], fd[W], fg[W];
+            const int j = e / V;
+            read_vector(x, col, j, fx);
+            read_vector(dy, col, j, fd);
+            if (col.whole(j) || col(j) < C) {
+                read_param<V>(gammas, P.gamma, col(j), C, 1.0f, fg);
+            } else {
 #pragma unroll
-            for (int h = 0; h < W; h += V) {
-                const int j = (e + h) / V;
-                read_vector(x, col, j, *reinterpret_cast<float(*)[V]>(fx + h));
-                read_vector(dy, col, j, *reinterpret_cast<float(*)[V]>(fd + h));
-                float(&gv)[V] = *reinterpret_cast<float(*)[V]>(fg + h);
-                if (col.whole(j) || col(j) < C) {
-                    read_param<V>(gammas, P.gamma, col(j), C, 1.0f, gv);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) gv[i] = 0.0f;
-                }
+                for (int i = 0; i < V; ++i) fg[i] = 0.0f;
             }
 #pragma unroll
             for (int i = 0; i < W / 2; ++i) {
-                xh[i] = mul2(add2(two(fx[2 * i], fx[2 * i + 1]), minus), scale);
-                d[i] = two(fd[2 * i], fd[2 * i + 1]);
-                g[i] = mul2(d[i], two(fg[2 * i], fg[2 * i + 1]));
+                d[i] = add2(two(fx[2 * i], fx[2 * i + 1]), minus);
+                g[i] = two(fd[2 * i], fd[2 * i + 1]);
+                ga[i] = two(fg[2 * i], fg[2 * i + 1]);
             }
         };
         two_f32 s0 = 0, s1 = 0;
 #pragma unroll
         for (int e = 0; e < E; e += W) {
-            two_f32 xh[W / 2], d[W / 2], g[W / 2];
-            load(e, xh, d, g);
+            two_f32 d[W / 2], g[W / 2], ga[W / 2];
+            load(e, d, g, ga);
 #pragma unroll
             for (int i = 0; i < W / 2; ++i) {
-                a_g[e / 2 + i] = fma2(d[i], xh[i], a_g[e / 2 + i]);
-                a_b[e / 2 + i] = add2(a_b[e / 2 + i], d[i]);
+                a_b[e / 2 + i] = add2(a_b[e / 2 + i], g[i]);
+                g[i] = mul2(g[i], scale);
+                a_g[e / 2 + i] = fma2(g[i], d[i], a_g[e / 2 + i]);
+                g[i] = mul2(g[i], ga[i]);
                 s0 = add2(s0, g[i]);
-                s1 = fma2(g[i], xh[i], s1);
+                s1 = fma2(g[i], d[i], s1);
             }
         }
         float sums[2] = {sum2(s0), ok ? sum2(s1) : __uint_as_float(0x7FC00000u)};
@@ -875,23 +871,20 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
         if (T == 32) __syncwarp();
         if (t == 0 && r != first) issue(r + (R.stages - 1) * step, s == 0 ? R.stages - 1 : s - 1);
         if (P.dX) {
-            const float c0 = -sums[0] * inv, c1 = -sums[1] * inv;
+            const float c0 = -sums[0] * inv, c1 = -sums[1] * inv * rstd * rstd;
             const two_f32 k0 = two(c0, c0), k1 = two(c1, c1);
             TO *o = static_cast<TO *>(P.dX) + r * P.lddx;
             const TO *const add = P.add ? static_cast<const TO *>(P.add) + r * P.lddx : nullptr;
 #pragma unroll
             for (int e = 0; e < E; e += W) {
-                two_f32 xh[W / 2], d[W / 2], g[W / 2];
-                load(e, xh, d, g);
+                two_f32 d[W / 2], g[W / 2], ga[W / 2];
+                load(e, d, g, ga);
                 float f[W];
 #pragma unroll
-                for (int i = 0; i < W / 2; ++i) each(mul2(fma2(xh[i], k1, add2(g[i], k0)), scale), f[2 * i], f[2 * i + 1]);
-#pragma unroll
-                for (int h = 0; h < W; h += V) {
-                    const int j = (e + h) / V;
-                    if (add) add_vector(*reinterpret_cast<float(*)[V]>(f + h), add, col, j);
-                    if (col.whole(j) || col(j) < C) store(o + col(j), *reinterpret_cast<const float(*)[V]>(f + h));
-                }
+                for (int i = 0; i < W / 2; ++i) each(fma2(d[i], k1, fma2(g[i], mul2(ga[i], scale), k0)), f[2 * i], f[2 * i + 1]);
+                const int j = e / V;
+                if (add) add_vector(f, add, col, j);
+                if (col.whole(j) || col(j) < C) store(o + col(j), f);
             }
         }
         if (++s == R.stages) { s = 0; ph ^= 1u; }
@@ -994,28 +987,47 @@ __global__ void __launch_bounds__(kStripeThreads) norm_bwd_stripe_kernel(const _
 // dgamma and dbeta: a column's parts in 32 runs, all of a run's loads at once (with eight runs, one load after the other, the fold of 148
 // parts took longer than what it folds), and the runs in order.
 constexpr int kPartBlocks = 148, kRuns = 32, kPerRun = (kPartBlocks + kRuns - 1) / kRuns;
-__global__ void __launch_bounds__(32 * kRuns) norm_fold_kernel(const float *part, int parts, long long C, float *dgamma, float *dbeta)
+// W columns a thread, so that up to 4736 channels, or 9472, are a block an SM, which may start early.
+template <int W> __global__ void __launch_bounds__(32 * kRuns) norm_fold_kernel(const float *part, int parts, long long C, float *dgamma, float *dbeta)
 {
-    __shared__ float s[kRuns][32];
+    __shared__ float s[kRuns][32 * W];
     pdl_begin();
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
-    const long long c = (long long)blockIdx.x * 32 + lane;
-    float w[kPerRun], v = 0.0f;
+    const long long c = ((long long)blockIdx.x * 32 + lane) * W;
+    float w[kPerRun][W], v[W];
 #pragma unroll
     for (int k = 0; k < kPerRun; ++k) {
         const int p = run + kRuns * k;
-        w[k] = p < parts && c < 2 * C ? __ldg(part + (long long)p * 2 * C + c) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[k][i] = 0.0f;
+        if (p < parts && c < 2 * C) {
+            const float *const from = part + (long long)p * 2 * C + c;
+            if constexpr (W == 4) {
+                const float4 a = __ldg(reinterpret_cast<const float4 *>(from));
+                w[k][0] = a.x; w[k][1] = a.y; w[k][2] = a.z; w[k][3] = a.w;
+            } else if constexpr (W == 2) {
+                const float2 a = __ldg(reinterpret_cast<const float2 *>(from));
+                w[k][0] = a.x; w[k][1] = a.y;
+            } else {
+                w[k][0] = __ldg(from);
+            }
+        }
     }
 #pragma unroll
-    for (int k = 0; k < kPerRun; ++k) v += w[k];
-    s[run][lane] = v;
-    __syncthreads();
-    if (run == 0 && c < 2 * C) {
-        v = 0.0f;
+    for (int i = 0; i < W; ++i) {
+        v[i] = 0.0f;
 #pragma unroll
-        for (int k = 0; k < kRuns; ++k) v += s[k][lane];
-        float *out = c < C ? dgamma : dbeta;
-        if (out) out[c < C ? c : c - C] = v;
+        for (int k = 0; k < kPerRun; ++k) v[i] += w[k][i];
+        s[run][lane * W + i] = v[i];
+    }
+    __syncthreads();
+    if (run < W) {
+        const long long at = (long long)blockIdx.x * 32 * W + threadIdx.x;
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kRuns; ++k) sum += s[k][threadIdx.x];
+        float *const out = at < C ? dgamma : dbeta;
+        if (at < 2 * C && out) out[at < C ? at : at - C] = sum;
     }
 }
 
@@ -1062,22 +1074,22 @@ struct RingShape {
     Ring ring;
     size_t smem;
 };
-bool ring_shape(RingShape &r, long long C, int E, int threads, size_t stage, size_t second, size_t params)
+bool ring_shape(RingShape &r, size_t bytes, long long C, int E, int threads, size_t stage, size_t second, size_t params)
 {
     r.T = (int)((C + 32 * E - 1) / (32 * E)) * 32;
     if (r.T > threads) return false;
     r.teams = std::min(threads / r.T, r.T > 32 ? 15 : kMaxTeams);          // a block has fifteen named barriers beside its own
     params = (params + 127) / 128 * 128;
-    if (params > kRingBytes / 2) params = 0;
-    while (r.teams > 1 && 2 * r.teams * stage > kRingBytes - params) --r.teams;
-    const int stages = (int)std::min<size_t>(kMaxRing, (kRingBytes - params) / (r.teams * stage));
+    if (params > bytes / 2) params = 0;
+    while (r.teams > 1 && 2 * r.teams * stage > bytes - params) --r.teams;
+    const int stages = (int)std::min<size_t>(kMaxRing, (bytes - params) / (r.teams * stage));
     r.ring = {stages, (int)stage, (int)second, (int)params};
     r.smem = params + r.teams * stages * stage;
     return stages >= 2 && r.teams * r.T >= 256 + 32;
 }
 template <typename Kernel> int allow_ring(Kernel kernel, int device, bool (&done)[64])
 {
-    if (!done[device]) TWN_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes));
+    if (!done[device]) TWN_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFwdRingBytes));
     done[device] = true;
     return TWN_OK;
 }
@@ -1093,7 +1105,7 @@ template <typename TX, typename TY, int V, int E, int TT> int launch_fwd_ring(co
 template <typename TX, typename TY, int V, int E> bool fwd_ring(FwdParams &P, const twn_device_info &dev, cudaStream_t s, int &rc)
 {
     RingShape r;
-    if (!ring_shape(r, P.C, E, fwd_ring_threads<E>(), P.C * sizeof(TX), 0, 2 * sizeof(float) * P.C)) return false;
+    if (!ring_shape(r, kFwdRingBytes, P.C, E, fwd_ring_threads<E>(), P.C * sizeof(TX), 0, 2 * sizeof(float) * P.C)) return false;
     P.T = r.T;
     const int filled = P.C == (long long)r.T * E ? r.T : 0;
     if constexpr (E == 64) {
@@ -1121,17 +1133,13 @@ template <typename TD, typename TX, typename TO, int V, int E> bool bwd_ring(Bwd
 {
     RingShape r;
     const size_t second = P.C * sizeof(TD);
-    if (!ring_shape(r, P.C, E, kBwdThreads, second + P.C * sizeof(TX), second, sizeof(float) * P.C)) return false;
+    if (!ring_shape(r, kBwdRingBytes, P.C, E, kBwdThreads, second + P.C * sizeof(TX), second, sizeof(float) * P.C)) return false;
     P.T = r.T;
     P.parts = (int)std::min<long long>((P.M + r.teams - 1) / r.teams, std::min(dev.sm_count, kPartBlocks));
     // at most 512 threads of 32 columns: 128 KB
     r.smem = std::max<size_t>(r.smem, r.teams > 1 ? r.teams * 2 * sizeof(float) * P.C : 0);
     const int filled = P.C == (long long)r.T * E ? r.T : 0;
-    rc = filled == 64    ? launch_bwd_ring<TD, TX, TO, V, E, 64>(P, r, dev, s)
-         : filled == 128 ? launch_bwd_ring<TD, TX, TO, V, E, 128>(P, r, dev, s)
-         : filled == 256 ? launch_bwd_ring<TD, TX, TO, V, E, 256>(P, r, dev, s)
-         : filled == 512 ? launch_bwd_ring<TD, TX, TO, V, E, 512>(P, r, dev, s)
-                         : launch_bwd_ring<TD, TX, TO, V, E, 0>(P, r, dev, s);
+    rc = filled == 512 ? launch_bwd_ring<TD, TX, TO, V, E, 512>(P, r, dev, s) : launch_bwd_ring<TD, TX, TO, V, E, 0>(P, r, dev, s);
     return true;
 }
 
@@ -1141,8 +1149,8 @@ template <typename TX, typename TY, int V> int fwd(FwdParams &P, const twn_devic
         int rc = TWN_OK;
         if (P.C > 256 && P.M * P.C >= kRingElements &&
             (P.C <= 512 ? fwd_ring<TX, TY, V, 16>(P, dev, s, rc)
-         : P.C <= 1024 ? fwd_ring<TX, TY, V, 32>(P, dev, s, rc)
-                       : fwd_ring<TX, TY, V, 64>(P, dev, s, rc)))
+             : P.C <= 1024 ? fwd_ring<TX, TY, V, 32>(P, dev, s, rc)
+                           : fwd_ring<TX, TY, V, 64>(P, dev, s, rc)))
             return rc;
     }
     if (P.C <= 32 * 8) return launch_fwd<TX, TY, V, 8, 0>(P, team_for(P.C, 8, 4, 32), s);
@@ -1191,7 +1199,7 @@ template <typename TD, typename TX, typename TO, int V, int E> int bwd_rows(BwdP
     P.parts = (int)std::max<long long>(1, std::min<long long>((P.M + teams - 1) / teams, std::min(dev.sm_count, kPartBlocks)));
     const int parties = threads / std::max(P.T, 32);
     const size_t sums = parties > 1 && P.part ? parties * 2 * sizeof(float) * P.C : 0;
-    const size_t smem = V > 1 ? std::max<size_t>(sums, (size_t)kBwdStages * threads * bwd_stage_bytes<TD, TX, E>()) : sums;
+    const size_t smem = V > 1 ? std::max<size_t>(sums, (size_t)bwd_stages<TD, TX>() * threads * bwd_stage_bytes<TD, TX, E>()) : sums;
     switch (P.T) {
         case 4: return launch_bwd_rows<TD, TX, TO, V, E, V == 1 ? 0 : 4>(P, threads, smem, dev, s);
         case 8: return launch_bwd_rows<TD, TX, TO, V, E, V == 1 ? 0 : 8>(P, threads, smem, dev, s);
@@ -1205,10 +1213,10 @@ template <typename TD, typename TX, typename TO, int V, int E> int bwd_rows(BwdP
 }
 template <typename TD, typename TX, typename TO, int V> int bwd(BwdParams &P, float *dgamma, float *dbeta, const twn_device_info &dev, cudaStream_t s)
 {
-    constexpr int E = V == 8 && sizeof(TD) == 2 && sizeof(TX) == 2 ? 16 : 8;
+    constexpr int E = V > 1 ? 16 : 8;
     int rc = TWN_OK;
     bool served = false;
-    if constexpr (V > 1) served = P.C > 2048 && P.M * P.C >= kRingElements && bwd_ring<TD, TX, TO, V, 32>(P, dev, s, rc);
+    if constexpr (V > 1) served = P.bulk && P.C > kBwdThreads * E && P.M * P.C >= kRingElements && bwd_ring<TD, TX, TO, V, 32>(P, dev, s, rc);
     if (served) {
         if (rc != TWN_OK) return rc;
     } else if (V == 1 && P.C <= kBwdThreads * 16 && (P.C > kBwdThreads * E || P.M * P.C >= 1 << 23)) {
@@ -1229,14 +1237,18 @@ template <typename TD, typename TX, typename TO, int V> int bwd(BwdParams &P, fl
         cfg.stream = s;
         TWN_CUDA_OK(cudaLaunchKernelEx(&cfg, norm_bwd_stripe_kernel<TD, TX, TO, V>, P));
     }
-    if (P.part)
-        TWN_CUDA_OK(twn_launch_small(norm_fold_kernel, (int)((2 * P.C + 31) / 32), 32 * kRuns, 0, s, P.part, P.parts, P.C, dgamma, dbeta));
+    if (P.part == nullptr) return TWN_OK;
+    auto fold = [&](auto kernel, int W) {
+        return twn_launch_small(kernel, (int)((2 * P.C + 32 * W - 1) / (32 * W)), 32 * kRuns, 0, s, P.part, P.parts, P.C, dgamma, dbeta);
+    };
+    const long long narrow = 16 * kPdlBlocks;            // channels whose columns, one a thread, are that many blocks
+    TWN_CUDA_OK(P.C <= narrow || P.C % 2 ? fold(norm_fold_kernel<1>, 1) : P.C <= 2 * narrow || P.C % 4 ? fold(norm_fold_kernel<2>, 2) : fold(norm_fold_kernel<4>, 4));
     return TWN_OK;
 }
 template <typename TD, typename TX, typename TO>
 int bwd_any(BwdParams &P, bool vec, float *dgamma, float *dbeta, const twn_device_info &dev, cudaStream_t s)
 {
-    constexpr int V = sizeof(TD) == 4 && sizeof(TX) == 4 ? 4 : 8;
+    constexpr int V = sizeof(TD) == 4 || sizeof(TX) == 4 ? 4 : 8;
     return vec ? bwd<TD, TX, TO, V>(P, dgamma, dbeta, dev, s) : bwd<TD, TX, TO, 1>(P, dgamma, dbeta, dev, s);
 }
 
@@ -1302,9 +1314,11 @@ extern "C" int twn_layer_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy
     P.part = sums ? static_cast<float *>(workspace) : nullptr;
     P.row_sums = reinterpret_cast<float *>(static_cast<char *>(workspace) + part_bytes(C));
     P.lddy = lddy; P.ldx = ldx; P.lddx = lddx; P.M = M; P.C = C;
-    const int V = dy_dtype == TWN_F32 && x_dtype == TWN_F32 ? 4 : 8;
+    // vectors of 16 bytes of the wider type, so that a warp's copies are next to each other
+    const int V = dy_dtype == TWN_F32 || x_dtype == TWN_F32 ? 4 : 8;
     const bool vec = vector_rows(dY, dy_dtype, lddy, V) && vector_rows(X, x_dtype, ldx, V) && (!dX || vector_rows(dX, dx_dtype, lddx, V)) && (!residual || vector_rows(residual, dx_dtype, lddx, V)) &&
                      C % V == 0 && twn_aligned(gamma, 16);
+    P.bulk = C % 8 == 0 && vector_rows(dY, dy_dtype, lddy, 8) && vector_rows(X, x_dtype, ldx, 8);
     cudaStream_t s = twn_cu(stream);
     const int key = (dy_dtype == TWN_BF16) * 4 + (x_dtype == TWN_BF16) * 2 + (dX && dx_dtype == TWN_BF16);
     switch (key) {
