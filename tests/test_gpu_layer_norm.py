@@ -153,8 +153,10 @@ def _bwd_reference(dy, x, gamma, mean, rstd):
     return xh, g, (g - c0 - xh * c1) * rstd.double()[:, None], (dy * xh).sum(0), dy.sum(0)
 
 
-def _check_bwd(M, C, dt, xt, ot, lddy, ldx, lddx, gamma=True, offset=0, seed=11, sums=True, data=True, in_place=None, residual=None):
+def _check_bwd(M, C, dt, xt, ot, lddy, ldx, lddx, gamma=True, offset=0, seed=11, sums=True, data=True, in_place=None, residual=None, shift=0.0):
     x, xbuf = _rows(seed, M, C, ldx, xt, offset)
+    if shift:
+        x.add_(shift)
     dy, dbuf = _rows(seed + 5, M, C, lddy, dt, offset)
     ga = 1 + 0.3 * _normal(seed + 2, C) if gamma else None
     _, m, r, _ = _fwd_reference(x, None, None, EPS)
@@ -199,6 +201,20 @@ def test_backward(M, C, dt, xt, ot):
 @pytest.mark.parametrize("dt,xt,ot", [(F, F, F), (B, B, B), (B, F, B), (F, B, F)])
 def test_backward_large(M, C, dt, xt, ot):
     _check_bwd(M, C, dt, xt, ot, C, C + 8, C + 24, gamma=C % 3 > 0)
+
+
+@pytest.mark.parametrize("M,C", [(200, 12004), (90, 12004), (300, 8188), (5000, 212), (70, 16384), (40, 32768)])
+@pytest.mark.parametrize("dt,xt,ot", [(F, F, F), (B, B, B), (B, F, B), (F, B, F)])
+def test_backward_rows_of_eight_bytes(M, C, dt, xt, ot):
+    """C % 8 == 4: rows of bf16 lie on 8-byte boundaries, those of fp32 on 16; and rows beside them that fill their threads."""
+    _check_bwd(M, C, dt, xt, ot, C, C + 4, C + 12)
+
+
+@pytest.mark.parametrize("dt,xt,ot", [(F, F, F), (B, F, F)])
+@pytest.mark.parametrize("M,C", [(700, 1001), (700, 1024), (80, 16384)])
+def test_backward_rows_far_from_zero(M, C, dt, xt, ot):
+    """Rows at 300 with a deviation of 1.5: X - mean is off by what the fp32 mean is off, which the bound counts."""
+    _check_bwd(M, C, dt, xt, ot, C, C, C, shift=300.0)
 
 
 @pytest.mark.parametrize("M,C", [(3, 20), (50, 1000), (41, 1001), (300, 4096), (70, 16384), (9000, 1001), (20, 20000), (30, 9001)])

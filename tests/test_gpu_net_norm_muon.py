@@ -146,6 +146,26 @@ def test_a_captured_step_gives_the_bits_of_a_direct_one():
         assert torch.equal(a.extra["W"], b.extra["W"]) and torch.equal(a.extra["packed"], b.extra["packed"])
 
 
+@pytest.mark.parametrize("key", ["gamma", "beta", "mean", "rstd", "dgamma", "dbeta", "ws"])
+def test_a_norm_s_buffer_may_be_replaced_between_passes(key):
+    dlogits = torch.from_numpy(dg.draw(9, "dl", 24 * 16, "normal")).cuda().view(24, 16).to(torch.bfloat16)
+
+    def results(net):
+        net.train_step(dlogits)
+        torch.cuda.synchronize()
+        return [net.act["fc"].clone()] + [L.extra["dW"].clone() for L in net.layers.values()] + [net.norm[f"{n}.d{k}"].clone()
+                                                                                                 for n in ("n0", "n1", "last") for k in ("gamma", "beta")]
+
+    net = _net(optimizer=None)
+    want = results(net)
+    old = net.norm["n1." + key]
+    net.norm["n1." + key] = old.clone()
+    old.view(torch.uint8).fill_(255)
+    for a, b in zip(want, results(net)):
+        assert torch.equal(a, b)
+    assert bool((old.view(torch.uint8) == 255).all())
+
+
 def test_inference_and_an_unknown_rule():
     a, b = _net(train=False, optimizer=None), _net(train=True, optimizer=None)
     for net in (a, b):
