@@ -13,15 +13,18 @@ struct FwdParams {
     int T;
 };
 
-// One row per team, in registers.  C <= T * E.  A team of more than a warp is a block.
-template <typename TX, typename TY, int V, int E, int TT>
-__global__ void __launch_bounds__(TT > 32 ? TT : TT == 32 || E < 16 ? 128 : 1024, TT <= 32 || V == 1 ? 1 : 1024 / (TT ? TT : 1)) norm_fwd_kernel(const __grid_constant__ FwdParams P)
+constexpr int kFwdThreads = 512;             // of a block, but for teams of 1024
+
+// One row per team, in registers.  C <= T * E.  MANY: teams of more than a warp share a block, with a named barrier each; the number of a barrier that is not
+// known at compile time takes all sixteen, and fewer small blocks fit an SM (10000 rows of 1001: 46 us for 22.7 of a block a team).
+template <typename TX, typename TY, int V, int E, int TT, bool MANY>
+__global__ void __launch_bounds__(MANY || TT <= 32 ? kFwdThreads : TT, TT <= 32 || V == 1 ? 1 : MANY ? 2 : 1024 / (TT ? TT : 1)) norm_fwd_kernel(const __grid_constant__ FwdParams P)
 {
     constexpr int NV = E / V, P2 = E / 2;
     __shared__ __align__(16) float red[2][32][2];
     unsigned int turn = 0;
     const int T = TT ? TT : P.T, t = threadIdx.x & (T - 1), C = (int)P.C;
-    const int teams = blockDim.x / T, team = threadIdx.x / T;
+    const int teams = blockDim.x / T, team = threadIdx.x / T, barrier = MANY ? team + 1 : 0;
     const float inv = 1.0f / (float)C;
     const Columns<V, TT> col{T, t, C};
     pdl_begin();
@@ -43,8 +46,8 @@ __global__ void __launch_bounds__(TT > 32 ? TT : TT == 32 || E < 16 ? 128 : 1024
             }
         }
         float s[1] = {sum2(s2)};
-        if constexpr (TT > 0) team_sum<TT>(s, red, turn, 0);
-        else team_sum(s, T, red, turn, 0);
+        if constexpr (TT > 0) team_sum<TT>(s, red, turn, barrier);
+        else team_sum(s, T, red, turn, barrier);
         const float mean = s[0] * inv;
         const two_f32 minus = two(-mean, -mean);
 #pragma unroll
@@ -67,8 +70,8 @@ __global__ void __launch_bounds__(TT > 32 ? TT : TT == 32 || E < 16 ? 128 : 1024
 #pragma unroll
         for (int i = 0; i < P2; ++i) q2 = fma2(d[i], d[i], q2);
         float q[1] = {sum2(q2)};
-        if constexpr (TT > 0) team_sum<TT>(q, red, turn, 0);
-        else team_sum(q, T, red, turn, 0);
+        if constexpr (TT > 0) team_sum<TT>(q, red, turn, barrier);
+        else team_sum(q, T, red, turn, barrier);
         const float rstd = rsqrtf(fmaf(q[0], inv, P.eps));
         if (!live) continue;
         const two_f32 scale = two(rstd, rstd);
@@ -266,9 +269,19 @@ __global__ void __launch_bounds__(1024) norm_fwd_long_kernel(const __grid_consta
 template <typename TX, typename TY, int V, int E, int TT> int launch_fwd(FwdParams &P, int T, cudaStream_t s)
 {
     P.T = T;
-    const int block = T > 32 ? T : 128, teams = block / T;
-    const long long grid = std::min<long long>((P.M + teams - 1) / teams, 148ll * 64);
-    TWN_CUDA_OK(twn_launch_small(norm_fwd_kernel<TX, TY, V, E, TT>, (int)grid, block, 0, s, P));
+    int teams = T > 32 ? 1 : 128 / T;
+    // Up to two rows for every team of a block an SM: a launch of that many blocks may start early.  Above, more and smaller blocks balance better.
+    const int most = T > kFwdThreads ? 1 : kFwdThreads / T;
+    if (P.M <= 2ll * kPdlBlocks * most) {
+        teams = (int)std::min<long long>((P.M + kPdlBlocks - 1) / kPdlBlocks, most);
+        teams = (teams * T + 31) / 32 * 32 / T;              // whole warps
+    }
+    const int block = teams * T;
+    const long long grid = std::min<long long>((P.M + teams - 1) / teams, 2ll * kPdlBlocks * most >= P.M ? kPdlBlocks : 148ll * 64);
+    if (TT > 32 && TT < kFwdThreads && teams > 1)
+        TWN_CUDA_OK(twn_launch_small(norm_fwd_kernel<TX, TY, V, E, TT, (TT > 32 && TT < kFwdThreads)>, (int)grid, block, 0, s, P));
+    else
+        TWN_CUDA_OK(twn_launch_small(norm_fwd_kernel<TX, TY, V, E, TT, false>, (int)grid, block, 0, s, P));
     return TWN_OK;
 }
 template <typename TX, typename TY, int V, int E, int TT> int launch_fwd_ring(const FwdParams &P, const RingShape &r, const twn_device_info &dev, cudaStream_t s)
