@@ -311,11 +311,18 @@ template <typename TX, typename TY, int V, int E> bool fwd_ring(FwdParams &P, co
     }
     return true;
 }
+// Rows that the register kernel takes with one block an SM, one or two for a team, it takes faster (two of more than 8192 elements it does not):
+// 1030 x 1024 bf16 2.7 us, 4.6 through a ring, 500 x 4096 4.3 and 5.1, 148 x 8000 3.2 and 8.4, 148 x 16384 4.2 and 5.7; 2600 x 1024 6.2 and 4.6.
+bool few_rows(const FwdParams &P)
+{
+    if (P.C > 8192) return P.C <= 16384 && P.M <= kPdlBlocks;
+    return P.M <= 2ll * kPdlBlocks * (kFwdThreads / team_for(P.C, 16, 32, 512));
+}
 template <typename TX, typename TY, int V> int fwd(FwdParams &P, const twn_device_info &dev, cudaStream_t s)
 {
     if constexpr (V > 1) {
         int rc = TWN_OK;
-        if (P.C > 256 && P.M * P.C >= kRingElements &&
+        if (P.C > 256 && P.M * P.C >= kRingElements && !few_rows(P) &&
             (P.C <= 512 ? fwd_ring<TX, TY, V, 16>(P, dev, s, rc)
              : P.C <= 1024 ? fwd_ring<TX, TY, V, 32>(P, dev, s, rc)
                            : fwd_ring<TX, TY, V, 64>(P, dev, s, rc)))

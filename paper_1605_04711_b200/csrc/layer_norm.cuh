@@ -270,9 +270,8 @@ template <typename T, int V, int TT> __device__ __forceinline__ void add_vector(
 }
 
 // ---- rows through shared memory ---------------------------------------------------------------------------------------------
-// Large tensors of aligned rows.  With 16 elements a thread, all of them in registers, a row of 4096 took 31 instructions an element,
-// most of them the fixed part of a row: two sums, the barriers, the root, the addresses; with more, few rows fit the registers, and
-// too little is on its way.  Here rows come by bulk copies into a ring in shared memory, up to 192 KB an SM on their way, for threads
+// Large tensors of aligned rows.  With 16 elements a thread, all of them in registers, most instructions are the fixed part of a row: two
+// sums, the barriers, the root, the addresses; with more, few rows fit the registers, and too little is on its way.  Here rows come by bulk copies into a ring in shared memory, up to 192 KB an SM on their way, for threads
 // of up to 64 elements.
 constexpr int kMaxRing = 8, kMaxTeams = 32;
 // Of the 227 KB that a block may have; 2.6 KB are barriers and sums.  Forward with 200 KB, two stages at 16384 x 4096 instead of three, took 48.0 us for 46.6;

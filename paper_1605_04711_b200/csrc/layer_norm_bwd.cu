@@ -19,7 +19,7 @@ constexpr int kBwdThreads = 512;
 
 // The column sums of a block's `parties` (teams, or warps of several teams), of which this thread belongs to number `me`, to `out`, [2][C]; they are added in
 // their order.  cols: [parties][2][C] in shared memory where there are several (with one after the other adding to one [2][C], the sixteen
-// warps of a block took 5 of 29 us for rows of 64).
+// warps of a block took 10 of 29 us for rows of 64).
 template <int V, int E, typename Col>
 __device__ __forceinline__ void join_sums(const float (&g)[E], const float (&b)[E], const Col &col, bool mine, int me, int parties, float *cols, float *out)
 {

@@ -95,6 +95,14 @@ def test_forward_large(M, C, xt, yt):
     _check_fwd(M, C, xt, yt, C, C + 24, gamma=C % 3 > 0, beta=C % 5 > 0)
 
 
+@pytest.mark.parametrize("M,C", [(148, 1001), (149, 1001), (296, 4001), (297, 4001), (2368, 1001), (2369, 1024), (1184, 2048), (1185, 2048), (4736, 512), (4737, 512),
+                                 (149, 8192), (297, 8192), (148, 16384), (149, 16384), (296, 16383), (5000, 33), (4737, 500), (200, 40), (19000, 60)])
+@pytest.mark.parametrize("xt,yt", [(F, F), (B, B), (F, B)])
+def test_forward_where_the_blocks_change(M, C, xt, yt):
+    """The most rows that one launch of a block an SM takes, for its teams' sizes, and one more."""
+    _check_fwd(M, C, xt, yt, C, C)
+
+
 @pytest.mark.parametrize("ldx,ldy,offset", [(1008, 1024, 0), (1001, 1000, 0), (1000, 1000, 1), (1000, 1003, 8), (1024, 1024, 0)])
 @pytest.mark.parametrize("xt,yt", [(F, F), (B, B), (F, B), (B, F)])
 def test_forward_pitches_and_offsets(ldx, ldy, offset, xt, yt):
