@@ -17,7 +17,7 @@
 // 0.02 in five; from about eight steps on it would run away, so more than five steps go the other way (orthogonalize.cu).
 //
 // Range.  The Gram matrix is summed before the norm, its trace, is known.  Where that leaves the range in which fp32 keeps its
-// digits, it is summed again from G times a power of two.
+// digits, it is summed again from G times a power of two, that of the trace where it says how large G is (second_scale).
 //
 // What bounds it: 14 dependent products of 128 x 128 x 128 (three MMA passes, 0.8 us each) with the elements' way through registers
 // between them (about as long), two passes over the matrix by eight SMs, and four cluster barriers.
@@ -252,6 +252,18 @@ __device__ __forceinline__ void tmem_row16(uint32_t taddr, float (&v)[16])
     for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(w[j]);
 }
 
+// What G is multiplied by before its Gram matrix is summed again, the trace of the first sum being finite or not, at most 1e30 or not.
+// From 1e-30 on (of up to 2^20 squares those that fell below fp32, 1e-38 each, are less than a hundredth) and where it is finite the trace
+// gives it: 2^-h for a trace of 2^2h, 1 to 4 the second time.  Below, G has a norm under 1.1e-15 and 2^100 brings its trace, 2e-90 at
+// least for one denormal element, to 3e-30 at least and 2e30 at most; above, its elements are 1e16 at least in all, and 2^-100 leaves
+// 2e-22 to 1e23.  (2^100 for every trace below 1e-20 took a row's 2.1e-22 beyond fp32.)
+__device__ __forceinline__ float second_scale(double trace)
+{
+    if (!isfinite(trace)) return 0x1p-100f;
+    if (trace < 1e-30) return 0x1p100f;
+    return (float)ldexp(1.0, -(ilogb(trace) >> 1));
+}
+
 template <int KIND> __global__ void __launch_bounds__(kThreads, 1) ns_small_kernel(const __grid_constant__ NsSmallParams P)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -405,7 +417,7 @@ template <int KIND> __global__ void __launch_bounds__(kThreads, 1) ns_small_kern
                 const bool finite = isfinite(trace);
                 const bool far = !finite || trace > 1e30 || trace < 1e-20;
                 sm->again = attempt == 0 && far;
-                sm->pre = !finite || trace > 1.0 ? 0x1p-100f : 0x1p100f;
+                sm->pre = second_scale(trace);
                 const double scaled = sqrt(trace), least = (double)P.eps * (double)pre;
                 sm->factor = !finite ? __uint_as_float(0x7FC00000u) : trace == 0.0 ? 0.0f : (float)(1.0 / (scaled > least ? scaled : least));
                 if (!sm->again && !finite && P.status) atomicMin(P.status, (int)TWN_ERR_NONFINITE);
