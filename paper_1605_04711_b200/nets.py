@@ -123,6 +123,37 @@ class Layer(_Counted):
         return self.B * self.Ho * self.Wo * self.K * self.Cout
 
 
+def backward_order(ops, is_shortcut):
+    """The operations of a network in the order of its backward pass: the last first, but for projection shortcuts.
+
+    A projection shortcut shares its input with what begins its block.  Its backward pass is taken after that of the block's first
+    convolution: the dense gradient is written first, and the strided shortcut then adds into it in place, which lets
+    twn_conv2d_bwd_data skip the residue classes its single tap never reaches.  Where no convolution that reads the same input is still to come
+    (the block begins with a layer norm or a pooling), it is taken after the last that is; and in its own place where none is: before
+    the layer that made the input in every case, which needs the whole gradient."""
+    order, put_off = [], {}                  # put_off: by the index of the operation that they are taken after
+    for i in range(len(ops) - 1, -1, -1):
+        op = ops[i]
+        if op[0] == "layer" and is_shortcut(op[1]):
+            src = op[1].src
+            layers, others = [], []          # readers that are still to come
+            for j in range(i - 1, -1, -1):
+                if ops[j][0] != "layer":
+                    if ops[j][2] == src:
+                        others.append(j)
+                elif not is_shortcut(ops[j][1]):
+                    if ops[j][1].src == src:
+                        layers.append(j)
+                    elif ops[j][1].residual == src:
+                        others.append(j)
+            if layers or others:
+                put_off.setdefault(layers[0] if layers else others[-1], []).append(op)
+                continue
+        order.append(op)
+        order.extend(put_off.pop(i, []))
+    return order
+
+
 class TernaryNet(_Counted):
     """A chain of ternary conv / FC layers with pooling glue, all buffers preallocated.  A buffer or parameter may be
     replaced between two passes (act, aux, grad, a layer's extra, ...); the next pass uses the new one."""
@@ -466,26 +497,14 @@ class TernaryNet(_Counted):
                 return None
             return P if consumers.get(P.name) == [L] else None
 
-        # A projection shortcut (a layer read only as the residual input of another layer) shares its input with
-        # the first convolution of its block.  Its backward pass is taken after that convolution's: the dense
-        # gradient is written first, and the strided shortcut then adds into it in place, which lets
-        # twn_conv2d_bwd_data skip the residue classes its single tap never reaches.
+        # A projection shortcut is a layer read only as the residual input of another layer.
         def is_shortcut(L):
             if L.relu or L.residual or L.fold or L.small_cin or L.src == "input":
                 return False
             users = consumers.get(L.name, [])
             return users == [None]
-        order, deferred = [], {}
-        for op in reversed(self.ops):
-            if op[0] == "layer" and is_shortcut(op[1]):
-                deferred[op[1].src] = op
-                continue
-            order.append(op)
-            if op[0] == "layer" and op[1].src in deferred:
-                order.append(deferred.pop(op[1].src))
-        order.extend(deferred.values())
 
-        for op in order:
+        for op in backward_order(self.ops, is_shortcut):
             kind = op[0]
             if kind == "layer":
                 L: Layer = op[1]
