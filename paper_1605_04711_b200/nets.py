@@ -277,6 +277,14 @@ class TernaryNet(_Counted):
                 self.act[name] = torch.zeros_like(x, dtype=torch.bfloat16)
                 new = {"gamma": torch.ones(C, device="cuda"), "beta": torch.zeros(C, device="cuda")}
                 if self.train:
+                    if x.dtype != torch.bfloat16:
+                        # a layer's output in fp32 (or a view of one), whose gradient is bf16 like any other
+                        made_by = src
+                        while made_by not in self.layers:
+                            made_by = next(o[2] for o in self.ops if o[0] == "flatten" and o[1] == made_by)
+                        if self.layers[made_by].relu:
+                            raise NotImplementedError("the gate of a ReLU is read from a bf16 activation")
+                        self.grad[src] = torch.zeros_like(x, dtype=torch.bfloat16)
                     new |= {k: torch.zeros(M, device="cuda") for k in ("mean", "rstd")}
                     new |= {k: torch.zeros(C, device="cuda") for k in ("dgamma", "dbeta")}
                     new["ws"] = torch.empty(twn.layer_norm_bwd_workspace_bytes(M, C), dtype=torch.uint8, device="cuda")

@@ -56,8 +56,18 @@ def _layers_before():
             _layer("down", "up", 128, C, residual="proj"), *_tail("down")]
 
 
+def _wide_source():
+    """A norm of a layer whose output is kept in fp32."""
+    return [_layer("x0", "input", 64, C, relu=True), _layer("x", "x0", C, C, out_f32=True), ("layernorm", "n", "x"), _layer("up", "n", C, C, relu=True), *_tail("up")]
+
+
+def _flat_wide_source():
+    return [_layer("x0", "input", 64, C, relu=True), _layer("x", "x0", C, 8, out_f32=True), ("flatten", "f", "x"), ("layernorm", "n", "f"),
+            _layer("fc", "n", 128, 16, H=1, out_f32=True)]
+
+
 NETS = {"norm": _norm_block(False), "norm, projection first": _norm_block(True), "pool": _pool_block(), "two projections": _two_projections(),
-        "projection alone": _projection_alone(), "layers, projection first": _layers_before()}
+        "projection alone": _projection_alone(), "layers, projection first": _layers_before(), "fp32 source": _wide_source(), "fp32 source, flat": _flat_wide_source()}
 
 
 def reference(net, x, T, norm, dlogits):
@@ -80,6 +90,8 @@ def reference(net, x, T, norm, dlogits):
             v, n = act[op[2]], net.act[op[2]].double()
             split = lambda t: t.unfold(1, 2, 2).unfold(2, 2, 2).flatten(4)  # noqa: E731
             act[op[1]] = split(v).gather(4, split(n).argmax(4, keepdim=True)).squeeze(4)
+        elif op[0] == "flatten":
+            act[op[1]] = act[op[2]].flatten(1)[:, None, None]
         else:
             act[op[1]] = act[op[2]].mean((1, 2), keepdim=True)
     y = act[net.ops[-1][1].name]
@@ -92,7 +104,7 @@ def test_every_gradient_is_that_of_64_bits(which):
     net = nets.TernaryNet("shortcuts", B, (4, 4, 64), NETS[which], seed=3, train=True)
     norms = [op[1] for op in net.ops if op[0] == "layernorm"]
     for i, name in enumerate(norms):
-        net.norm[name + ".gamma"].copy_(torch.from_numpy(1 + dg.draw(5, f"g{i}", C, "normal", 0.0, 0.2)).cuda())
+        net.norm[name + ".gamma"].copy_(torch.from_numpy(1 + dg.draw(5, f"g{i}", net.norm[name + ".gamma"].numel(), "normal", 0.0, 0.2)).cuda())
     net.set_input(dg.draw_bf16(7, "x", B * 16 * 64, "normal"))
     dlogits = torch.from_numpy(dg.draw(9, "dl", B * 16, "normal")).cuda().view(B, 16).to(torch.bfloat16)
     for _ in range(2):
@@ -106,3 +118,13 @@ def test_every_gradient_is_that_of_64_bits(which):
     for name in norms:
         for k in ("gamma", "beta"):
             _near(net.norm[f"{name}.d{k}"], dn[f"{name}.{k}"], 22 * 2.0 ** -8)
+
+
+def test_a_relu_of_an_fp32_output_is_not_trained_through():
+    """The gate of a ReLU is read from bf16."""
+    ops = [_layer("x", "input", 64, C, out_f32=True, relu=True), ("layernorm", "n", "x"), *_tail("n")]
+    flat = [_layer("x", "input", 64, 8, out_f32=True, relu=True), ("flatten", "f", "x"), ("layernorm", "n", "f"), _layer("fc", "n", 128, 16, H=1, out_f32=True)]
+    for o in (ops, flat):
+        with pytest.raises(NotImplementedError):
+            nets.TernaryNet("gate", B, (4, 4, 64), o, train=True)
+        nets.TernaryNet("gate", B, (4, 4, 64), o)
