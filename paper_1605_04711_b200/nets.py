@@ -171,7 +171,9 @@ class TernaryNet(_Counted):
         every layer's filters as the rows of a matrix.
 
         An operation ("layernorm", name, src) normalises every pixel of src over its channels.  Its gamma and beta, and
-        after a backward pass their gradients, are norm[name + ".gamma"], ".beta", ".dgamma" and ".dbeta"."""
+        after a backward pass their gradients, are norm[name + ".gamma"], ".beta", ".dgamma" and ".dbeta".  A step's update is that of
+        the master weights alone, under either rule: gamma and beta stay as they are, like a layer's scale and shift, and are the
+        caller's to update from the gradients beside them."""
         self._changes = _Changes()
         self.name, self.B, self.in_shape, self.ops = name, batch, in_shape, ops
         self.seed, self.delta_factor, self.train = seed, delta_factor, train

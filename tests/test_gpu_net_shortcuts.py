@@ -128,3 +128,16 @@ def test_a_relu_of_an_fp32_output_is_not_trained_through():
         with pytest.raises(NotImplementedError):
             nets.TernaryNet("gate", B, (4, 4, 64), o, train=True)
         nets.TernaryNet("gate", B, (4, 4, 64), o)
+
+
+@pytest.mark.parametrize("rule", ["sgd", "muon"])
+def test_the_norms_parameters_are_the_caller_s(rule):
+    """An update moves the weights; gamma and beta stay, with their gradients beside them."""
+    net = nets.TernaryNet("kept", B, (4, 4, 64), _norm_block(False), seed=3, train=True, optimizer={"rule": rule, "lr": 0.02, "momentum": 0.9, "weight_decay": 0.0})
+    net.set_input(dg.draw_bf16(7, "x", B * 16 * 64, "normal"))
+    dlogits = torch.from_numpy(dg.draw(9, "dl", B * 16, "normal")).cuda().view(B, 16).to(torch.bfloat16)
+    net.train_step(dlogits)
+    torch.cuda.synchronize()
+    for name in ("n", "last"):
+        assert bool((net.norm[name + ".gamma"] == 1).all()) and bool((net.norm[name + ".beta"] == 0).all())
+        assert float(net.norm[name + ".dgamma"].abs().max()) > 0 and float(net.norm[name + ".dbeta"].abs().max()) > 0
