@@ -270,7 +270,7 @@ int twn_ternarize_codes_batch(const twn_ternarize_item_t *items, int count, void
  *              the device must not share it.
  *   dev_status optional device int32, zero before the call: TWN_ERR_NONFINITE where a G holds a NaN or an infinity (its O is
  *              then NaNs, the other matrices are unaffected), TWN_ERR_TIMEOUT as in twn_gemm.
- * fp16 products, fp32 sums; X is carried in 22 bits and the diagonals of A and of b A + c A^2 in fp32, so five steps are within
+ * fp16 products, fp32 sums; X is carried in 22 bits (of a G far below eps too) and the diagonals of A and of b A + c A^2 in fp32, so five steps are within
  * 1e-3 (2-norm, relative) of 64-bit arithmetic for matrices of independent elements, and within 4e-3 for low rank (one included)
  * and for singular values that fall off.  Where blocks of equal elements make the roundings of the products align it can be
  * more (up to 1e-2 seen in 150 such matrices, 1.3e-3 in the middle).  A call of small matrices alone (sides of at most 128 and

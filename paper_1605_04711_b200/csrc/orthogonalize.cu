@@ -14,7 +14,11 @@
 //   X_i  = (a + beta_i) X_i + (B' X)_i                      (A' = A without its diagonal alpha, B' likewise)
 // and alpha_i is the sum of squares of a row of X in full, not of its upper half: an identity, whose roundings all
 // align, is served to 1e-6 (4e-3 with the product's diagonal).  Five steps, relative to 64 bits: 5e-4 to 8e-4 for full spectra, 1e-3
-// for a matrix of rank 32, 2e-3 for rank one, where a plain bf16 iteration is off by 1e-2, 0.2 and 1.  X starts at 256 times its value (its elements are near 1/sqrt(m n)), which the first step takes out.
+// for a matrix of rank 32, 2e-3 for rank one, where a plain bf16 iteration is off by 1e-2, 0.2 and 1.
+//
+// Range.  X is held times a power of two (scale_of): 256 at the start, where its elements are near 1/sqrt(m n), and 1 from the first step
+// on.  Where G is smaller than eps, d = |G|_F / eps times, X stays small until the steps have grown it, each by a at most: there it is
+// held at 64 to 256 times the bound d a^k of its norm, so that it keeps its 22 bits however small d is.
 //
 // Layout.  X, A and B live in the workspace as blocks of 64x64 fp16 (8 KB), in the 128-byte swizzle that the tensor core
 // wants, the row blocks of a column block one after the other.  A tile of 128 rows by 64 columns is then 16 KB in a row, one
@@ -56,6 +60,8 @@ constexpr int kMaxSplit = 4;                 // blocks that share a tile's reduc
 constexpr int kMaxParts = 512;               // of a matrix's sum of squares
 constexpr long long kPartElements = 8192;
 constexpr int kSweepBlock = 256;
+constexpr int kMaxSteps = 32;
+constexpr size_t kScaleBytes = 8 * kMaxSteps;
 
 enum { kGram = 0, kSquare = 1, kApply = 2 };
 
@@ -66,6 +72,7 @@ struct NsItem {
     void *O;
     uint16_t *x[2], *lo, *A, *B; // blocks
     float *alpha, *beta;         // diagonals
+    float2 *scale;               // what the sums of a step's A, and of its B X, are multiplied by
     float *squares;              // [cb][64 rb]: sums of squares of 64 elements of a row of X
     double *part;                // sums of squares
     long long count;             // elements
@@ -79,7 +86,7 @@ struct NsItem {
 
 struct NsParams {
     NsItem item[kMaxItems];
-    int count, units, step, last;
+    int count, units, step, last, steps;
     float momentum, eps;
     int look_ahead;
     int32_t *status;
@@ -230,6 +237,15 @@ __device__ __forceinline__ float row_squares(const float (&f)[8])
     return q;
 }
 
+// The power of two that the X before a step is held times, for |G|_F / eps = d below 1 and 1 at eps or above: see the top.
+__device__ __forceinline__ float scale_of(double d, int step, int steps)
+{
+    if (step == steps) return 1.0f;
+    if (d >= 1.0) return step == 0 ? kStart : 1.0f;
+    for (int k = 0; k < step; ++k) d *= (double)kA;
+    return d > 0.0 ? (float)ldexp(1.0, min(126, max(0, 7 - ilogb(d)))) : 1.0f;
+}
+
 // X of the first step, a block of 64x64 at a time: normalised, split into two fp16 numbers, padded with zeros.
 __global__ void __launch_bounds__(kSweepBlock) ns_start_kernel(const __grid_constant__ NsParams P)
 {
@@ -248,9 +264,14 @@ __global__ void __launch_bounds__(kSweepBlock) ns_start_kernel(const __grid_cons
             for (int p = threadIdx.x; p < it.parts; p += kSweepBlock) s += it.part[p];
             const double norm = sqrt(block_sum(s, red));
             if (b == 0 && threadIdx.x == 0 && P.status && !isfinite(norm)) atomicMin(P.status, (int)TWN_ERR_NONFINITE);
+            const double d = norm < (double)P.eps ? norm / (double)P.eps : 1.0;
+            if (b == 0 && threadIdx.x < P.steps) {
+                const float inverse = 1.0f / scale_of(d, threadIdx.x, P.steps);
+                it.scale[threadIdx.x] = make_float2(inverse * inverse, inverse * scale_of(d, threadIdx.x + 1, P.steps));
+            }
             // in two factors, so that neither leaves the range of fp32
-            pre = norm > 1e18 ? 0x1p-100f : 1.0f;
-            factor = norm == 0.0 ? 0.0f : (float)((double)kStart / (fmax(norm, (double)P.eps) * (double)pre));
+            pre = norm > 1e18 ? 0x1p-100f : norm < 1e-18 ? 0x1p100f : 1.0f;
+            factor = norm == 0.0 ? 0.0f : (float)((double)scale_of(d, 0, P.steps) / (fmax(norm, (double)P.eps) * (double)pre));
             nan = norm == norm ? 0.0f : __uint_as_float(0x7FC00000u);      // fmax drops a NaN
             have = t;
         }
@@ -424,7 +445,8 @@ __device__ __forceinline__ size_t mirror_piece(const NsItem &it, int r0, int c0)
 // before the sums are there.
 template <int PHASE> struct Ahead;
 template <> struct Ahead<kGram> {
-    __device__ __forceinline__ void load(const NsItem &, const NsParams &, int, int) {}
+    float unscale;
+    __device__ __forceinline__ void load(const NsItem &it, const NsParams &P, int, int) { unscale = it.scale[P.step].x; }
 };
 template <> struct Ahead<kSquare> {
     uint4 a[8];
@@ -445,7 +467,7 @@ template <> struct Ahead<kSquare> {
 };
 template <> struct Ahead<kApply> {
     uint4 hi[4], lo[4];          // of the first four units
-    float row[8];
+    float row[8], unscale;
     __device__ __forceinline__ void load4(const NsItem &it, const NsParams &P, int r0, int c0, int u0)
     {
         const uint16_t *const x = it.x[P.step & 1], *const rest = it.lo;
@@ -459,6 +481,7 @@ template <> struct Ahead<kApply> {
     __device__ __forceinline__ void load(const NsItem &it, const NsParams &P, int r0, int c0)
     {
         load4(it, P, r0, c0, 0);
+        unscale = it.scale[P.step].y;
 #pragma unroll
         for (int u = 0; u < 8; ++u) row[u] = (it.beta + r0 + ((threadIdx.x & 31) >> 3))[4 * u];
     }
@@ -470,7 +493,8 @@ __device__ __forceinline__ void finish_symmetric(const NsItem &it, const NsParam
 {
     const int lane = threadIdx.x & 31;
     const bool diagonal = r0 >= c0 && r0 < c0 + 64;
-    const float unscale = P.step == 0 ? 1.0f / (kStart * kStart) : 1.0f;
+    float unscale = 1.0f;
+    if constexpr (PHASE == kGram) unscale = ahead.unscale;
     uint16_t *const to = PHASE == kGram ? it.A : it.B;
     if (PHASE == kGram && diagonal) write_alpha(it, unscale, r0 + lane);
     const int p = lane & 7;
@@ -529,11 +553,10 @@ __device__ __forceinline__ void finish_symmetric(const NsItem &it, const NsParam
 // (a row a thread, 16 bytes each from another one, took 7 to 12 us for four blocks), adds them in the blocks' order, and leaves the
 // sum in its own part, which nobody else reads there, for the mirror image.
 template <int PHASE>
-__device__ __forceinline__ void finish_split(const NsItem &it, const NsParams &P, float *buf, uint32_t first, int r0, int c0, bool mirror, int me, int split)
+__device__ __forceinline__ void finish_split(const NsItem &it, const NsParams &P, float *buf, uint32_t first, float unscale, int r0, int c0, bool mirror, int me, int split)
 {
     const int lane = threadIdx.x & 31, p = lane & 7;
     const bool diagonal = r0 >= c0 && r0 < c0 + 64;
-    const float unscale = P.step == 0 ? 1.0f / (kStart * kStart) : 1.0f;
     uint16_t *const to = PHASE == kGram ? it.A : it.B;
     const uint32_t addr = smem_u32(buf);
     const Pieces at(it, r0, c0);
@@ -626,7 +649,7 @@ __device__ __forceinline__ void store_out8(const NsItem &it, long long at, const
 template <bool DEEP> __device__ __forceinline__ void finish_apply(const NsItem &it, const NsParams &P, Ahead<kApply> &ahead, float *buf, int r0, int c0)
 {
     const int lane = threadIdx.x & 31, p = lane & 7, cur = P.step & 1;
-    const float unscale = P.step == 0 ? 1.0f / kStart : 1.0f;
+    const float unscale = ahead.unscale;
     uint16_t *const next = it.x[cur ^ 1], *const rest = it.lo;
     const Pieces at(it, r0, c0);
     Ahead<kApply> second;
@@ -972,8 +995,10 @@ __global__ void __launch_bounds__(kNsThreads, kTileStages > 3 ? 1 : 2) ns_tile_k
 
     const int w = warp - 2, q = warp & 3, half = w >> 2;
     const int r0 = 128 * i + 32 * q, c0 = 128 * j + 64 * half;
+    float unscale = 1.0f;
     if (warp >= 2 && live) {
         Ahead<PHASE> ahead;
+        if (PHASE == kGram && split > 1) unscale = it.scale[P.step].x;
         if (split == 1) ahead.load(it, P, r0, c0);
         // all products are done, so all copies have landed: the ring is free
         if (mbar_wait_warp(&sm->acc_full, 0u, abort_flag, P.status, 32)) {
@@ -992,7 +1017,7 @@ __global__ void __launch_bounds__(kNsThreads, kTileStages > 3 ? 1 : 2) ns_tile_k
         if (clustered) {
             cluster_sync();
             if (warp >= 2 && live && split > 1)
-                finish_split<PHASE>(it, P, sm->sums[w], cluster_rank() & ~(uint32_t)(split - 1), r0, c0, j < i, me, split);
+                finish_split<PHASE>(it, P, sm->sums[w], cluster_rank() & ~(uint32_t)(split - 1), unscale, r0, c0, j < i, me, split);
             __syncwarp();
             cluster_done();                            // no block's memory goes while another reads it
         }
@@ -1052,7 +1077,7 @@ size_t scratch_bytes(const Shape &s)
 {
     if (s.m == 0) return 0;
     return 3 * (size_t)(s.rb * s.cb) * kBlockBytes + 2 * (size_t)(s.rb * s.rb) * kBlockBytes + (2 + (size_t)s.cb) * (size_t)s.rb * 64 * sizeof(float) +
-           align256((size_t)s.parts * sizeof(double));
+           kScaleBytes + align256((size_t)s.parts * sizeof(double));
 }
 // Points an item at its scratch and returns what comes after it.
 char *place(NsItem &it, const Shape &s, char *p)
@@ -1067,6 +1092,7 @@ char *place(NsItem &it, const Shape &s, char *p)
     it.alpha = reinterpret_cast<float *>(take((size_t)s.rb * 64 * sizeof(float)));
     it.beta = reinterpret_cast<float *>(take((size_t)s.rb * 64 * sizeof(float)));
     it.squares = reinterpret_cast<float *>(take((size_t)s.cb * (size_t)s.rb * 64 * sizeof(float)));
+    it.scale = reinterpret_cast<float2 *>(take(kScaleBytes));
     it.part = reinterpret_cast<double *>(take(align256((size_t)s.parts * sizeof(double))));
     it.m = (int)s.m; it.n = (int)s.n; it.rb = (int)s.rb; it.cb = (int)s.cb; it.parts = (int)s.parts;
     it.sym_pair = s.sym_pair; it.apply_pair = s.apply_pair;
@@ -1221,6 +1247,7 @@ int run_steps(NsParams &P, int steps, char *base, size_t bytes, Extents &extents
         return run_small(P, steps, s);
     }
     P.base = reinterpret_cast<const uint16_t *>(base);
+    P.steps = steps;
     enum { kNorm, kStartList, kSymPair, kGramTile, kSquareTile, kApplyPair, kApplyTile, kLists };
     NsParams list[kLists];
     auto all = [](const NsItem &) { return true; };
@@ -1257,7 +1284,6 @@ int run_steps(NsParams &P, int steps, char *base, size_t bytes, Extents &extents
     return TWN_OK;
 }
 
-constexpr int kMaxSteps = 32;
 constexpr double kMinEps = 1e-30;            // the factor of the first step stays in the range of fp32
 
 int check_shape(int64_t rows, int64_t cols)

@@ -18,6 +18,8 @@
 //
 // Range.  The Gram matrix is summed before the norm, its trace, is known.  Where that leaves the range in which fp32 keeps its
 // digits, it is summed again from G times a power of two, that of the trace where it says how large G is (second_scale).
+// X0 of a G below eps has a norm d = |G|_F / eps below 1, however small: the last product is taken with G over its own norm, and its
+// result times d.
 //
 // What bounds it: 14 dependent products of 128 x 128 x 128 (three MMA passes, 0.8 us each) with the elements' way through registers
 // between them (about as long), two passes over the matrix by eight SMs, and four cluster barriers.
@@ -47,8 +49,8 @@ struct __align__(1024) SmallSmem {
     uint32_t tmem_base;
     volatile int abort_flag;
     double red[kThreads / 32];
-    // what block 0 says: 1 / max(norm, eps) for X0 = G pre * factor; whether to sum again with pre
-    float factor, pre;
+    // what block 0 says: 1 / max(norm, eps) for X0 = G pre * factor, 1 / norm, and norm / max(norm, eps); whether to sum again with pre
+    float factor, by_norm, below, pre;
     int again;
 };
 
@@ -313,7 +315,7 @@ template <int KIND> __global__ void __launch_bounds__(kThreads, 1) ns_small_kern
     const uint32_t t_row = tmem + ((uint32_t)(32 * q) << 16);
 
     // ---- Gram matrix, its trace ------------------------------------------------------------------------------------------
-    float pre = 1.0f, factor = 0.0f;
+    float pre = 1.0f, factor = 0.0f, by_norm = 0.0f, below = 1.0f;
     constexpr int planes = KIND == kBf16 ? 1 : 3;
 #pragma unroll 1
     for (int attempt = 0; attempt < 2; ++attempt) {
@@ -420,12 +422,16 @@ template <int KIND> __global__ void __launch_bounds__(kThreads, 1) ns_small_kern
                 sm->pre = second_scale(trace);
                 const double scaled = sqrt(trace), least = (double)P.eps * (double)pre;
                 sm->factor = !finite ? __uint_as_float(0x7FC00000u) : trace == 0.0 ? 0.0f : (float)(1.0 / (scaled > least ? scaled : least));
+                sm->by_norm = finite && scaled < least && trace != 0.0 ? (float)(1.0 / scaled) : sm->factor;
+                sm->below = finite && scaled < least ? (float)(scaled / least) : 1.0f;
                 if (!sm->again && !finite && P.status) atomicMin(P.status, (int)TWN_ERR_NONFINITE);
             }
         }
         whole_cluster();
         const bool again = ld_cluster_u32(at_block(smem_u32(&sm->again), 0)) != 0;
         factor = __uint_as_float(ld_cluster_u32(at_block(smem_u32(&sm->factor), 0)));
+        by_norm = __uint_as_float(ld_cluster_u32(at_block(smem_u32(&sm->by_norm), 0)));
+        below = __uint_as_float(ld_cluster_u32(at_block(smem_u32(&sm->below), 0)));
         if (!again) break;
         pre = __uint_as_float(ld_cluster_u32(at_block(smem_u32(&sm->pre), 0)));
         whole_cluster();                                 // all have read it
@@ -551,7 +557,7 @@ template <int KIND> __global__ void __launch_bounds__(kThreads, 1) ns_small_kern
             const uint32_t at = (uint32_t)part * kHalfMatrix + (uint32_t)(piece >> 3) * 16384 + swizzled(r, 8 * (piece & 7));
             *reinterpret_cast<uint4 *>(sm->mat[2] + at) = __ldcg(reinterpret_cast<const uint4 *>(scratch + at));
         }
-    const float x_scale = factor * kScaleX, unscale = 1.0f / (kScaleQ * kScaleX);
+    const float x_scale = by_norm * kScaleX, unscale = 1.0f / (kScaleQ * kScaleX), out_scale = below * it.out_scale;
     float power = kScaleQ;                               // a^steps, beside the product
     for (int k = 0; k < P.steps; ++k) power *= kNsA;
     {
@@ -632,7 +638,7 @@ template <int KIND> __global__ void __launch_bounds__(kThreads, 1) ns_small_kern
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = fmaf(power, v[j], d[j]) * unscale * it.out_scale;
+                for (int j = 0; j < 16; ++j) v[j] = fmaf(power, v[j], d[j]) * unscale * out_scale;
                 if (!tall && it.vec_out) {
 #pragma unroll
                     for (int j = 0; j < 16; j += 8) {
