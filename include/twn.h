@@ -272,8 +272,8 @@ int twn_ternarize_codes_batch(const twn_ternarize_item_t *items, int count, void
  *              then NaNs, the other matrices are unaffected), TWN_ERR_TIMEOUT as in twn_gemm.
  * fp16 products, fp32 sums; X is carried in 22 bits (of a G far below eps too) and the diagonals of A and of b A + c A^2 in fp32, so five steps are within
  * 1e-3 (2-norm, relative) of 64-bit arithmetic for matrices of independent elements, and within 4e-3 for low rank (one included)
- * and for singular values that fall off.  Where blocks of equal elements make the roundings of the products align it can be
- * more (up to 1e-2 seen in 150 such matrices, 1.3e-3 in the middle).  A call of small matrices alone (sides of at most 128 and
+ * and for singular values that fall off.  Where equal rows or blocks of equal elements make the roundings of the products align it can
+ * be more (up to 1e-2 seen in 150 such matrices, 1.3e-3 in the middle; 1.7e-2 at most for equal rows).  A call of small matrices alone (sides of at most 128 and
  * 8192, five steps at most) takes its polynomial from the m x m matrix A in 22 bits: within 1e-4 for independent elements, and
  * within 4e-3 where singular values fall off over orders of magnitude (up to 1.1e-3 seen).
  * Deterministic; among the matrices of one call the others do not change a matrix's bits, but whether all are small does.

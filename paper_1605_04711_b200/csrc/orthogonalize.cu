@@ -413,12 +413,18 @@ __device__ __forceinline__ void load8(const float *p, float (&v)[8])
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
 
-// The diagonal of A for a warp's rows: the sums of squares of whole rows of X.
+// The diagonal of A for a warp's rows: the sums of squares of whole rows of X, 512 blocks of columns at a time, and those sums.
 __device__ __forceinline__ void write_alpha(const NsItem &it, float unscale, int r)
 {
     float a = 0.0f;
+#pragma unroll 1
+    for (int g0 = 0; g0 < it.cb; g0 += 512) {
+        float run = 0.0f;
+        const int end = min(g0 + 512, it.cb);
 #pragma unroll 16
-    for (int g = 0; g < it.cb; ++g) a += it.squares[(size_t)g * (64 * it.rb) + r];
+        for (int g = g0; g < end; ++g) run += it.squares[(size_t)g * (64 * it.rb) + r];
+        a += run;
+    }
     it.alpha[r] = a * unscale;
 }
 __device__ __forceinline__ float of_square(float sum, float a, float alphas) { return kB * a + kC * (sum + alphas * a); }
@@ -895,17 +901,42 @@ ns_pair_kernel(const __grid_constant__ CUtensorMap rows128, const __grid_constan
 // A 128x128 tile a block, two blocks on an SM with rings of three stages, or one with six where there are no more blocks than SMs (a
 // block's reduction of 64 took 0.46 us with three, 1.5 times what the feed from L2 needs).  `split` blocks of a cluster share a tile's reduction; each leaves its sums in
 // the shared memory that was its ring, and finishes every split-th unit of the whole tile.
+//
+// LONG: reductions of more than kChunk blocks.  The tensor core's sums are cut off at every addition (16 columns), half a unit in the last place too
+// small on average; where the rows of X agree that goes all one way, 2^-25 of a sum for every 16 columns of a block's share (2 x 2^20 of
+// mean 1: 7e-3 off in the result, 2 x 2^24: 8e-2).  So the sums of kChunk blocks, 2^-16 too small, are added in fp32 to those before, in
+// tensor memory beside them, while the ring fills.
+constexpr int kChunk = 128;
 template <int STAGES> struct __align__(1024) TileSmem {
     union {
         uint8_t ring[STAGES][kStageBytes];
         float sums[kEpiWarps][kWarpTile];
     };
-    unsigned long long full[STAGES], empty[STAGES], acc_full;
+    unsigned long long full[STAGES], empty[STAGES], acc_full, acc_empty;
     uint32_t tmem_base;
     volatile int abort_flag;
 };
 
-template <int PHASE, int kTileStages>
+// 64 columns of a warp's 32 rows: `more` added to `sums`, or put there.
+__device__ __forceinline__ void add_sums(uint32_t sums, uint32_t more, bool first)
+{
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+        uint32_t v[32], w[32];
+        tmem_ld32(more + 32 * g, v);
+        tmem_wait_ld(v);
+        if (!first) {
+            tmem_ld32(sums + 32 * g, w);
+            tmem_wait_ld(w);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(w[j]) + __uint_as_float(v[j]));
+        }
+        tmem_st32(sums + 32 * g, v);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+    }
+}
+
+template <int PHASE, int kTileStages, bool LONG>
 __global__ void __launch_bounds__(kNsThreads, kTileStages > 3 ? 1 : 2) ns_tile_kernel(const __grid_constant__ NsParams P, bool clustered)
 {
     pdl_launch_dependents();
@@ -914,15 +945,17 @@ __global__ void __launch_bounds__(kNsThreads, kTileStages > 3 ? 1 : 2) ns_tile_k
     Smem *sm = reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     volatile int *abort_flag = &sm->abort_flag;
     const int warp = threadIdx.x >> 5;
+    constexpr uint32_t kColumns = LONG ? 256 : 128;      // of tensor memory
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kTileStages; ++s) { mbar_init(&sm->full[s], 1); mbar_init(&sm->empty[s], 1); }
         mbar_init(&sm->acc_full, 1);
+        mbar_init(&sm->acc_empty, kEpiWarps);
         sm->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(128u) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     // the tile's place needs the parameters alone: read while the kernel before this one ends
@@ -981,10 +1014,15 @@ __global__ void __launch_bounds__(kNsThreads, kTileStages > 3 ? 1 : 2) ns_tile_k
             uint32_t s = 0, ph = 0;
             bool ok = true;
             for (int k = k0; k < k1; ++k) {
+                const int in_chunk = LONG ? (k - k0) % kChunk : k - k0;
+                if (LONG && in_chunk == 0 && k > k0) {
+                    tc_commit(&sm->acc_full);
+                    if (!mbar_wait(&sm->acc_empty, ((k - k0) / kChunk - 1) & 1, abort_flag, P.status, 0)) { ok = false; break; }
+                }
                 if (!mbar_wait(&sm->full[s], ph, abort_flag, P.status, 0)) { ok = false; break; }
                 tc_fence_after();
                 const uint64_t off = s * (uint64_t)(kStageBytes >> 4);
-                ns_mma_block<PHASE, false>(tmem, a0 + off, b0 + off, idesc, k == k0);
+                ns_mma_block<PHASE, false>(tmem, a0 + off, b0 + off, idesc, in_chunk == 0);
                 tc_commit(&sm->empty[s]);
                 if (++s == kTileStages) { s = 0; ph ^= 1u; }
             }
@@ -1000,10 +1038,23 @@ __global__ void __launch_bounds__(kNsThreads, kTileStages > 3 ? 1 : 2) ns_tile_k
         Ahead<PHASE> ahead;
         if (PHASE == kGram && split > 1) unscale = it.scale[P.step].x;
         if (split == 1) ahead.load(it, P, r0, c0);
-        // all products are done, so all copies have landed: the ring is free
-        if (mbar_wait_warp(&sm->acc_full, 0u, abort_flag, P.status, 32)) {
+        const uint32_t acc = tmem + ((uint32_t)(32 * q) << 16) + 64 * half;
+        const int chunks = LONG ? (k1 - k0 + kChunk - 1) / kChunk : 1;
+        bool ok = true;
+        for (int c = 0; LONG && c + 1 < chunks && ok; ++c) {
+            ok = mbar_wait_warp(&sm->acc_full, c & 1, abort_flag, P.status, 32);
+            if (!ok) break;
             tc_fence_after();
-            dump_sums(tmem + ((uint32_t)(32 * q) << 16) + 64 * half, sm->sums[w]);
+            add_sums(acc + 128, acc, c == 0);
+            tc_fence_before();
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) mbar_arrive(&sm->acc_empty);
+        }
+        // all products are done, so all copies have landed: the ring is free
+        if (ok && mbar_wait_warp(&sm->acc_full, (chunks - 1) & 1, abort_flag, P.status, 32)) {
+            tc_fence_after();
+            if (LONG && chunks > 1) add_sums(acc + 128, acc, false);
+            dump_sums(acc + (LONG && chunks > 1 ? 128 : 0), sm->sums[w]);
             tc_fence_before();
             __syncwarp();
             if (split == 1) {
@@ -1032,7 +1083,7 @@ __global__ void __launch_bounds__(kNsThreads, kTileStages > 3 ? 1 : 2) ns_tile_k
     }
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(128u) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kColumns) : "memory");
     }
 }
 
@@ -1043,7 +1094,7 @@ struct Shape {
     int64_t m, n, rb, cb, parts;
     bool fits, sym_pair, apply_pair;
 };
-constexpr int64_t kMaxShort = 32768, kMaxLong = 1 << 24;
+constexpr int64_t kMaxShort = 32768, kMaxLong = 1 << 24, kPairLong = 1 << 17;
 // How a matrix is served goes by its own sizes alone, so it has the same bits in every batch.
 Shape shape_of(int64_t rows, int64_t cols)
 {
@@ -1056,7 +1107,8 @@ Shape shape_of(int64_t rows, int64_t cols)
     // Pairs need tiles for most of the 74 of them.  Triangles: 36 tiles (2048 rows) 344 us with pairs, 239 without, 55 (2560 rows) 450 and 439,
     // 136 (4096 rows) two rounds of pairs for 3.6 of single blocks.  B X: 36 tiles (512 x 4608) 167 and 145, 64 (4096 x 1024) 200 and 189,
     // 81 (2300 x 2300) 438 and 462, 96 (3000 x 2000) 311 and 343.
-    s.sym_pair = m256 > 10;
+    // Pairs have no tensor memory left for the sums of a long reduction (see LONG).
+    s.sym_pair = m256 > 10 && s.n <= kPairLong;
     s.apply_pair = m256 * n256 > 64;
     const bool wide = s.sym_pair || s.apply_pair;
     s.rb = wide ? 4 * m256 : 2 * m128;
@@ -1158,13 +1210,13 @@ template <int PHASE> int launch_pair(const NsParams &P, const CUtensorMap (&map)
     TWN_CUDA_OK(launch_clusters(ns_pair_kernel<PHASE>, 2 * std::min(P.units, dev.sm_count / 2), 2, smem, s, map[0], map[1], P));
     return TWN_OK;
 }
-template <int PHASE, int STAGES> int launch_tile(const NsParams &P, int grid, int cluster, const twn_device_info &dev, cudaStream_t s)
+template <int PHASE, int STAGES, bool LONG> int launch_tile(const NsParams &P, int grid, int cluster, const twn_device_info &dev, cudaStream_t s)
 {
     static bool done[64] = {false};
     const size_t smem = sizeof(TileSmem<STAGES>) + 1024;
-    const int rc = allow_smem(ns_tile_kernel<PHASE, STAGES>, smem, done[dev.ordinal]);
+    const int rc = allow_smem(ns_tile_kernel<PHASE, STAGES, LONG>, smem, done[dev.ordinal]);
     if (rc != TWN_OK) return rc;
-    TWN_CUDA_OK(launch_clusters(ns_tile_kernel<PHASE, STAGES>, grid, cluster, smem, s, P, cluster > 1));
+    TWN_CUDA_OK(launch_clusters(ns_tile_kernel<PHASE, STAGES, LONG>, grid, cluster, smem, s, P, cluster > 1));
     return TWN_OK;
 }
 template <int PHASE> int launch_tile(const NsParams &P, const twn_device_info &dev, cudaStream_t s)
@@ -1173,7 +1225,12 @@ template <int PHASE> int launch_tile(const NsParams &P, const twn_device_info &d
     if (PHASE != kApply)
         for (int t = 0; t < P.count; ++t) cluster = std::max(cluster, P.item[t].split);
     const int grid = (P.units + cluster - 1) / cluster * cluster;
-    return grid <= dev.sm_count ? launch_tile<PHASE, 6>(P, grid, cluster, dev, s) : launch_tile<PHASE, 3>(P, grid, cluster, dev, s);
+    if constexpr (PHASE == kGram) {
+        bool chunks = false;
+        for (int t = 0; t < P.count; ++t) chunks |= (P.item[t].n + 63) / 64 > (int64_t)kChunk * P.item[t].split;
+        if (chunks) return grid <= dev.sm_count ? launch_tile<PHASE, 6, true>(P, grid, cluster, dev, s) : launch_tile<PHASE, 3, true>(P, grid, cluster, dev, s);
+    }
+    return grid <= dev.sm_count ? launch_tile<PHASE, 6, false>(P, grid, cluster, dev, s) : launch_tile<PHASE, 3, false>(P, grid, cluster, dev, s);
 }
 
 // All blocks of the workspace as one matrix of 128-byte rows, in copies of 128 and of 64 of them.
