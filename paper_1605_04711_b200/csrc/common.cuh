@@ -29,6 +29,13 @@ struct twn_device_info {
 // current device is not compute capability 10.x.
 int twn_current_device(twn_device_info *info);
 
+namespace twn_detail {
+// twn_sgd_update_batch with dW as the whole update: W = W - lr * (dW + weight_decay * W), and what it leaves for the next thresholds.  An
+// item's V is not used.
+int apply_updates(const twn_sgd_item_t *items, int count, float lr, float weight_decay, double delta_factor, void *workspace,
+                  size_t workspace_bytes, twn_stream_t stream);
+}  // namespace twn_detail
+
 static inline bool twn_aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 static inline cudaStream_t twn_cu(twn_stream_t s) { return reinterpret_cast<cudaStream_t>(s); }

@@ -1451,10 +1451,7 @@ extern "C" int twn_muon_update_batch(const twn_muon_item_t *items, int count, fl
         it.vec_in = 1;
         it.vec_out = in.cols % 8 == 0;
         it.out_scale = in.rows > in.cols ? (float)std::sqrt((double)in.rows / (double)in.cols) : 1.0f;
-        // the update with the orthogonalised matrix as gradient and no momentum; that sweep's V is the matrix itself,
-        // every element of which it reads before it writes it
-        apply[t].dW = static_cast<const float *>(it.O);
-        apply[t].V = static_cast<float *>(it.O);
+        apply[t].dW = static_cast<const float *>(it.O);      // the whole update: a sweep without a momentum
     }
     const size_t need = twn_muon_workspace_bytes(items, count);
     TWN_REQUIRE(workspace_bytes >= need, TWN_ERR_WORKSPACE);
@@ -1467,5 +1464,5 @@ extern "C" int twn_muon_update_batch(const twn_muon_item_t *items, int count, fl
         const int rc = run_steps(P, steps, static_cast<char *>(workspace), need, extents, twn_cu(stream));
         if (rc != TWN_OK) return rc;
     }
-    return twn_sgd_update_batch(apply, count, lr, 0.0f, weight_decay, delta_factor, sweep_ws, sweep_bytes, stream);
+    return twn_detail::apply_updates(apply, count, lr, weight_decay, delta_factor, sweep_ws, sweep_bytes, stream);
 }

@@ -976,12 +976,18 @@ __device__ __forceinline__ float sgd_one(float w, float g, float &v, float lr, f
     return __fsub_rn(w, __fmul_rn(lr, v));
 }
 
-__device__ __forceinline__ void sgd_four(float4 &w, const float4 g, float4 &v, float lr, float mu, float wd, double &a0, double &a1)
+// KEEPS: with a momentum of its own; else the gradient is the whole update, and V is neither read nor written.
+template <bool KEEPS> __device__ __forceinline__ float update_one(float w, float g, float &v, float lr, float mu, float wd)
 {
-    w.x = sgd_one(w.x, g.x, v.x, lr, mu, wd);
-    w.y = sgd_one(w.y, g.y, v.y, lr, mu, wd);
-    w.z = sgd_one(w.z, g.z, v.z, lr, mu, wd);
-    w.w = sgd_one(w.w, g.w, v.w, lr, mu, wd);
+    if (KEEPS) return sgd_one(w, g, v, lr, mu, wd);
+    return __fsub_rn(w, __fmul_rn(lr, __fadd_rn(g, __fmul_rn(wd, w))));
+}
+template <bool KEEPS> __device__ __forceinline__ void sgd_four(float4 &w, const float4 g, float4 &v, float lr, float mu, float wd, double &a0, double &a1)
+{
+    w.x = update_one<KEEPS>(w.x, g.x, v.x, lr, mu, wd);
+    w.y = update_one<KEEPS>(w.y, g.y, v.y, lr, mu, wd);
+    w.z = update_one<KEEPS>(w.z, g.z, v.z, lr, mu, wd);
+    w.w = update_one<KEEPS>(w.w, g.w, v.w, lr, mu, wd);
     a0 += (double)fabsf(w.x); a1 += (double)fabsf(w.y); a0 += (double)fabsf(w.z); a1 += (double)fabsf(w.w);
 }
 
@@ -996,7 +1002,7 @@ __device__ __forceinline__ void write_next(const SgdItem &it, double factor, dou
 // The blocks' sums meet through distributed shared memory where one cluster of at most eight blocks does, else in the
 // workspace, where a launch of their own folds them, one block per tensor, that is there when this one ends (in a cooperative
 // launch with a barrier 590 thousand weights took 6.2 us, 4.4 now, 8.4 million 32.4 and 30.3).
-template <int N, bool CLUSTER>
+template <int N, bool CLUSTER, bool KEEPS>
 __global__ void __launch_bounds__(kSweepThreads, kSweepBlocksPerSm)
 sgd_update_kernel(const __grid_constant__ SgdLaunch<N> P, void *ws_raw)
 {
@@ -1027,29 +1033,30 @@ sgd_update_kernel(const __grid_constant__ SgdLaunch<N> P, void *ws_raw)
         double a0 = 0.0, a1 = 0.0;
         long long i = (long long)vb * kSweepThreads + threadIdx.x;
         // two iterations in flight: six 16-byte loads per thread, 1024 threads per SM
+        const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         for (; i + stride < n4; i += 2 * stride) {
-            float4 w = W4[i], v = V4[i], w2 = W4[i + stride], v2 = V4[i + stride];
+            float4 w = W4[i], v = KEEPS ? V4[i] : none, w2 = W4[i + stride], v2 = KEEPS ? V4[i + stride] : none;
             const float4 d = __ldg(G4 + i), d2 = __ldg(G4 + i + stride);
-            sgd_four(w, d, v, P.lr, P.mu, P.wd, a0, a1);
+            sgd_four<KEEPS>(w, d, v, P.lr, P.mu, P.wd, a0, a1);
             W4[i] = w;
-            V4[i] = v;
-            sgd_four(w2, d2, v2, P.lr, P.mu, P.wd, a0, a1);
+            if (KEEPS) V4[i] = v;
+            sgd_four<KEEPS>(w2, d2, v2, P.lr, P.mu, P.wd, a0, a1);
             W4[i + stride] = w2;
-            V4[i + stride] = v2;
+            if (KEEPS) V4[i + stride] = v2;
         }
         if (i < n4) {
-            float4 w = W4[i], v = V4[i];
-            sgd_four(w, __ldg(G4 + i), v, P.lr, P.mu, P.wd, a0, a1);
+            float4 w = W4[i], v = KEEPS ? V4[i] : none;
+            sgd_four<KEEPS>(w, __ldg(G4 + i), v, P.lr, P.mu, P.wd, a0, a1);
             W4[i] = w;
-            V4[i] = v;
+            if (KEEPS) V4[i] = v;
         }
         if (vb == 0) {
             const long long e = (n4 << 2) + threadIdx.x;
             if (e < it.n) {
-                float v = it.V[e];
-                const float w = sgd_one(it.W[e], __ldg(it.dW + e), v, P.lr, P.mu, P.wd);
+                float v = KEEPS ? it.V[e] : 0.0f;
+                const float w = update_one<KEEPS>(it.W[e], __ldg(it.dW + e), v, P.lr, P.mu, P.wd);
                 it.W[e] = w;
-                it.V[e] = v;
+                if (KEEPS) it.V[e] = v;
                 a0 += (double)fabsf(w);
             }
         }
@@ -1496,7 +1503,7 @@ bool batch_items(const twn_ternarize_item_t *items, int count, Launch<kMaxBatch>
     return true;
 }
 
-template <int N>
+template <int N, bool KEEPS>
 int launch_sgd(SgdLaunch<N> &P, void *ws, cudaStream_t s)
 {
     twn_device_info dev;
@@ -1513,10 +1520,10 @@ int launch_sgd(SgdLaunch<N> &P, void *ws, cudaStream_t s)
         if (P.blocks <= kSmallParts) {
             unsigned int grid = 1;
             while (grid < P.blocks) grid *= 2;
-            return launch_cluster(sgd_update_kernel<N, true>, grid, s, P, ws);
+            return launch_cluster(sgd_update_kernel<N, true, KEEPS>, grid, s, P, ws);
         }
     }
-    TWN_CUDA_OK(twn_launch_pdl(true, sgd_update_kernel<N, false>, (int)std::min(P.blocks, (unsigned int)(dev.sm_count * kSweepBlocksPerSm)),
+    TWN_CUDA_OK(twn_launch_pdl(true, sgd_update_kernel<N, false, KEEPS>, (int)std::min(P.blocks, (unsigned int)(dev.sm_count * kSweepBlocksPerSm)),
                                kSweepThreads, 0, s, P, ws));
     TWN_CUDA_OK(twn_launch_pdl(true, sgd_fold_kernel<N>, P.count, kSweepThreads, 0, s, P, ws));
     return TWN_OK;
@@ -1621,12 +1628,12 @@ extern "C" int twn_sgd_update(float *W, const float *dW, float *V, int64_t n, fl
     P.count = 1;
     P.lr = lr; P.mu = momentum; P.wd = weight_decay; P.factor = delta_factor;
     P.item[0] = SgdItem{W, dW, V, n, stats_next, 0};
-    return launch_sgd(P, workspace, twn_cu(stream));
+    return launch_sgd<1, true>(P, workspace, twn_cu(stream));
 }
 
-extern "C" int twn_sgd_update_batch(const twn_sgd_item_t *items, int count, float lr, float momentum,
-                                    float weight_decay, double delta_factor, void *workspace, size_t workspace_bytes,
-                                    twn_stream_t stream)
+template <bool KEEPS>
+static int update_batch(const twn_sgd_item_t *items, int count, float lr, float momentum, float weight_decay, double delta_factor,
+                        void *workspace, size_t workspace_bytes, twn_stream_t stream)
 {
     TWN_REQUIRE(count >= 0 && count <= kMaxBatch, TWN_ERR_INVALID_ARG);
     if (count == 0) return TWN_OK;
@@ -1640,12 +1647,25 @@ extern "C" int twn_sgd_update_batch(const twn_sgd_item_t *items, int count, floa
     P.lr = lr; P.mu = momentum; P.wd = weight_decay; P.factor = delta_factor;
     for (int t = 0; t < count; ++t) {
         const twn_sgd_item_t &it = items[t];
-        TWN_REQUIRE(it.n >= 0 && (it.n == 0 || (it.W && it.dW && it.V)), TWN_ERR_INVALID_ARG);
+        TWN_REQUIRE(it.n >= 0 && (it.n == 0 || (it.W && it.dW && (it.V || !KEEPS))), TWN_ERR_INVALID_ARG);
         TWN_REQUIRE(twn_aligned(it.W, 16) && twn_aligned(it.dW, 16) && twn_aligned(it.V, 16) &&
                         twn_aligned(it.stats_next, 8), TWN_ERR_MISALIGNED);
         P.item[t] = SgdItem{it.W, it.dW, it.V, it.n, it.stats_next, 0};
     }
-    return launch_sgd(P, workspace, twn_cu(stream));
+    return launch_sgd<kMaxBatch, KEEPS>(P, workspace, twn_cu(stream));
+}
+
+extern "C" int twn_sgd_update_batch(const twn_sgd_item_t *items, int count, float lr, float momentum,
+                                    float weight_decay, double delta_factor, void *workspace, size_t workspace_bytes,
+                                    twn_stream_t stream)
+{
+    return update_batch<true>(items, count, lr, momentum, weight_decay, delta_factor, workspace, workspace_bytes, stream);
+}
+
+int twn_detail::apply_updates(const twn_sgd_item_t *items, int count, float lr, float weight_decay, double delta_factor, void *workspace,
+                              size_t workspace_bytes, twn_stream_t stream)
+{
+    return update_batch<false>(items, count, lr, 0.0f, weight_decay, delta_factor, workspace, workspace_bytes, stream);
 }
 
 // ---- the variant that allocates nothing ------------------------------------------------
