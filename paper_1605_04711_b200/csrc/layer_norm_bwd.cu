@@ -433,7 +433,8 @@ __global__ void __launch_bounds__(kStripeThreads) norm_bwd_stripe_kernel(const _
 // dgamma and dbeta: a column's parts in 32 runs, all of a run's loads at once (with eight runs, one load after the other, the fold of 148
 // parts took longer than what it folds), and the runs in order.
 constexpr int kPartBlocks = 148, kRuns = 32, kPerRun = (kPartBlocks + kRuns - 1) / kRuns;
-// W columns a thread, so that up to 4736 channels, or 9472, are a block an SM, which may start early.
+// W columns a thread, so that up to 4736 channels, or 9472, are a block an SM, which may start early: while the launch before it still writes the parts,
+// so their loads are plain ones, not those of data that nobody writes.
 template <int W> __global__ void __launch_bounds__(32 * kRuns) norm_fold_kernel(const float *part, int parts, long long C, float *dgamma, float *dbeta)
 {
     __shared__ float s[kRuns][32 * W];
@@ -449,13 +450,13 @@ template <int W> __global__ void __launch_bounds__(32 * kRuns) norm_fold_kernel(
         if (p < parts && c < 2 * C) {
             const float *const from = part + (long long)p * 2 * C + c;
             if constexpr (W == 4) {
-                const float4 a = __ldg(reinterpret_cast<const float4 *>(from));
+                const float4 a = *reinterpret_cast<const float4 *>(from);
                 w[k][0] = a.x; w[k][1] = a.y; w[k][2] = a.z; w[k][3] = a.w;
             } else if constexpr (W == 2) {
-                const float2 a = __ldg(reinterpret_cast<const float2 *>(from));
+                const float2 a = *reinterpret_cast<const float2 *>(from);
                 w[k][0] = a.x; w[k][1] = a.y;
             } else {
-                w[k][0] = __ldg(from);
+                w[k][0] = *from;
             }
         }
     }
