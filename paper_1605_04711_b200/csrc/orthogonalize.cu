@@ -413,9 +413,12 @@ __device__ __forceinline__ void load8(const float *p, float (&v)[8])
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
 
-// The diagonal of A for a warp's rows: the sums of squares of whole rows of X, 512 blocks of columns at a time, and those sums.
-__device__ __forceinline__ void write_alpha(const NsItem &it, float unscale, int r)
+// The diagonal of A for a warp's rows, if its tile lies on it: the sums of squares of whole rows of X, 512 blocks of columns at a time, and
+// those sums.  It needs no product, so it is done while they run.
+__device__ __forceinline__ void write_alpha(const NsItem &it, float unscale, int r0, int c0)
 {
+    if (r0 < c0 || r0 >= c0 + 64) return;
+    const int r = r0 + (threadIdx.x & 31);
     float a = 0.0f;
 #pragma unroll 1
     for (int g0 = 0; g0 < it.cb; g0 += 512) {
@@ -502,7 +505,6 @@ __device__ __forceinline__ void finish_symmetric(const NsItem &it, const NsParam
     float unscale = 1.0f;
     if constexpr (PHASE == kGram) unscale = ahead.unscale;
     uint16_t *const to = PHASE == kGram ? it.A : it.B;
-    if (PHASE == kGram && diagonal) write_alpha(it, unscale, r0 + lane);
     const int p = lane & 7;
     const Pieces at(it, r0, c0);
 #pragma unroll
@@ -631,7 +633,6 @@ __device__ __forceinline__ void finish_split(const NsItem &it, const NsParams &P
             }
         }
     }
-    if (PHASE == kGram && diagonal && me == 0) write_alpha(it, unscale, r0 + lane);
 }
 
 __device__ __forceinline__ void store_out(const NsItem &it, long long at, float v)
@@ -865,6 +866,7 @@ ns_pair_kernel(const __grid_constant__ CUtensorMap rows128, const __grid_constan
                 const int c0 = 256 * J + 64 * b;
                 Ahead<PHASE> ahead;
                 ahead.load(it, P, r0, c0);
+                if constexpr (PHASE == kGram) write_alpha(it, ahead.unscale, r0, c0);
                 if (b < 2 && !mbar_wait_warp(&sm->acc_full[lu & 1], (lu >> 1) & 1u, abort_flag, P.status, 32)) { ok = false; break; }
                 tc_fence_after();
                 dump_sums(tmem + ((uint32_t)(32 * q) << 16) + (lu & 1) * 256 + 64 * b, buf);
@@ -1036,8 +1038,11 @@ __global__ void __launch_bounds__(kNsThreads, kTileStages > 3 ? 1 : 2) ns_tile_k
     float unscale = 1.0f;
     if (warp >= 2 && live) {
         Ahead<PHASE> ahead;
-        if (PHASE == kGram && split > 1) unscale = it.scale[P.step].x;
         if (split == 1) ahead.load(it, P, r0, c0);
+        if constexpr (PHASE == kGram) {
+            unscale = it.scale[P.step].x;
+            if (me == 0) write_alpha(it, unscale, r0, c0);
+        }
         const uint32_t acc = tmem + ((uint32_t)(32 * q) << 16) + 64 * half;
         const int chunks = LONG ? (k1 - k0 + kChunk - 1) / kChunk : 1;
         bool ok = true;
