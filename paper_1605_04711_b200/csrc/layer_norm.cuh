@@ -5,10 +5,16 @@
 //             dgamma = sum over the rows of dy xh,  dbeta = sum over the rows of dy
 //   computed with d = x - mean and h = rstd g, so that xh is never formed:  dx = h - sum(h) / C - d rstd^2 sum(h d) / C
 //
-// Both are bound by HBM: a row is read once and stays in registers until its result is written.  A team of T threads (4 to
-// 1024, a power of two) has a row, E elements a thread; its sums are shuffle trees, and one barrier where it is more than a
-// warp.  The variance is that of the differences from the mean (a second tree), never a difference of two sums: rows far from
+// Both are bound by HBM.  A team of T threads has a row, E elements a thread; its sums are shuffle trees, and one barrier where it is
+// more than a warp.  The variance is that of the differences from the mean (a second tree), never a difference of two sums: rows far from
 // zero keep their digits.  All arithmetic is fp32, rounded once to the type of the output.
+//
+//   forward    registers (T a power of two from 4 to 1024): the row is read once and stays there until its result is written; small
+//              tensors, single elements, rows of 8193 to 32768.  Large tensors of aligned rows of 257 to 32768 that a ring's two stages
+//              hold: bulk copies into shared memory, read once from there (T any number of warps).  Longer rows are read three times, from L2 after the first.
+//   backward   rows of up to 8192 (T a power of two from 4 to 512): read once, into shared memory by the threads' own copies, or into registers
+//              where elements are single.  Aligned rows of 8193 to 16384: bulk copies into a ring, read twice from there (T any number
+//              of warps).  Other rows in two launches that read dY and X each: the rows' sums, then stripes of columns (which do form xh).
 #pragma once
 
 #include <algorithm>

@@ -223,43 +223,43 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_kernel(const __grid_c
     join_sums<V>(g, b, col, (int)threadIdx.x % span < T, threadIdx.x / span, blockDim.x / span, cols, out);
 }
 
-// Rows of more than 8192 elements, through shared memory by bulk copies (see norm_fwd_ring_kernel; up to 8192 it is behind the one above by up to 1.6 times).  The sums over the rows fill the registers, so a row is read
-// twice from its stage, for its two sums and for its gradient; the stage is refilled after the next row's sums, when the whole team has
-// left it.
+// Rows of more than 8192 elements, through shared memory by bulk copies (see norm_fwd_ring_kernel; up to 8192 it is behind the one above by up to 1.6 times).
+// A block is one team of at least 288 threads, and has a row at a time.  The sums over the rows fill the registers, so a row is read twice
+// from its stage, for its two sums and for its gradient; the stage is refilled after the next row's sums, when the whole team has left it.
 template <typename TD, typename TX, typename TO, int V, int E, int TT>
 __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __grid_constant__ BwdParams P, const __grid_constant__ Ring R)
 {
     constexpr int P2 = E / 2, W = V;         // elements worked on at a time
     extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ unsigned long long full[kMaxTeams][kMaxRing];
+    __shared__ unsigned long long full[kMaxRing];
     __shared__ __align__(16) float red[2][32][2];
     __shared__ volatile int gave_up;
     unsigned int turn = 0;
-    const int T = TT ? TT : P.T, team = threadIdx.x / T, t = threadIdx.x - team * T, C = TT ? TT * E : (int)P.C;
-    const int teams = blockDim.x / T, barrier = teams > 1 ? team + 1 : 0;
+    const int T = TT ? TT : P.T, t = threadIdx.x, C = TT ? TT * E : (int)P.C;
     const float inv = 1.0f / (float)C;
     const Columns<V, TT> col{T, t, C};
-    if (t == 0)
-        for (int s = 0; s < R.stages; ++s) mbar_init(&full[team][s], 1);
-    if (threadIdx.x == 0) gave_up = 0;
+    if (t == 0) {
+        for (int s = 0; s < R.stages; ++s) mbar_init(&full[s], 1);
+        gave_up = 0;
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
     pdl_begin();
-    uint8_t *const mine = ring + R.params + (size_t)team * R.stages * R.stage_bytes;
-    const long long first = (long long)blockIdx.x * teams + team, step = (long long)gridDim.x * teams;
+    uint8_t *const stages = ring + R.params;
+    const long long first = blockIdx.x, step = gridDim.x;
     auto issue = [&](long long r, int s) {
         if (r >= P.M) return;
-        uint8_t *const st = mine + (size_t)s * R.stage_bytes;
-        mbar_expect_tx(&full[team][s], C * (uint32_t)(sizeof(TD) + sizeof(TX)));
-        bulk_load(st, static_cast<const TD *>(P.dY) + r * P.lddy, C * (uint32_t)sizeof(TD), &full[team][s]);
-        bulk_load(st + R.second, static_cast<const TX *>(P.X) + r * P.ldx, C * (uint32_t)sizeof(TX), &full[team][s]);
+        uint8_t *const st = stages + (size_t)s * R.stage_bytes;
+        mbar_expect_tx(&full[s], C * (uint32_t)(sizeof(TD) + sizeof(TX)));
+        bulk_load(st, static_cast<const TD *>(P.dY) + r * P.lddy, C * (uint32_t)sizeof(TD), &full[s]);
+        bulk_load(st + R.second, static_cast<const TX *>(P.X) + r * P.ldx, C * (uint32_t)sizeof(TX), &full[s]);
     };
     if (t == 0)
         for (int s = 0; s < R.stages; ++s) issue(first + s * step, s);
     const bool in_ring = TT ? TT * E * sizeof(float) <= kBwdRingBytes / 2 : R.params > 0;
     float *const gammas = in_ring ? reinterpret_cast<float *>(ring) : nullptr;
     if (in_ring) {
-        for (int c = threadIdx.x; c < C; c += blockDim.x) gammas[param_at<V>(c, C)] = P.gamma ? P.gamma[c] : 1.0f;
+        for (int c = threadIdx.x; c < C; c += T) gammas[param_at<V>(c, C)] = P.gamma ? P.gamma[c] : 1.0f;
         __syncthreads();
     }
     two_f32 a_g[P2], a_b[P2];
@@ -271,8 +271,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
     for (long long r = first; r < P.M; r += step) {
         const float mean = n_mean, rstd = n_rstd;
         if (r + step < P.M) { n_mean = P.mean[r + step]; n_rstd = P.rstd[r + step]; }
-        const bool ok = mbar_wait(&full[team][s], ph, &gave_up, nullptr, 0);
-        const uint8_t *const st = mine + (size_t)s * R.stage_bytes;
+        const bool ok = mbar_wait(&full[s], ph, &gave_up, nullptr, 0);
+        const uint8_t *const st = stages + (size_t)s * R.stage_bytes;
         const TX *const x = reinterpret_cast<const TX *>(st + R.second);
         const TD *const dy = reinterpret_cast<const TD *>(st);
         const two_f32 minus = two(-mean, -mean), scale = two(rstd, rstd);
@@ -311,10 +311,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
             }
         }
         float sums[2] = {sum2(s0), ok ? sum2(s1) : __uint_as_float(0x7FC00000u)};
-        if constexpr (TT > 0) team_sum<TT>(sums, red, turn, barrier);
-        else team_sum(sums, T, red, turn, barrier);
+        if constexpr (TT > 0) team_sum<TT>(sums, red, turn, 0);
+        else team_sum(sums, T, red, turn, 0);
         // the whole team has left the row before this one: its stage is free
-        if (T == 32) __syncwarp();
         if (t == 0 && r != first) issue(r + (R.stages - 1) * step, s == 0 ? R.stages - 1 : s - 1);
         if (P.dX) {
             const float c0 = -sums[0] * inv, c1 = -sums[1] * inv * rstd * rstd;
@@ -336,12 +335,10 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
         if (++s == R.stages) { s = 0; ph ^= 1u; }
     }
     if (P.part == nullptr) return;
-    __syncthreads();                         // no copy is on its way: the ring takes the sums, the teams in turn
-    float *const cols = reinterpret_cast<float *>(ring), *const out = P.part + (long long)blockIdx.x * 2 * C;
     float g[E], b[E];
 #pragma unroll
     for (int i = 0; i < P2; ++i) { each(a_g[i], g[2 * i], g[2 * i + 1]); each(a_b[i], b[2 * i], b[2 * i + 1]); }
-    join_sums<V>(g, b, col, true, team, teams, cols, out);
+    join_sums<V>(g, b, col, true, 0, 1, nullptr, P.part + (long long)blockIdx.x * 2 * C);
 }
 
 // Long rows, first pass: sum(g) / C and sum(g xh) / C of every row.
@@ -484,7 +481,7 @@ int launch_bwd_ring(const BwdParams &P, const RingShape &r, const twn_device_inf
     static bool done[64] = {false};
     const int rc = allow_ring(norm_bwd_ring_kernel<TD, TX, TO, V, E, TT>, dev.ordinal, done);
     if (rc != TWN_OK) return rc;
-    TWN_CUDA_OK(twn_launch_small(norm_bwd_ring_kernel<TD, TX, TO, V, E, TT>, P.parts, r.T * r.teams, r.smem, s, P, r.ring));
+    TWN_CUDA_OK(twn_launch_small(norm_bwd_ring_kernel<TD, TX, TO, V, E, TT>, P.parts, r.T, r.smem, s, P, r.ring));
     return TWN_OK;
 }
 template <typename TD, typename TX, typename TO, int V, int E> bool bwd_ring(BwdParams &P, const twn_device_info &dev, cudaStream_t s, int &rc)
@@ -493,9 +490,7 @@ template <typename TD, typename TX, typename TO, int V, int E> bool bwd_ring(Bwd
     const size_t second = P.C * sizeof(TD);
     if (!ring_shape(r, kBwdRingBytes, P.C, E, kBwdThreads, second + P.C * sizeof(TX), second, sizeof(float) * P.C)) return false;
     P.T = r.T;
-    P.parts = (int)std::min<long long>((P.M + r.teams - 1) / r.teams, std::min(dev.sm_count, kPartBlocks));
-    // at most 512 threads of 32 columns: 128 KB
-    r.smem = std::max<size_t>(r.smem, r.teams > 1 ? r.teams * 2 * sizeof(float) * P.C : 0);
+    P.parts = (int)std::min<long long>(P.M, std::min(dev.sm_count, kPartBlocks));
     const int filled = P.C == (long long)r.T * E ? r.T : 0;
     rc = filled == 512 ? launch_bwd_ring<TD, TX, TO, V, E, 512>(P, r, dev, s) : launch_bwd_ring<TD, TX, TO, V, E, 0>(P, r, dev, s);
     return true;
