@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(fwd_ring_threads<E>(), 1) norm_fwd_ring_kernel
     uint32_t ph = 0;
     for (long long r = first; r < P.M; r += step) {
         // a wait that ran out is no row: its results are NaNs
-        const bool ok = mbar_wait(&full[team][s], ph, &gave_up, nullptr, 0);
+        const bool ok = row_is_there(&full[team][s], ph, &gave_up);
         const TX *const row = reinterpret_cast<const TX *>(mine + (size_t)s * R.stage_bytes);
         two_f32 d[P2], s2 = 0, q2 = 0;
         {
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(fwd_ring_threads<E>(), 1) norm_fwd_ring_kernel
         else team_sum(sum, T, red, turn, barrier);
         // the whole team has its elements: the stage is free
         if (T == 32) __syncwarp();
-        if (t == 0) issue(r + R.stages * step, s);
+        if (t == 0 && ok) issue(r + R.stages * step, s);
         const float mean = sum[0] * inv;
         const two_f32 minus = two(-mean, -mean);
 #pragma unroll
@@ -215,6 +215,7 @@ __global__ void __launch_bounds__(fwd_ring_threads<E>(), 1) norm_fwd_ring_kernel
         }
         if (++s == R.stages) { s = 0; ph ^= 1u; }
     }
+    leave_rows(&gave_up);
 }
 
 // Rows longer than the registers of a block: the row is read three times, from L2 after the first.

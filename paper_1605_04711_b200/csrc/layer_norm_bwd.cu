@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
     for (long long r = first; r < P.M; r += step) {
         const float mean = n_mean, rstd = n_rstd;
         if (r + step < P.M) { n_mean = P.mean[r + step]; n_rstd = P.rstd[r + step]; }
-        const bool ok = mbar_wait(&full[s], ph, &gave_up, nullptr, 0);
+        const bool ok = row_is_there(&full[s], ph, &gave_up);
         const uint8_t *const st = stages + (size_t)s * R.stage_bytes;
         const TX *const x = reinterpret_cast<const TX *>(st + R.second);
         const TD *const dy = reinterpret_cast<const TD *>(st);
@@ -310,11 +310,12 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
                 s1 = fma2(g[i], d[i], s1);
             }
         }
+        if (!ok) drop_sums(a_g, a_b);
         float sums[2] = {sum2(s0), ok ? sum2(s1) : __uint_as_float(0x7FC00000u)};
         if constexpr (TT > 0) team_sum<TT>(sums, red, turn, 0);
         else team_sum(sums, T, red, turn, 0);
         // the whole team has left the row before this one: its stage is free
-        if (t == 0 && r != first) issue(r + (R.stages - 1) * step, s == 0 ? R.stages - 1 : s - 1);
+        if (t == 0 && r != first && ok) issue(r + (R.stages - 1) * step, s == 0 ? R.stages - 1 : s - 1);
         if (P.dX) {
             const float c0 = -sums[0] * inv, c1 = -sums[1] * inv * rstd * rstd;
             const two_f32 k0 = two(c0, c0), k1 = two(c1, c1);
@@ -334,6 +335,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
         }
         if (++s == R.stages) { s = 0; ph ^= 1u; }
     }
+    leave_rows(&gave_up);
     if (P.part == nullptr) return;
     float g[E], b[E];
 #pragma unroll

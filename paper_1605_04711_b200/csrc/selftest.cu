@@ -6,6 +6,7 @@
 // point executes it on purpose, with a short limit, on a barrier that nothing ever arrives on.  Nothing here
 // faults or waits without bound.
 #include "common.cuh"
+#include "layer_norm.cuh"
 #include "tc_ptx.cuh"
 
 namespace {
@@ -38,7 +39,42 @@ wait_timeout_kernel(int32_t *status, unsigned long long limit_ns, int *order)
     if (threadIdx.x == 0) order[3] = abort_flag;
 }
 
+// Rows of a layer norm: two waits on such a barrier, of which the second ends soon, and the sums that they have spoilt.
+__global__ void __launch_bounds__(64) row_wait_kernel(float *sums, int *waits, unsigned long long limit_ns)
+{
+    __shared__ unsigned long long bar;
+    __shared__ volatile int gave_up;
+    if (threadIdx.x == 0) {
+        mbar_init(&bar, 1);
+        gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    two_f32 a[2] = {two(1.0f, 2.0f), two(3.0f, 4.0f)}, b[2] = {two(5.0f, 6.0f), two(7.0f, 8.0f)};
+    for (int row = 0; row < 2; ++row) {
+        const bool ok = row_is_there(&bar, 0, &gave_up, limit_ns);
+        if (!ok) drop_sums(a, b);
+        waits[2 * threadIdx.x + row] = ok ? 1 : 0;
+        for (int i = 0; i < 2; ++i) { a[i] = add2(a[i], two(1.0f, 1.0f)); b[i] = add2(b[i], two(1.0f, 1.0f)); }
+    }
+    leave_rows(&gave_up);
+    float *const out = sums + 8 * threadIdx.x;
+    for (int i = 0; i < 2; ++i) { each(a[i], out[2 * i], out[2 * i + 1]); each(b[i], out[4 + 2 * i], out[4 + 2 * i + 1]); }
+}
+
 }  // namespace
+
+// dev_sums: device float[64][8], the column sums of 64 threads; dev_waits: device int[64][2], whether their waits reported success.
+extern "C" int twn_selftest_row_wait(float *dev_sums, int *dev_waits, unsigned long long limit_ns, twn_stream_t stream)
+{
+    TWN_REQUIRE(dev_sums && dev_waits && limit_ns > 0 && limit_ns <= 100000000ull, TWN_ERR_INVALID_ARG);
+    twn_device_info dev;
+    const int rc = twn_current_device(&dev);
+    if (rc != TWN_OK) return rc;
+    row_wait_kernel<<<1, 64, 0, twn_cu(stream)>>>(dev_sums, dev_waits, limit_ns);
+    TWN_CUDA_OK(cudaGetLastError());
+    return TWN_OK;
+}
 
 // dev_status: device int32, zero before the call; receives TWN_ERR_TIMEOUT.  dev_out: device int[4]: whether
 // each of the three waits reported success (all 0) and the block's abort flag (1).
