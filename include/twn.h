@@ -626,6 +626,8 @@ int twn_act_bwd(const void *dY, const void *Y, const float *scale, int64_t n, in
  *   X      TWN_F32 or TWN_BF16 (x_dtype) [M, ldx], ldx >= C;  Y likewise (y_dtype, ldy); both aligned to their
  *          element.  Y may be X itself (same type and pitch).  Columns C.. of Y's rows are not touched.
  *   gamma, beta   fp32 [C] or NULL (1, 0);  mean, rstd  fp32 [M] outputs for the backward pass, or NULL.
+ *   What the call writes lies apart from all else that it reads or writes, but for Y in the place of X (else TWN_ERR_INVALID_ARG); rows of
+ *   one buffer that lie between each other's are apart.
  *   1 <= C <= 2^31, eps >= 0.  M = 0 is fine and launches nothing.
  * Arithmetic is fp32, the variance that of the differences from the mean, each output rounded once.  A row with a NaN
  * or an infinity gives NaNs in that row alone.  With eps = 0 a row of equal values gives NaNs (0 * inf).
@@ -645,7 +647,8 @@ int twn_layer_norm_fwd(const void *X, int32_t x_dtype, int64_t ldx, int64_t M, i
  *   gamma      fp32 [C] or NULL (1);  mean, rstd  fp32 [M], what twn_layer_norm_fwd wrote.
  *   residual   type and pitch of dX, or NULL: a second branch of the gradient (the shortcut around a block that begins
  *              with the norm), added before the rounding; may be dX itself.
- *   dX, dgamma, dbeta (fp32 [C]) are overwritten; each may be NULL.  M = 0 gives zero gradients.
+ *   dX, dgamma, dbeta (fp32 [C]) are overwritten; each may be NULL.  M = 0 gives zero gradients.  What the call writes, its workspace
+ *              too, lies apart from all else, as above, but for dX in the place of dY, X or residual.
  *   workspace  at least twn_layer_norm_bwd_workspace_bytes(M, C) bytes, 256-byte aligned; contents need not be
  *              preserved or initialised.  Two calls that overlap on the device must not share it.
  * The sums over the rows are fp32, split by M and C and added in a fixed order (deterministic).

@@ -369,6 +369,12 @@ extern "C" int twn_layer_norm_fwd(const void *X, int32_t x_dtype, int64_t ldx, i
     for (const void *p : {(const void *)gamma, (const void *)beta, (const void *)mean, (const void *)rstd})
         TWN_REQUIRE(twn_aligned(p, 4), TWN_ERR_MISALIGNED);
     if (M == 0) return TWN_OK;
+    Places places;
+    places.matrix(Y, y_dtype, ldy, M, C, true);
+    places.matrix(X, x_dtype, ldx, M, C, false);
+    for (const void *p : {(const void *)gamma, (const void *)beta}) places.vector(p, 4 * C, false);
+    for (const void *p : {(const void *)mean, (const void *)rstd}) places.vector(p, 4 * M, true);
+    TWN_REQUIRE(places.apart(), TWN_ERR_INVALID_ARG);
     twn_device_info dev;
     rc = twn_current_device(&dev);
     if (rc != TWN_OK) return rc;

@@ -19,6 +19,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdint>
 
 #include <cuda_bf16.h>
 
@@ -337,6 +338,60 @@ int check_matrix(const void *p, int dtype, long long ld, long long M, long long 
     TWN_REQUIRE(M == 0 || ld <= (1ll << 58) / M, TWN_ERR_TOO_LARGE);
     return TWN_OK;
 }
+// Bytes that a call reads or writes: `rows` runs of `width`, `pitch` apart.
+struct Place {
+    long long begin, pitch, width, rows;
+    long long end() const { return begin + (rows - 1) * pitch + width; }
+};
+Place place_of(const void *p, int dtype, long long ld, long long M, long long C)
+{
+    const long long size = (long long)size_of(dtype), at = (long long)reinterpret_cast<uintptr_t>(p);
+    if (ld == C || M == 1) return {at, M * C * size, M * C * size, 1};
+    return {at, ld * size, C * size, M};
+}
+Place place_of(const void *p, long long bytes) { return {(long long)reinterpret_cast<uintptr_t>(p), bytes, bytes, 1}; }
+// Whether two of them share a byte.  Of a's rows the first 64 that reach b are looked at: with one pitch, or where b is one run, two of them
+// tell; rows of two pitches that meet only further down are the caller's to avoid.
+bool meet(const Place &a, const Place &b)
+{
+    if (a.begin >= b.end() || b.begin >= a.end()) return false;
+    const long long first = std::max(0ll, (b.begin - a.begin - a.width + a.pitch) / a.pitch);
+    for (long long i = first; i < std::min(first + 64, a.rows); ++i) {
+        const long long lo = a.begin + i * a.pitch, hi = lo + a.width;
+        // the first row of b that ends behind lo
+        const long long j = lo < b.begin + b.width ? 0 : (lo - b.begin - b.width) / b.pitch + 1;
+        if (j < b.rows && b.begin + j * b.pitch < hi) return true;
+    }
+    return false;
+}
+// What a call writes lies apart from all else that it reads and writes, but for a matrix of the same place, type and pitch.
+struct Places {
+    struct One {
+        Place at;
+        int dtype;               // -1: not a matrix
+        bool written;
+    } all[12];
+    int n = 0;
+    void matrix(const void *p, int dtype, long long ld, long long M, long long C, bool written)
+    {
+        if (p) all[n++] = {place_of(p, dtype, ld, M, C), dtype, written};
+    }
+    void vector(const void *p, long long bytes, bool written)
+    {
+        if (p) all[n++] = {place_of(p, bytes), -1, written};
+    }
+    bool apart() const
+    {
+        for (int i = 0; i < n; ++i)
+            for (int j = i + 1; j < n; ++j) {
+                const One &a = all[i], &b = all[j];
+                if (!a.written && !b.written) continue;
+                const bool same = a.dtype >= 0 && a.dtype == b.dtype && a.at.begin == b.at.begin && a.at.pitch == b.at.pitch && a.at.width == b.at.width;
+                if (!same && meet(a.at, b.at)) return false;
+            }
+        return true;
+    }
+};
 // Rows whose runs of V elements are aligned to their loads (of 16 bytes at most).
 bool vector_rows(const void *p, int dtype, long long ld, int V)
 {

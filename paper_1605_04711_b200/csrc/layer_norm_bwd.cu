@@ -600,6 +600,18 @@ extern "C" int twn_layer_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy
     TWN_REQUIRE(twn_aligned(workspace, 256), TWN_ERR_MISALIGNED);
     const bool sums = dgamma != nullptr || dbeta != nullptr;
     if (M == 0 && !sums) return TWN_OK;
+    Places places;
+    if (M > 0) {
+        places.matrix(dX, dx_dtype, lddx, M, C, true);
+        places.matrix(dY, dy_dtype, lddy, M, C, false);
+        places.matrix(X, x_dtype, ldx, M, C, false);
+        places.matrix(residual, dx_dtype, lddx, M, C, false);
+        for (const void *p : {(const void *)mean, (const void *)rstd}) places.vector(p, 4 * M, false);
+    }
+    places.vector(gamma, 4 * C, false);
+    for (const void *p : {(const void *)dgamma, (const void *)dbeta}) places.vector(p, 4 * C, true);
+    places.vector(workspace, (long long)twn_layer_norm_bwd_workspace_bytes(M, C), true);
+    TWN_REQUIRE(places.apart(), TWN_ERR_INVALID_ARG);
     twn_device_info dev;
     rc = twn_current_device(&dev);
     if (rc != TWN_OK) return rc;
