@@ -263,7 +263,7 @@ int twn_ternarize_codes_batch(const twn_ternarize_item_t *items, int count, void
  *   items      HOST array of up to 32 matrices, read during the call only; their tiles share the launches.
  *     G        TWN_F32 or TWN_BF16 [rows, cols], contiguous;  O likewise, its own type; both aligned to their element.
  *              O may be G (same type).  An empty matrix is skipped.  min(rows, cols) <= 32768, max <= 2^24.
- *              The matrices are worked on at the same time: an O that overlaps anything else is refused (TWN_ERR_INVALID_ARG).
+ *              The matrices are worked on at the same time: an O, or a workspace, that overlaps anything else is refused (TWN_ERR_INVALID_ARG).
  *   steps      1 .. 32;  eps  1e-30 .. 1e30 (1e-7 is usual).
  *   workspace  at least twn_orthogonalize_workspace_bytes(items, count) bytes (only rows and cols are read; 0 for shapes that
  *              the call refuses), 256-byte aligned; contents need not be preserved or initialised.  Two calls that overlap on

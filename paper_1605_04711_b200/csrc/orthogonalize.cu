@@ -1285,7 +1285,7 @@ struct Extent {
     bool written;
 };
 struct Extents {
-    Extent e[3 * kMaxItems];
+    Extent e[3 * kMaxItems + 1];
     int n = 0;
     void add(const void *p, size_t bytes, bool written) { e[n++] = {static_cast<const char *>(p), static_cast<const char *>(p) + bytes, written}; }
     bool apart()
@@ -1410,6 +1410,7 @@ extern "C" int twn_orthogonalize_batch(const twn_orthogonalize_item_t *items, in
     if (P.count == 0) return TWN_OK;
     P.eps = (float)eps;
     P.status = dev_status;
+    extents.add(workspace, need, true);
     return run_steps(P, steps, static_cast<char *>(workspace), need, extents, twn_cu(stream));
 }
 
@@ -1466,6 +1467,7 @@ extern "C" int twn_muon_update_batch(const twn_muon_item_t *items, int count, fl
     P.look_ahead = look_ahead;
     P.status = dev_status;
     if (P.count > 0) {
+        extents.add(workspace, need, true);
         const int rc = run_steps(P, steps, static_cast<char *>(workspace), need, extents, twn_cu(stream));
         if (rc != TWN_OK) return rc;
     }
