@@ -630,7 +630,8 @@ int twn_act_bwd(const void *dY, const void *Y, const float *scale, int64_t n, in
  *   one buffer that lie between each other's are apart.
  *   1 <= C <= 2^31, eps >= 0.  M = 0 is fine and launches nothing.
  * Arithmetic is fp32, the variance that of the differences from the mean, each output rounded once.  A row with a NaN
- * or an infinity gives NaNs in that row alone.  With eps = 0 a row of equal values gives NaNs (0 * inf).
+ * or an infinity gives NaNs in that row alone.  With eps = 0 a row of equal values gives NaNs (0 * inf).  The squares of
+ * the differences are fp32 as well: where their sum passes 3.4e38 (differences of 1e18 and more) rstd is 0.
  * Rows on their way to a kernel are waited for a second at most; one that has not come by then gives NaNs, as do the rows after it in
  * its block (and in the backward pass dgamma and dbeta).  Deterministic; M and C choose the kernel, so a row may be rounded differently in batches of different size.  Rows and
  * bases on 16-byte boundaries, C % 8 == 0 and 16-byte aligned gamma and beta take the fast path.

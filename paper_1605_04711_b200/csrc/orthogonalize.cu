@@ -1100,7 +1100,8 @@ struct Shape {
     bool fits, sym_pair, apply_pair;
 };
 constexpr int64_t kMaxShort = 32768, kMaxLong = 1 << 24, kPairLong = 1 << 17;
-// How a matrix is served goes by its own sizes alone, so it has the same bits in every batch.
+// How a matrix is served goes by its own sizes and by whether all matrices of the call are small (all_small), not by the others' sizes or
+// number, so it has the same bits in every other batch.
 Shape shape_of(int64_t rows, int64_t cols)
 {
     Shape s = {};

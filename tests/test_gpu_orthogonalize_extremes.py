@@ -98,3 +98,12 @@ def test_the_largest_square():
             assert d <= 8 * 1e-3 * total / k
             lost += d * d
     assert lost ** 0.5 <= 1e-3 * total
+
+
+def test_small_ones_have_the_same_bits_beside_any_larger_one():
+    """Not those that they have in a call of small matrices alone, which goes another way."""
+    small = [_matrix("any", r, c) for r, c in ((64, 576), (1, 33), (300, 4), (128, 8192))]
+    first = _run(small + [_matrix("any", 300, 300)])
+    for other in ([_matrix("any", 1000, 513)], [_matrix("any", 129, 40000), _matrix("any", 2820, 2900)]):
+        for O, want in zip(_run(small + other), first[:4]):
+            assert torch.equal(O, want)
