@@ -218,7 +218,8 @@ __global__ void __launch_bounds__(fwd_ring_threads<E>(), 1) norm_fwd_ring_kernel
     leave_rows(&gave_up);
 }
 
-// Rows longer than the registers of a block: the row is read three times, from L2 after the first.
+// Rows longer than the registers of a block: the row is read three times, from L2 after the first.  A thread adds its vectors' sums in fp64, so that the
+// row's sums are as good as those of shorter rows however many they are (in fp32 rows of 2^22 to 2^27 had 1 / deviation off by 5e-6 to 3.5e-5).
 template <typename TX, typename TY, int V>
 __global__ void __launch_bounds__(1024) norm_fwd_long_kernel(const __grid_constant__ FwdParams P)
 {
@@ -228,24 +229,32 @@ __global__ void __launch_bounds__(1024) norm_fwd_long_kernel(const __grid_consta
     pdl_begin();
     for (long long r = blockIdx.x; r < P.M; r += gridDim.x) {
         const TX *x = static_cast<const TX *>(P.X) + r * P.ldx;
-        float s[1] = {0.0f}, f[V];
+        float s[1], f[V];
+        double total = 0.0;
         for (long long col = (long long)threadIdx.x * V; col < P.C; col += 1024 * V) {
             Vec<TX, V> v;
             v.load(x + col);
             v.get(f);
+            float v_sum = f[0];
 #pragma unroll
-            for (int i = 0; i < V; ++i) s[0] += f[i];
+            for (int i = 1; i < V; ++i) v_sum += f[i];
+            total += (double)v_sum;
         }
+        s[0] = (float)total;
         team_sum(s, 1024, red, turn, 0);
         const float mean = s[0] * inv;
-        float q[1] = {0.0f};
+        float q[1];
+        total = 0.0;
         for (long long col = (long long)threadIdx.x * V; col < P.C; col += 1024 * V) {
             Vec<TX, V> v;
             v.load(x + col);
             v.get(f);
+            float v_sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) q[0] = fmaf(f[i] - mean, f[i] - mean, q[0]);
+            for (int i = 0; i < V; ++i) v_sum = fmaf(f[i] - mean, f[i] - mean, v_sum);
+            total += (double)v_sum;
         }
+        q[0] = (float)total;
         team_sum(q, 1024, red, turn, 0);
         const float rstd = rsqrtf(fmaf(q[0], inv, P.eps));
         TY *y = static_cast<TY *>(P.Y) + r * P.ldy;

@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_bwd_ring_kernel(const __g
     join_sums<V>(g, b, col, true, 0, 1, nullptr, P.part + (long long)blockIdx.x * 2 * C);
 }
 
-// Long rows, first pass: sum(g) / C and sum(g xh) / C of every row.
+// Long rows, first pass: sum(g) / C and sum(g xh) / C of every row, a thread's vectors added in fp64 (see norm_fwd_long_kernel).
 template <typename TD, typename TX, int V>
 __global__ void __launch_bounds__(kBwdThreads) norm_bwd_sums_kernel(const __grid_constant__ BwdParams P)
 {
@@ -355,11 +355,11 @@ __global__ void __launch_bounds__(kBwdThreads) norm_bwd_sums_kernel(const __grid
         const TD *dy = static_cast<const TD *>(P.dY) + r * P.lddy;
         const TX *xr = static_cast<const TX *>(P.X) + r * P.ldx;
         const float mean = P.mean[r], rstd = P.rstd[r];
-        float s[2] = {0.0f, 0.0f};
+        double total[2] = {0.0, 0.0};
         for (long long col = (long long)threadIdx.x * V; col < P.C; col += kBwdThreads * V) {
             Vec<TD, V> vd;
             Vec<TX, V> vx;
-            float d[V], x[V], ga[V];
+            float d[V], x[V], ga[V], v_sum[2] = {0.0f, 0.0f};
             vd.load(dy + col);
             vx.load(xr + col);
             vd.get(d);
@@ -368,10 +368,13 @@ __global__ void __launch_bounds__(kBwdThreads) norm_bwd_sums_kernel(const __grid
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float g = d[i] * ga[i];
-                s[0] += g;
-                s[1] = fmaf(g, (x[i] - mean) * rstd, s[1]);
+                v_sum[0] += g;
+                v_sum[1] = fmaf(g, (x[i] - mean) * rstd, v_sum[1]);
             }
+            total[0] += (double)v_sum[0];
+            total[1] += (double)v_sum[1];
         }
+        float s[2] = {(float)total[0], (float)total[1]};
         team_sum(s, kBwdThreads, red, turn, 0);
         if (threadIdx.x == 0) {
             P.row_sums[2 * r] = s[0] * inv;
