@@ -1,6 +1,8 @@
 // Group norm with an activation, forward (see group_norm.cuh).
 #include "group_norm.cuh"
 
+#include <type_traits>
+
 namespace {
 
 // Of some values of a group: their sum less that of as many references, the sum of squares of their differences from their mean, their count.
@@ -208,15 +210,25 @@ template <int V, typename Write> __device__ __forceinline__ void join_groups(con
     }
 }
 
-template <int ACT> __device__ __forceinline__ two_f32 activate(two_f32 z)
+// Of two channels of J pixels.  (SiLU below -43 is what it is there, -9e-18.)
+template <int ACT, int J> __device__ __forceinline__ void activate(two_f32 (&z)[J])
 {
-    if (ACT == kRelu) return at_least2(z, 0.0f);
+    if (ACT != kNone)
+#pragma unroll
+        for (int j = 0; j < J; ++j) z[j] = at_least2(z[j], ACT == kRelu ? 0.0f : kLeastZ);
     if (ACT == kSilu) {
-        // (below -43 it is what it is there, -9e-18)
-        z = at_least2(z, kLeastZ);
-        return mul2(z, sigmoid2(z));
+        two_f32 e[J], f[J];
+        sigmoids(z, e, f);
+#pragma unroll
+        for (int j = 0; j < J; ++j) z[j] = mul2(z[j], f[j]);
     }
-    return z;
+}
+// Of one channel of two pixels.
+__device__ __forceinline__ two_f32 silu(two_f32 z)
+{
+    two_f32 e;
+    z = at_least2(z, kLeastZ);
+    return mul2(z, sigmoid2(z, e));
 }
 
 // (gamma and beta may lie on any multiple of four bytes)
@@ -258,14 +270,31 @@ template <int V> struct Affine {
             b[i] = two(be[2 * i < V ? 2 * i : 0], be[j]);
         }
     }
-    template <int ACT> __device__ __forceinline__ void operator()(const float (&x)[V], float (&y)[V]) const
+    // Of J pixels.
+    template <int ACT, int J, typename TX> __device__ __forceinline__ void operator()(const Vec<TX, V> (&v)[J], float (&y)[J][V]) const
     {
+        float x[J][V];
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            float y0, y1;
-            each(activate<ACT>(fma2(add2(two(x[2 * i < V ? 2 * i : 0], x[V > 1 ? 2 * i + 1 : 0]), m[i]), a[i], b[i])), y0, y1);
-            y[2 * i < V ? 2 * i : 0] = y0;
-            if (V > 1) y[V > 1 ? 2 * i + 1 : 0] = y1;
+        for (int j = 0; j < J; ++j) v[j].get(x[j]);
+        if constexpr (V == 1 && J == 2) {
+            // (one channel: the two pixels are a pair)
+            each(silu(fma2(add2(two(x[0][0], x[1][0]), m[0]), a[0], b[0])), y[0][0], y[1][0]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const int l = 2 * i < V ? 2 * i : 0, h = V > 1 ? 2 * i + 1 : 0;
+                two_f32 z[J];
+#pragma unroll
+                for (int j = 0; j < J; ++j) z[j] = fma2(add2(two(x[j][l], x[j][h]), m[i]), a[i], b[i]);
+                activate<ACT, J>(z);
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    float y0, y1;
+                    each(z[j], y0, y1);
+                    y[j][l] = y0;
+                    if (V > 1) y[j][h] = y1;
+                }
+            }
         }
     }
 };
@@ -295,15 +324,21 @@ __device__ __forceinline__ void apply_tile(const GnFwd &P, const Tile<V> &t, con
 {
     TY *y = static_cast<TY *>(P.Y) + (t.b * P.cut.HW + t.first + t.ty) * P.ldy + t.channel();
     const long long step = t.R * P.ldy;
-#pragma unroll 4
-    for (int i = 0; i < t.n; ++i) {
-        Vec<TX, V> v;
-        float x[V], o[V];
-        v.load(slots + i * (kGnThreads * V));
-        v.get(x);
-        affine.template operator()<ACT>(x, o);
-        store(y + i * step, o);
-    }
+    constexpr int J = kAtOnce<ACT>;
+    auto work = [&](int i, auto pixels) {
+        constexpr int n = decltype(pixels)::value;
+        Vec<TX, V> v[n];
+        float o[n][V];
+#pragma unroll
+        for (int j = 0; j < n; ++j) v[j].load(slots + (i + j) * (kGnThreads * V));
+        affine.template operator()<ACT, n>(v, o);
+#pragma unroll
+        for (int j = 0; j < n; ++j) store(y + (i + j) * step, o[j]);
+    };
+    int i = 0;
+#pragma unroll (4 / J)
+    for (; i + J <= t.n; i += J) work(i, std::integral_constant<int, J>());
+    if (J > 1 && i < t.n) work(i, std::integral_constant<int, 1>());
 }
 
 // 64 x 12544 x 64 bf16 with a ReLU in 51 us, 4.0 TB/s: bound by latency.  Two blocks of 8 warps an SM issue on 40 % of the cycles, and half of what they issue joins sums; a
@@ -445,25 +480,26 @@ __device__ __forceinline__ void apply_rows(const GnFwd &P, const Tile<V> &t, con
     const TX *x = static_cast<const TX *>(P.X) + (t.b * P.cut.HW + t.first + t.ty) * P.ldx + t.channel();
     TY *y = static_cast<TY *>(P.Y) + (t.b * P.cut.HW + t.first + t.ty) * P.ldy + t.channel();
     const long long in = t.R * P.ldx, out = t.R * P.ldy;
+    constexpr int J = kAtOnce<ACT>;
     int i = 0;
-    float f[V], o[V];
     for (; i + 8 <= t.n; i += 8) {
-        Vec<TX, V> w[8];
+        Vec<TX, V> w[8 / J][J];
+        float o[J][V];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j].load(x + (i + j) * in);
+        for (int j = 0; j < 8; ++j) w[j / J][j % J].load(x + (i + j) * in);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            w[j].get(f);
-            affine.template operator()<ACT>(f, o);
-            store(y + (i + j) * out, o);
+        for (int j = 0; j < 8; j += J) {
+            affine.template operator()<ACT, J>(w[j / J], o);
+#pragma unroll
+            for (int k = 0; k < J; ++k) store(y + (i + j + k) * out, o[k]);
         }
     }
     for (; i < t.n; ++i) {
-        Vec<TX, V> v;
-        v.load(x + i * in);
-        v.get(f);
-        affine.template operator()<ACT>(f, o);
-        store(y + i * out, o);
+        Vec<TX, V> v[1];
+        float o[1][V];
+        v[0].load(x + i * in);
+        affine.template operator()<ACT, 1>(v, o);
+        store(y + i * out, o[0]);
     }
 }
 template <typename TX, typename TY, int V>

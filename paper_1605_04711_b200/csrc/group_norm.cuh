@@ -188,7 +188,7 @@ template <int V> __device__ __forceinline__ void load_floats(float (&f)[V], cons
     }
 }
 
-// 1 / (1 + exp(-z)) of two numbers of at least -43, so that one reciprocal serves both.
+// SiLU of z below this counts as that of this.
 constexpr float kLeastZ = -43.0f, kMinusLog2e = -1.4426950408889634f;
 __device__ __forceinline__ float ex2(float x)
 {
@@ -209,12 +209,35 @@ __device__ __forceinline__ float at_least(float x, float least)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(least));
     return r;
 }
-__device__ __forceinline__ two_f32 sigmoid2(two_f32 z)
+// Pixels that are worked on at once: SiLU's reciprocals serve two.
+template <int ACT> constexpr int kAtOnce = ACT == kSilu ? 2 : 1;
+// exp(-z) and 1 / (1 + exp(-z)) of two neighbouring channels of J pixels, z at least kLeastZ.  One reciprocal serves a channel of two pixels, whose z are NaN together, and never two
+// channels, which may be of different groups.  (One for each z: 64 x 3136 x 256 bf16 in 57.4 us for 54.9.)
+template <int J> __device__ __forceinline__ void sigmoids(const two_f32 (&z)[J], two_f32 (&e)[J], two_f32 (&f)[J])
 {
-    float t0, t1;
+    two_f32 s[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        float t0, t1;
+        each(mul2(z[j], two(kMinusLog2e, kMinusLog2e)), t0, t1);
+        e[j] = two(ex2(t0), ex2(t1));
+        s[j] = add2(e[j], two(1.0f, 1.0f));
+    }
+    float p0, p1;
+    each(J == 2 ? mul2(s[0], s[J - 1]) : s[0], p0, p1);
+    f[0] = two(reciprocal(p0), reciprocal(p1));
+    if (J == 2) {
+        f[J - 1] = mul2(f[0], s[0]);
+        f[0] = mul2(f[0], s[J - 1]);
+    }
+}
+// Of one channel of two pixels.
+__device__ __forceinline__ two_f32 sigmoid2(two_f32 z, two_f32 &e)
+{
+    float t0, t1, s0, s1;
     each(mul2(z, two(kMinusLog2e, kMinusLog2e)), t0, t1);
-    float s0, s1;
-    each(add2(two(ex2(t0), ex2(t1)), two(1.0f, 1.0f)), s0, s1);
+    e = two(ex2(t0), ex2(t1));
+    each(add2(e, two(1.0f, 1.0f)), s0, s1);
     const float r = reciprocal(s0 * s1);
     return two(r * s1, r * s0);
 }

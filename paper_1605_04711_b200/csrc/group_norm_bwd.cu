@@ -1,6 +1,8 @@
 // Group norm with an activation, backward (see group_norm.cuh).
 #include "group_norm.cuh"
 
+#include <type_traits>
+
 namespace {
 
 struct GnBwd {
@@ -108,22 +110,26 @@ __device__ __noinline__ bool positive_z(const GnBwd &p, long long b, int c, floa
     return xh * (p.gamma ? (double)p.gamma[c] : 1.0) + (p.beta ? (double)p.beta[c] : 0.0) > 0.0;
 }
 
-// Pairs of a thread's vector: dz and the differences from the mean.
-template <typename TD, typename TX, int V, int ACT>
-__device__ __forceinline__ void vector_dz(const GnBwd &p, const Tile<V> &t, const Channels<V> &ch, const Vec<TD, V> &vd, const Vec<TX, V> &vx,
-                                          two_f32 (&dz)[Channels<V>::P], two_f32 (&d)[Channels<V>::P])
+// Pairs of a thread's vectors of J pixels: dz and the differences from the mean.
+template <typename TD, typename TX, int V, int ACT, int J>
+__device__ __forceinline__ void vector_dz(const GnBwd &p, const Tile<V> &t, const Channels<V> &ch, const Vec<TD, V> (&vd)[J], const Vec<TX, V> (&vx)[J],
+                                          two_f32 (&dz)[J][Channels<V>::P], two_f32 (&d)[J][Channels<V>::P])
 {
-    float dy[V], x[V];
-    vd.get(dy);
-    vx.get(x);
-    float z[V];
-    if (ACT == kRelu) {
+    float dy[J][V], x[J][V];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        vd[j].get(dy[j]);
+        vx[j].get(x[j]);
+    }
+    if constexpr (ACT == kRelu) {
+        static_assert(J == 1, "");
+        float z[V];
         bool doubt = false;
 #pragma unroll
         for (int i = 0; i < Channels<V>::P; ++i) {
             const int l = 2 * i < V ? 2 * i : 0, h = V > 1 ? 2 * i + 1 : 0;
             float lo, hi;
-            each(fma2(add2(two(x[l], V > 1 ? x[h] : 0.0f), ch.m[i]), ch.a[i], ch.b[i]), lo, hi);
+            each(fma2(add2(two(x[0][l], V > 1 ? x[0][h] : 0.0f), ch.m[i]), ch.a[i], ch.b[i]), lo, hi);
             z[l] = lo;
             if (V > 1) z[h] = hi;
         }
@@ -132,27 +138,71 @@ __device__ __forceinline__ void vector_dz(const GnBwd &p, const Tile<V> &t, cons
         if (doubt)
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (fabsf(z[i]) < ch.doubt) z[i] = positive_z(p, t.b, t.channel() + i, x[i]) ? 1.0f : 0.0f;
+                if (fabsf(z[i]) < ch.doubt) z[i] = positive_z(p, t.b, t.channel() + i, x[0][i]) ? 1.0f : 0.0f;
         // (a NaN goes on)
 #pragma unroll
-        for (int i = 0; i < V; ++i) dy[i] = z[i] > 0.0f ? dy[i] : at_least(z[i], 0.0f);
+        for (int i = 0; i < V; ++i) dy[0][i] = z[i] > 0.0f ? dy[0][i] : at_least(z[i], 0.0f);
     }
 #pragma unroll
     for (int i = 0; i < Channels<V>::P; ++i) {
         const int l = 2 * i < V ? 2 * i : 0, h = V > 1 ? 2 * i + 1 : 0;
-        d[i] = add2(two(x[l], V > 1 ? x[h] : 0.0f), ch.m[i]);
-        dz[i] = two(dy[l], V > 1 ? dy[h] : 0.0f);
-        if (ACT == kSilu) {
-            // dy f (1 + z (1 - f)) = dy f^2 (s + z e),  e = exp(-z), s = 1 + e, f = 1 / s  (below -43 it is next to nothing)
-            const two_f32 z = at_least2(fma2(d[i], ch.a[i], ch.b[i]), kLeastZ);
-            float t0, t1, s0, s1;
-            each(mul2(z, two(kMinusLog2e, kMinusLog2e)), t0, t1);
-            const two_f32 e = two(ex2(t0), ex2(t1)), s = add2(e, two(1.0f, 1.0f));
-            each(s, s0, s1);
-            const float r = reciprocal(s0 * s1);
-            const two_f32 f = two(r * s1, r * s0);
-            dz[i] = mul2(mul2(dz[i], f), mul2(f, fma2(z, e, s)));
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            d[j][i] = add2(two(x[j][l], V > 1 ? x[j][h] : 0.0f), ch.m[i]);
+            dz[j][i] = two(dy[j][l], V > 1 ? dy[j][h] : 0.0f);
         }
+        if constexpr (ACT == kSilu) {
+            // dy f (1 + z (1 - f)) = dy f (1 + z e f),  e = exp(-z), f = 1 / (1 + e)  (below -43 it is next to nothing)
+            if constexpr (V == 1 && J == 2) {
+                // (one channel: the two pixels are a pair)
+                float d0, d1, o0, o1;
+                each(d[0][0], d0, o0);
+                each(d[1][0], d1, o1);
+                const two_f32 z = at_least2(fma2(two(d0, d1), ch.a[0], ch.b[0]), kLeastZ);
+                two_f32 e;
+                const two_f32 f = sigmoid2(z, e);
+                each(mul2(mul2(two(dy[0][0], dy[1][0]), f), fma2(z, mul2(e, f), two(1.0f, 1.0f))), o0, o1);
+                dz[0][0] = two(o0, 0.0f);
+                dz[1][0] = two(o1, 0.0f);
+            } else {
+                two_f32 z[J], e[J], f[J];
+#pragma unroll
+                for (int j = 0; j < J; ++j) z[j] = at_least2(fma2(d[j][i], ch.a[i], ch.b[i]), kLeastZ);
+                sigmoids(z, e, f);
+#pragma unroll
+                for (int j = 0; j < J; ++j) dz[j][i] = mul2(mul2(dz[j][i], f[j]), fma2(z[j], mul2(e[j], f[j]), two(1.0f, 1.0f)));
+            }
+        }
+    }
+}
+
+// Pixels from `begin` to `end` of a thread, which take(i, dY, X) loads: use(i, dz, differences) for each.  PIXELS a turn of the loop.
+template <typename TD, typename TX, int V, int ACT, int PIXELS, typename Take, typename Use>
+__device__ __forceinline__ void pixel_by_pixel(const GnBwd &p, const Tile<V> &t, const Channels<V> &ch, int begin, int end, const Take &take, const Use &use)
+{
+    constexpr int J = kAtOnce<ACT>;
+    auto work = [&](int i, auto pixels) {
+        constexpr int n = decltype(pixels)::value;
+        Vec<TD, V> vd[n];
+        Vec<TX, V> vx[n];
+        two_f32 dz[n][Channels<V>::P], d[n][Channels<V>::P];
+#pragma unroll
+        for (int j = 0; j < n; ++j) take(i + j, vd[j], vx[j]);
+        vector_dz<TD, TX, V, ACT, n>(p, t, ch, vd, vx, dz, d);
+#pragma unroll
+        for (int j = 0; j < n; ++j) use(i + j, dz[j], d[j]);
+    };
+    int i = begin;
+#pragma unroll (PIXELS / J)
+    for (; i + J <= end; i += J) work(i, std::integral_constant<int, J>());
+    if (J > 1 && i < end) work(i, std::integral_constant<int, 1>());
+}
+template <int N> __device__ __forceinline__ void add_sums(two_f32 (&A)[N], two_f32 (&D)[N], const two_f32 (&dz)[N], const two_f32 (&d)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        A[j] = add2(A[j], dz[j]);
+        D[j] = fma2(dz[j], d[j], D[j]);
     }
 }
 
@@ -324,24 +374,14 @@ __device__ __forceinline__ void resident(const GnBwd &P, const Tile<V> &t, const
     constexpr int N = Channels<V>::P;
     const int tiles = P.cut.tiles;
     const Channels<V> ch(P, raw);
-    two_f32 A[N], D[N], dz[N], d[N];
+    two_f32 A[N], D[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) A[i] = D[i] = 0;
-    as_they_come(t.n, 0, [&](int begin, int end) {
-#pragma unroll 2
-        for (int i = begin; i < end; ++i) {
-            Vec<TD, V> vd;
-            Vec<TX, V> vx;
-            vd.load(ds + i * (kGnThreads * V));
-            vx.load(xs + i * (kGnThreads * V));
-            vector_dz<TD, TX, V, ACT>(P, t, ch, vd, vx, dz, d);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                A[j] = add2(A[j], dz[j]);
-                D[j] = fma2(dz[j], d[j], D[j]);
-            }
-        }
-    });
+    auto take = [&](int i, Vec<TD, V> &vd, Vec<TX, V> &vx) {
+        vd.load(ds + i * (kGnThreads * V));
+        vx.load(xs + i * (kGnThreads * V));
+    };
+    as_they_come(t.n, 0, [&](int begin, int end) { pixel_by_pixel<TD, TX, V, ACT, 2>(P, t, ch, begin, end, take, [&](int, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { add_sums<N>(A, D, dz, d); }); });
     if (tiles > 1) wait_for_all();                       // all blocks are there
     // to all blocks of the cluster (without dX to none, which may have ended)
     join_channels(P, t, A, D, at, of, P.dX ? tiles : 0, [&](int g, int kind, int to, float v) {
@@ -362,15 +402,8 @@ __device__ __forceinline__ void resident(const GnBwd &P, const Tile<V> &t, const
         const long long to_at = (t.b * P.cut.HW + t.first + t.ty) * P.lddx + t.channel(), step = t.R * P.lddx;
         TO *to = static_cast<TO *>(P.dX) + to_at;
         const TO *add = P.add ? static_cast<const TO *>(P.add) + to_at : nullptr;
-#pragma unroll 2
-        for (int i = 0; i < t.n; ++i) {
-            Vec<TD, V> vd;
-            Vec<TX, V> vx;
-            vd.load(ds + i * (kGnThreads * V));
-            vx.load(xs + i * (kGnThreads * V));
-            vector_dz<TD, TX, V, ACT>(P, t, ch, vd, vx, dz, d);
-            write_dx<V>(ch, te, dz, d, to + i * step, add ? add + i * step : nullptr);
-        }
+        pixel_by_pixel<TD, TX, V, ACT, 2>(P, t, ch, 0, t.n, take,
+                                 [&](int i, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { write_dx<V>(ch, te, dz, d, to + i * step, add ? add + i * step : nullptr); });
     }
 }
 
@@ -414,31 +447,32 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_bwd_kernel(const __grid_cons
 
 // 131072 pixels of 512 channels, one group, in 175 us: five passes over 134 MB would take 102.
 // ---- two reads ------------------------------------------------------------------------------------------------------------------
-// A thread's pixels from `i` to `end`, four at a time: their loads, then use(i, dY, X) for each.
-template <typename TD, typename TX, int V, typename Use> __device__ __forceinline__ void each_pixel(const GnBwd &P, const Tile<V> &t, int i, int end, Use use)
+// A thread's pixels from `i` to `end`, the loads of four at a time: use(i, dz, differences) for each.
+template <typename TD, typename TX, int V, int ACT, typename Use>
+__device__ __forceinline__ void each_pixel(const GnBwd &P, const Tile<V> &t, const Channels<V> &ch, int i, int end, const Use &use)
 {
+    constexpr int N = Channels<V>::P, J = kAtOnce<ACT>;
     const long long pixel = t.b * P.cut.HW + t.first + t.ty;
     const TD *dy = static_cast<const TD *>(P.dY) + pixel * P.lddy + t.channel();
     const TX *x = static_cast<const TX *>(P.X) + pixel * P.ldx + t.channel();
     const long long step_d = t.R * P.lddy, step_x = t.R * P.ldx;
     for (; i + 4 <= end; i += 4) {
-        Vec<TD, V> vd[4];
-        Vec<TX, V> vx[4];
+        Vec<TD, V> vd[4 / J][J];
+        Vec<TX, V> vx[4 / J][J];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            vd[j].load(dy + (i + j) * step_d);
-            vx[j].load(x + (i + j) * step_x);
+            vd[j / J][j % J].load(dy + (i + j) * step_d);
+            vx[j / J][j % J].load(x + (i + j) * step_x);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) use(i + j, vd[j], vx[j]);
+        for (int j = 0; j < 4; j += J) {
+            two_f32 dz[J][N], d[J][N];
+            vector_dz<TD, TX, V, ACT, J>(P, t, ch, vd[j / J], vx[j / J], dz, d);
+#pragma unroll
+            for (int k = 0; k < J; ++k) use(i + j + k, dz[k], d[k]);
+        }
     }
-    for (; i < end; ++i) {
-        Vec<TD, V> vd;
-        Vec<TX, V> vx;
-        vd.load(dy + i * step_d);
-        vx.load(x + i * step_x);
-        use(i, vd, vx);
-    }
+    pixel_by_pixel<TD, TX, V, ACT, J>(P, t, ch, i, end, [&](int k, Vec<TD, V> &vd, Vec<TX, V> &vx) { vd.load(dy + k * step_d); vx.load(x + k * step_x); }, use);
 }
 template <typename TD, typename TX, int V, int ACT>
 __device__ __forceinline__ void tile_sums(const GnBwd &P, const Tile<V> &t, two_f32 (&A)[Channels<V>::P], two_f32 (&D)[Channels<V>::P])
@@ -449,15 +483,7 @@ __device__ __forceinline__ void tile_sums(const GnBwd &P, const Tile<V> &t, two_
         two_f32 a[N], q[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) a[j] = q[j] = 0;
-        each_pixel<TD, TX, V>(P, t, i, min(t.n, i + kRun), [&](int, const Vec<TD, V> &vd, const Vec<TX, V> &vx) {
-            two_f32 dz[N], d[N];
-            vector_dz<TD, TX, V, ACT>(P, t, ch, vd, vx, dz, d);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                a[j] = add2(a[j], dz[j]);
-                q[j] = fma2(dz[j], d[j], q[j]);
-            }
-        });
+        each_pixel<TD, TX, V, ACT>(P, t, ch, i, min(t.n, i + kRun), [&](int, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { add_sums<N>(a, q, dz, d); });
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             A[j] = add2(A[j], a[j]);
@@ -465,7 +491,7 @@ __device__ __forceinline__ void tile_sums(const GnBwd &P, const Tile<V> &t, two_
         }
     }
 }
-template <typename TD, typename TX, int V> __global__ void __launch_bounds__(kGnThreads) gn_bwd_sums_kernel(const __grid_constant__ GnBwd P)
+template <typename TD, typename TX, int V> __global__ void __launch_bounds__(kGnThreads, 2) gn_bwd_sums_kernel(const __grid_constant__ GnBwd P)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     constexpr int N = Channels<V>::P;
@@ -495,13 +521,9 @@ __device__ __forceinline__ void apply_rows(const GnBwd &P, const Tile<V> &t, con
     const long long at = (t.b * P.cut.HW + t.first + t.ty) * P.lddx + t.channel(), step = t.R * P.lddx;
     TO *to = static_cast<TO *>(P.dX) + at;
     const TO *add = P.add ? static_cast<const TO *>(P.add) + at : nullptr;
-    each_pixel<TD, TX, V>(P, t, 0, t.n, [&](int i, const Vec<TD, V> &vd, const Vec<TX, V> &vx) {
-        two_f32 dz[N], d[N];
-        vector_dz<TD, TX, V, ACT>(P, t, ch, vd, vx, dz, d);
-        write_dx<V>(ch, te, dz, d, to + i * step, add ? add + i * step : nullptr);
-    });
+    each_pixel<TD, TX, V, ACT>(P, t, ch, 0, t.n, [&](int i, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { write_dx<V>(ch, te, dz, d, to + i * step, add ? add + i * step : nullptr); });
 }
-template <typename TD, typename TX, typename TO, int V> __global__ void __launch_bounds__(kGnThreads) gn_bwd_apply_kernel(const __grid_constant__ GnBwd P)
+template <typename TD, typename TX, typename TO, int V> __global__ void __launch_bounds__(kGnThreads, 2) gn_bwd_apply_kernel(const __grid_constant__ GnBwd P)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     const Tile<V> t(P.cut, blockIdx.x);
