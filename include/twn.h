@@ -767,10 +767,10 @@ int twn_layer_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy, const voi
  *   one buffer that lie between each other's are apart.
  *   1 <= C <= 2^20, C % groups = 0, eps >= 0, B and HW at most 2^31, B * HW at most 2^40.  B = 0 or HW = 0 is fine and launches nothing.
  * Arithmetic is fp32, each output rounded once.  The variance is that of differences, joined from parts with their means, never a difference of two
- * large sums.  A group with a NaN or an infinity gives NaNs in that group of that image alone; a NaN stays one through the activation.  With eps = 0
- * a group of equal values gives NaNs (0 * inf).  Deterministic; B, HW, C and groups choose how sums are split, so an image may be rounded
- * differently in batches of different size.  C % 8 == 0 (4 where a type is fp32), bases and pitches on 16-byte boundaries take the fast path, others
- * vectors of four, two or single elements.
+ * large sums.  SiLU takes z below -87 as -87, where it is -1.4e-36.  A group with a NaN or an infinity gives NaNs in that group of that image alone, a NaN in
+ * gamma or beta in its channel; a NaN stays one through the activation.  With eps = 0 a group of equal values gives NaNs (0 * inf).  Deterministic; B, HW, C and
+ * groups choose how sums are split, so an image may be rounded differently in batches of different size.  C % 8 == 0 (4 where a type is fp32), bases and
+ * pitches on 16-byte boundaries take the fast path, others vectors of four, two or single elements.
  */
 enum { TWN_ACT_NONE = 0, TWN_ACT_RELU = 1, TWN_ACT_SILU = 2 };
 size_t twn_group_norm_fwd_workspace_bytes(int64_t B, int64_t HW, int64_t C, int32_t groups);

@@ -210,7 +210,7 @@ template <int V, typename Write> __device__ __forceinline__ void join_groups(con
     }
 }
 
-// Of two channels of J pixels.  (SiLU below -43 is what it is there, -9e-18.)
+// Of two channels of J pixels.
 template <int ACT, int J> __device__ __forceinline__ void activate(two_f32 (&z)[J])
 {
     if (ACT != kNone)

@@ -152,7 +152,7 @@ __device__ __forceinline__ void vector_dz(const GnBwd &p, const Tile<V> &t, cons
             dz[j][i] = two(dy[j][l], V > 1 ? dy[j][h] : 0.0f);
         }
         if constexpr (ACT == kSilu) {
-            // dy f (1 + z (1 - f)) = dy f (1 + z e f),  e = exp(-z), f = 1 / (1 + e)  (below -43 it is next to nothing)
+            // dy f (1 + z (1 - f)) = dy f (1 + z e f),  e = exp(-z), f = 1 / (1 + e)
             if constexpr (V == 1 && J == 2) {
                 // (one channel: the two pixels are a pair)
                 float d0, d1, o0, o1;
