@@ -5,9 +5,11 @@
 
 namespace {
 
-// Of some values of a group: their sum less that of as many references, the sum of squares of their differences from their mean, their count.
+// Of n values of a group: their mean as it is in fp32, their sum less n times that, the sum of squares of their differences from the mean.  Parts are joined by the differences of their
+// means from one of those, which are no larger than what makes them differ: the group's mean keeps its digits however far from zero its values lie, and whichever of them is
+// far from the others.  (Sums in fp64 took as many digits and more time: four conversions a part, 80.2 us for 68.8 of 16 x 65536 x 24 fp32.)
 struct __align__(16) Moments {
-    float sum, m2, n, ref;           // (the reference, where it goes through memory)
+    float c, r, m2, n;
 };
 
 struct GnFwd {
@@ -22,33 +24,46 @@ struct GnFwd {
     float eps;
 };
 
-// Sum and mean (less the reference) and sum of squared differences of a group's values from their parts, which read(e) gives for e < count, in the
-// 2^lg neighbouring lanes that call it (Chan, Golub and LeVeque).  inv: 1 / the count of all.  The sum is taken in fp64: the mean may be far smaller than
-// what it is the mean of.
+// A group's values from their parts, which read(e) gives for e < count, in the 2^lg neighbouring lanes that call it (Chan, Golub and LeVeque): their sum and their mean less `c`, that of
+// the first part, and the sum of squared differences.  inv: 1 / their number.
 struct Joined {
-    double mean;
-    float sum, m2;
+    float c;
+    double sum, mean;
+    float m2;
 };
 template <typename Read> __device__ __forceinline__ Joined join(int lane, int lg, int count, double inv, Read read)
 {
     const int width = 1 << lg;
     Moments held = {0.0f, 0.0f, 0.0f, 0.0f};             // the first of a lane's parts
     if (lane < count) held = read(lane);
-    double s = (double)held.sum;
-    for (int e = lane + width; e < count; e += width) s += (double)read(e).sum;
+    const float c = count > 0 ? read(0).c : 0.0f;
+    auto sum_of = [&](const Moments &a) { return a.n > 0.0f ? (double)fmaf(a.n, a.c - c, a.r) : 0.0; };
+    double s = sum_of(held);
+    for (int e = lane + width; e < count; e += width) s += sum_of(read(e));
     s = all_sum(s, lg);
     const double mean = s * inv;
-    const float c = (float)mean;
+    const float m = (float)mean;
     float m2 = 0.0f;
     auto add = [&](const Moments &a) {
         // n (sum / n - mean)^2
-        const float d = fmaf(-a.n, c, a.sum);
+        const float d = fmaf(a.n, (a.c - c) - m, a.r);
         if (a.n > 0.0f) m2 += fmaf(d * __fdividef(1.0f, a.n), d, a.m2);
     };
     add(held);
     for (int e = lane + width; e < count; e += width) add(read(e));
-    return {mean, (float)s, all_sum(m2, lg)};
+    return {c, s, mean, all_sum(m2, lg)};
 }
+// n values with that mean and sum less n c: their mean in fp32, and what is left of their sum.
+__device__ __forceinline__ Moments moments_of(float c, double mean, double sum, float m2, float n)
+{
+    const float own = (float)((double)c + mean);
+    return {own, (float)fma(-(double)n, (double)own - (double)c, sum), m2, n};
+}
+__device__ __forceinline__ void send(const Moments *own, int rank, const Moments &m)
+{
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(peer_smem(own, rank)), "f"(m.c), "f"(m.r), "f"(m.m2), "f"(m.n) : "memory");
+}
+
 // Shared memory beside the tile: the moments of rows of threads, joined inside the warps where they can be; the groups' moments of every tile of the cluster;
 // their means and 1/deviations.
 __host__ __device__ __forceinline__ int beside_bytes(const Cut &k)
@@ -69,22 +84,6 @@ struct Beside {
         tile = smem + (beside_bytes(k) + 15) / 16 * 16;
     }
 };
-
-// Means are kept as differences from a reference, the group's first value in the image, until they are written: the parts of a group far from
-// zero would lose digits to their roundings (around 1000 the variance of groups of 300 values was off by 5e-6 of it).  They are read before any block
-// writes: Y may lie in the place of X.
-template <typename TX> __device__ __forceinline__ float reference(const GnFwd &P, long long b, int c)
-{
-    return (float)static_cast<const TX *>(P.X)[b * P.cut.HW * P.ldx + P.cut.by_group((uint32_t)c) * (uint32_t)P.cut.Cg];
-}
-template <typename TX, int V> __device__ __forceinline__ void references(const GnFwd &P, const Tile<V> &t, float (&ref)[V])
-{
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        ref[i] = 0.0f;
-        if ((i & ((1 << P.cut.lg_u) - 1)) == 0 && t.has()) ref[i] = reference<TX>(P, t.b, t.channel() + i);
-    }
-}
 
 // Sums of a thread's pixels: for each set of joined channels those of the differences from its first value and of their squares.  That value is one of
 // the group's, so what a difference of sums loses is a rounding of a square that the group's own sum of squares has as well.
@@ -133,7 +132,7 @@ template <int V> struct ThreadSums {
         }
     }
     // Joined over channels and, where rows of threads lie in a warp, over those: by the first of them to `to`, a thread's sets.  All threads call it.
-    __device__ __forceinline__ void store(int n, const Cut &k, const float (&ref)[V], bool writes, Moments *to) const
+    __device__ __forceinline__ void store(int n, const Cut &k, bool writes, Moments *to) const
     {
         float ss[V], qq[V], kk[V];
 #pragma unroll
@@ -144,51 +143,66 @@ template <int V> struct ThreadSums {
             each(q[i], lo, hi); qq[l] = lo; if (V > 1) qq[h] = hi;
             each(this->k[i], lo, hi); kk[l] = lo; if (V > 1) kk[h] = hi;
         }
-        if (k.lg_u == 0) store_sets<1>(n, ss, qq, kk, ref, k.least, writes, to);
-        if constexpr (V >= 2) if (k.lg_u == 1) store_sets<2>(n, ss, qq, kk, ref, k.least, writes, to);
-        if constexpr (V >= 4) if (k.lg_u == 2) store_sets<4>(n, ss, qq, kk, ref, k.least, writes, to);
-        if constexpr (V >= 8) if (k.lg_u == 3) store_sets<8>(n, ss, qq, kk, ref, k.least, writes, to);
+        if (k.lg_u == 0) store_sets<1>(n, ss, qq, kk, k.least, writes, to);
+        if constexpr (V >= 2) if (k.lg_u == 1) store_sets<2>(n, ss, qq, kk, k.least, writes, to);
+        if constexpr (V >= 4) if (k.lg_u == 2) store_sets<4>(n, ss, qq, kk, k.least, writes, to);
+        if constexpr (V >= 8) if (k.lg_u == 3) store_sets<8>(n, ss, qq, kk, k.least, writes, to);
     }
-    template <int U> static __device__ __forceinline__ void store_sets(int n, float (&ss)[V], float (&qq)[V], const float (&kk)[V], const float (&ref)[V], int least, bool writes, Moments *to)
+    template <int U> static __device__ __forceinline__ void store_sets(int n, float (&ss)[V], float (&qq)[V], const float (&kk)[V], int least, bool writes, Moments *to)
     {
         constexpr int Q = V / U;
-        float t[Q], v[Q], own[Q], s1[Q], q1[Q];
-        const float count = (float)(n * U);
-        float all = count;
+        // its own: mean, what that leaves of the sum, squares
+        float c[Q], r[Q], v[Q];
+        const float count = (float)(n * U), inv = n > 0 ? __frcp_rn(count) : 0.0f;
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
-            s1[i] = ss[i * U];
-            q1[i] = qq[i * U];
+            float s1 = ss[i * U], q1 = qq[i * U];
 #pragma unroll
-            for (int j = 1; j < U; ++j) { s1[i] += ss[i * U + j]; q1[i] += qq[i * U + j]; }
-            own[i] = n > 0 ? -kk[i * U] - ref[i * U] : 0.0f;
-            t[i] = fmaf(count, own[i], s1[i]);
-        }
-        // sums from the reference over the warp, then squares from its mean
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-            if (o >= least) {
-                all += __shfl_xor_sync(0xffffffffu, all, o);
-#pragma unroll
-                for (int i = 0; i < Q; ++i) t[i] += __shfl_xor_sync(0xffffffffu, t[i], o);
-            }
-        const float inv = all > 0.0f ? __fdividef(1.0f, all) : 0.0f;
-#pragma unroll
-        for (int i = 0; i < Q; ++i) {
-            const float d = fmaf(-t[i], inv, own[i]);
-            v[i] = fmaf(d, fmaf(count, d, 2.0f * s1[i]), q1[i]);
+            for (int j = 1; j < U; ++j) { s1 += ss[i * U + j]; q1 += qq[i * U + j]; }
+            const float first = -kk[i * U];
+            c[i] = fmaf(s1, inv, first);
+            r[i] = fmaf(-count, c[i] - first, s1);
+            v[i] = fmaf(-s1 * inv, s1, q1);
             // (an infinity and a NaN stay what they are; a sum of squares is not negative)
             if (v[i] < 0.0f) v[i] = 0.0f;
-            if (!(q1[i] < INFINITY)) v[i] = q1[i];
+            if (!(q1 < INFINITY)) v[i] = q1;
         }
+        // the warp's, as differences from the mean of the first lane that has these channels
+        float all = count;
+        if (least < 32) {
+            float t[Q], d[Q];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-            if (o >= least)
+            for (int i = 0; i < Q; ++i) {
+                const float of = __shfl_sync(0xffffffffu, c[i], (int)threadIdx.x & (least - 1));
+                d[i] = n > 0 ? c[i] - of : 0.0f;
+                t[i] = n > 0 ? fmaf(count, d[i], r[i]) : 0.0f;
+                c[i] = of;
+            }
 #pragma unroll
-                for (int i = 0; i < Q; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+            for (int o = 16; o > 0; o >>= 1)
+                if (o >= least) {
+                    all += __shfl_xor_sync(0xffffffffu, all, o);
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) t[i] += __shfl_xor_sync(0xffffffffu, t[i], o);
+                }
+            const float inv_all = all > 0.0f ? __fdividef(1.0f, all) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                const float mean = t[i] * inv_all, e = fmaf(count, d[i] - mean, r[i]);
+                if (n > 0) v[i] = fmaf(e * inv, e, v[i]);
+                const float of = c[i];
+                c[i] = of + mean;
+                r[i] = fmaf(-all, c[i] - of, t[i]);
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+                if (o >= least)
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        }
         if (writes)
 #pragma unroll
-            for (int i = 0; i < Q; ++i) to[i] = {t[i], v[i], all, 0.0f};
+            for (int i = 0; i < Q; ++i) to[i] = {c[i], r[i], v[i], all};
     }
 };
 
@@ -197,7 +211,7 @@ template <int V, typename Write> __device__ __forceinline__ void join_groups(con
 {
     const int sets_of = k.pieces > 1 ? t.cs >> k.lg_u : k.per, count = sets_of * k.rows_of_sums, across = k.sets;
     const float n = (float)t.rows * (float)(k.pieces > 1 ? t.cs : k.Cg);
-    const float inv = n > 0.0f ? 1.0f / n : 0.0f;
+    const float inv = n > 0.0f ? __fdividef(1.0f, n) : 0.0f;
     const int lg = k.lg_tile, width = 1 << lg, mine = threadIdx.x >> lg, lane = threadIdx.x & (width - 1);
     // (a warp without a group has nothing to do)
     for (int g0 = 0; g0 + (int)((threadIdx.x & ~31u) >> lg) < k.groups; g0 += kGnThreads >> lg) {
@@ -206,7 +220,7 @@ template <int V, typename Write> __device__ __forceinline__ void join_groups(con
             const int y = k.pieces > 1 ? e / sets_of : (int)k.by_per((uint32_t)e);
             return sets[y * across + g * k.per + e - y * sets_of];
         });
-        if (g < k.groups) write(g, lane, width, Moments{a.sum, a.m2, n, 0.0f});
+        if (g < k.groups) write(g, lane, width, moments_of(a.c, a.mean, a.sum, a.m2, n));
     }
 }
 
@@ -299,8 +313,7 @@ template <int V> struct Affine {
     }
 };
 
-// Mean and 1/deviation of the block's groups, the first of them group `first` of all images', from their parts, which read(g, e) gives for e < count, and
-// their references, which `mean` holds.  All threads call it.
+// Mean and 1/deviation of the block's groups, the first of them group `first` of all images', from their parts, which read(g, e) gives for e < count.  All threads call it.
 template <typename Read> __device__ __forceinline__ void finish_groups(const GnFwd &P, int groups, int count, bool write, long long first, float *mean, float *rstd, Read read)
 {
     const int lg = P.cut.lg_slab, mine = threadIdx.x >> lg, lane = threadIdx.x & ((1 << lg) - 1);
@@ -308,7 +321,7 @@ template <typename Read> __device__ __forceinline__ void finish_groups(const GnF
         const int g = g0 + mine;
         const Joined a = join(lane, lg, g < groups ? count : 0, P.cut.inv_n, [&](int e) { return read(g, e); });
         if (g < groups && lane == 0) {
-            mean[g] = (float)((double)mean[g] + a.mean);
+            mean[g] = (float)((double)a.c + a.mean);
             rstd[g] = rsqrtf(a.m2 * (float)P.cut.inv_n + P.eps);
             if (write) {
                 if (P.mean) P.mean[first + g] = mean[g];
@@ -353,9 +366,6 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_fwd_kernel(const __grid_cons
     const int u = 1 << P.cut.lg_u, tiles = P.cut.tiles, groups = P.cut.groups;
     pdl_begin();
     if (tiles > 1) arrive_first();
-    float ref[V];
-    references<TX>(P, t, ref);
-    const float first_ref = (int)threadIdx.x < groups ? reference<TX>(P, t.b, t.c0 + (int)threadIdx.x * P.cut.Cg) : 0.0f;
     TX *const slots = reinterpret_cast<TX *>(at.tile) + threadIdx.x * V;
     {
         const TX *from = static_cast<const TX *>(P.X) + (t.b * P.cut.HW + t.first + t.ty) * P.ldx + t.channel();
@@ -392,10 +402,8 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_fwd_kernel(const __grid_cons
             }
         });
         const int y = P.cut.joint > 1 ? (int)(threadIdx.x >> 5) : t.ty;
-        sums.store(t.n, P.cut, ref, P.cut.joint > 1 ? (int)(threadIdx.x & 31) < P.cut.least : t.has(), at.sets + y * P.cut.sets + t.tx * (V >> P.cut.lg_u));
+        sums.store(t.n, P.cut, P.cut.joint > 1 ? (int)(threadIdx.x & 31) < P.cut.least : t.has(), at.sets + y * P.cut.sets + t.tx * (V >> P.cut.lg_u));
     }
-    if ((int)threadIdx.x < groups) at.mean[threadIdx.x] = first_ref;
-    for (int g = threadIdx.x + kGnThreads; g < groups; g += kGnThreads) at.mean[g] = reference<TX>(P, t.b, t.c0 + g * P.cut.Cg);
     __syncthreads();
     if (tiles > 1) wait_for_all();                   // all blocks are there
     // to all blocks of the cluster
@@ -403,7 +411,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_fwd_kernel(const __grid_cons
         if (tiles == 1) {
             if (lane == 0) at.all[g] = of;
         } else {
-            for (int to = lane; to < tiles; to += width) send(at.all + g * tiles + t.tile, to, of.sum, of.m2, of.n, 0.0f);
+            for (int to = lane; to < tiles; to += width) send(at.all + g * tiles + t.tile, to, of);
         }
     });
     if (tiles == 1) {
@@ -436,8 +444,7 @@ __global__ void __launch_bounds__(kGnThreads) gn_sums_kernel(const __grid_consta
         const long long step = t.R * P.ldx;
         ThreadSums<V> sums;
         Vec<TX, V> v;
-        float f[V], ref[V];
-        references<TX>(P, t, ref);
+        float f[V];
         if (t.n > 0) v.load(x);
         else v.zero();
         v.get(f);
@@ -464,13 +471,13 @@ __global__ void __launch_bounds__(kGnThreads) gn_sums_kernel(const __grid_consta
             sums.add(run);
         }
         const int y = P.cut.joint > 1 ? (int)(threadIdx.x >> 5) : t.ty;
-        sums.store(t.n, P.cut, ref, P.cut.joint > 1 ? (int)(threadIdx.x & 31) < P.cut.least : t.has(), sets + y * P.cut.sets + t.tx * (V >> P.cut.lg_u));
+        sums.store(t.n, P.cut, P.cut.joint > 1 ? (int)(threadIdx.x & 31) < P.cut.least : t.has(), sets + y * P.cut.sets + t.tx * (V >> P.cut.lg_u));
     }
     __syncthreads();
     // one part of each group for the tile
     const int g0 = t.c0 / P.cut.Cg, piece = P.cut.pieces > 1 ? (t.c0 - g0 * P.cut.Cg) / P.cut.slab : 0;
     join_groups(t, P.cut, sets, [&](int g, int lane, int, const Moments &m) {
-        if (lane == 0) P.parts[((t.b * P.cut.G + g0 + g) * P.cut.pieces + piece) * P.cut.tiles + t.tile] = {m.sum, m.m2, m.n, reference<TX>(P, t.b, (g0 + g) * P.cut.Cg)};
+        if (lane == 0) P.parts[((t.b * P.cut.G + g0 + g) * P.cut.pieces + piece) * P.cut.tiles + t.tile] = m;
     });
 }
 
@@ -514,8 +521,6 @@ __global__ void __launch_bounds__(kGnThreads) gn_apply_kernel(const __grid_const
     const int groups = P.cut.groups, count = P.cut.pieces * P.cut.tiles;
     float *const mean = reinterpret_cast<float *>(smem), *const rstd = mean + groups;
     const long long first = t.b * P.cut.G + t.c0 / P.cut.Cg;
-    for (int g = threadIdx.x; g < groups; g += kGnThreads) mean[g] = P.parts[(first + g) * count].ref;
-    __syncthreads();
     finish_groups(P, groups, count, t.tile == 0 && t.c0 % P.cut.Cg == 0, first, mean, rstd, [&](int g, int k) { return P.parts[(first + g) * count + k]; });
     if (t.n == 0) return;
     const Affine<V> affine(P, t, ga, be, mean, rstd);

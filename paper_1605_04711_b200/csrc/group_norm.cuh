@@ -164,10 +164,6 @@ template <typename T> __device__ __forceinline__ T all_sum(T v, int lg)
 
 // What the blocks of a cluster send each other, before they meet at its barrier.  (With an arrival on a barrier in the receiver's memory behind every store, each with a
 // fence of its own, 64 x 12544 x 64 took 61 us forward for 57.)
-__device__ __forceinline__ void send(const void *own, int rank, float a, float b, float c, float d)
-{
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(peer_smem(own, rank)), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
-}
 __device__ __forceinline__ void send(const void *own, int rank, float a)
 {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_smem(own, rank)), "f"(a) : "memory");
