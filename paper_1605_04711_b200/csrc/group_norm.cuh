@@ -68,6 +68,7 @@ struct Cut {
     int pieces;                      // slabs of a group, where a group is more than a slab (the last may have fewer channels); else 1
     int lg_u;                        // channels (their logarithm) that a thread's sums are joined over
     int groups, per, sets;           // groups of a slab (1 for a piece); a group's sets of joined channels; a slab's
+    int head;                        // pixels of a thread that its sums' first anchor is the average of
     int R, joint, least;             // pixels of a block at once; of them, those that are joined inside a warp: lanes `least` apart (32 where none are)
     int rows_of_sums;                // rows of threads, or warps where those are joined
     int lg_tile, lg_slab;            // lanes (their logarithms) that join a group's sums, of a tile, of a slab's tiles
@@ -273,6 +274,8 @@ void finish_cut(Cut &k, int V)
     k.rows = (k.HW + k.tiles - 1) / k.tiles;
     k.groups = std::max(1, k.slab / k.Cg);
     k.R = kGnThreads / VW;
+    const long long pixels = (k.rows + k.R - 1) / k.R;
+    k.head = pixels <= 8 ? 1 : pixels <= 32 ? 2 : 4;
     // lanes of a warp with the same channels: where their places are the same in every warp
     k.joint = VW <= 32 && 32 % VW == 0 ? 32 / VW : 1;
     k.least = 32 / k.joint;
