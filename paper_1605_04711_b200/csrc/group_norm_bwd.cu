@@ -206,6 +206,17 @@ template <int N> __device__ __forceinline__ void add_sums(two_f32 (&A)[N], two_f
     }
 }
 
+// The sums of a run of pixels go to those of all.
+template <int N> __device__ __forceinline__ void end_run(two_f32 (&A)[N], two_f32 (&D)[N], two_f32 (&a)[N], two_f32 (&q)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        A[j] = add2(A[j], a[j]);
+        D[j] = add2(D[j], q[j]);
+        a[j] = q[j] = 0;
+    }
+}
+
 // Sums of N numbers over the lanes that are `least` apart, by halves: of two lanes each goes on with half of the numbers.  A lane ends with N / 2^steps of them (one at
 // least), the first of which has the index that it returns.
 template <int N, int OFF> __device__ __forceinline__ int fold_lanes(float *v, int least, int &left)
@@ -381,7 +392,26 @@ __device__ __forceinline__ void resident(const GnBwd &P, const Tile<V> &t, const
         vd.load(ds + i * (kGnThreads * V));
         vx.load(xs + i * (kGnThreads * V));
     };
-    as_they_come(t.n, 0, [&](int begin, int end) { pixel_by_pixel<TD, TX, V, ACT, 2>(P, t, ch, begin, end, take, [&](int, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { add_sums<N>(A, D, dz, d); }); });
+    if constexpr (kTileMost / (kGnThreads * V * (sizeof(TD) + sizeof(TX))) <= kRun) {
+        as_they_come(t.n, 0, [&](int begin, int end) { pixel_by_pixel<TD, TX, V, ACT, 2>(P, t, ch, begin, end, take, [&](int, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { add_sums<N>(A, D, dz, d); }); });
+    } else {
+        two_f32 a[N], q[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) a[j] = q[j] = 0;
+        int next = kRun;
+        as_they_come(t.n, 0, [&](int begin, int end) {
+            while (begin < end) {
+                const int stop = min(end, next);
+                pixel_by_pixel<TD, TX, V, ACT, 2>(P, t, ch, begin, stop, take, [&](int, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { add_sums<N>(a, q, dz, d); });
+                begin = stop;
+                if (stop == next) {
+                    end_run<N>(A, D, a, q);
+                    next += kRun;
+                }
+            }
+        });
+        end_run<N>(A, D, a, q);
+    }
     if (tiles > 1) wait_for_all();                       // all blocks are there
     // to all blocks of the cluster (without dX to none, which may have ended)
     join_channels(P, t, A, D, at, of, P.dX ? tiles : 0, [&](int g, int kind, int to, float v) {
@@ -479,16 +509,12 @@ __device__ __forceinline__ void tile_sums(const GnBwd &P, const Tile<V> &t, two_
 {
     constexpr int N = Channels<V>::P;
     const Channels<V> ch(P, Raw<V>(P, t));
+    two_f32 a[N], q[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) a[j] = q[j] = 0;
     for (int i = 0; i < t.n; i += kRun) {
-        two_f32 a[N], q[N];
-#pragma unroll
-        for (int j = 0; j < N; ++j) a[j] = q[j] = 0;
         each_pixel<TD, TX, V, ACT>(P, t, ch, i, min(t.n, i + kRun), [&](int, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { add_sums<N>(a, q, dz, d); });
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            A[j] = add2(A[j], a[j]);
-            D[j] = add2(D[j], q[j]);
-        }
+        end_run<N>(A, D, a, q);
     }
 }
 template <typename TD, typename TX, int V> __global__ void __launch_bounds__(kGnThreads, 2) gn_bwd_sums_kernel(const __grid_constant__ GnBwd P)
