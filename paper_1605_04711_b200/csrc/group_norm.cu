@@ -369,7 +369,7 @@ template <typename Read> __device__ __forceinline__ void finish_groups(const GnF
         const Joined a = join(lane, lg, g < groups ? count : 0, P.cut.inv_n, [&](int e) { return read(g, e); });
         if (g < groups && lane == 0) {
             mean[g] = (float)((double)a.c + a.mean);
-            rstd[g] = rsqrtf(a.m2 * (float)P.cut.inv_n + P.eps);
+            rstd[g] = __frsqrt_rn(fmaf(a.m2, (float)P.cut.inv_n, P.eps));
             if (write) {
                 if (P.mean) P.mean[first + g] = mean[g];
                 if (P.rstd) P.rstd[first + g] = rstd[g];
