@@ -392,7 +392,8 @@ int twn_adamw8_unpack_batch(const twn_adamw8_states_t *items, int count, twn_str
  *   items      HOST array; dW TWN_F32 or TWN_BF16 [n], 16-byte aligned.  norm, scale: device fp32, either may be NULL; scale is what
  *              twn_adamw_update_batch takes as grad_scale.  max_norm finite and above 0.
  *   workspace  at least twn_grad_norm_workspace_bytes of the sizes (HOST array), 256-byte aligned, contents need not be initialised.
- * Squares and sums are fp64.  With a NaN among the gradients both are NaN; with an infinity norm is infinite and scale 0.  Deterministic.
+ * Squares and sums are fp64.  With a NaN among the gradients both are NaN; with an infinity norm is infinite and scale 0.  A norm of finite gradients above
+ * the numbers of fp32 is given as infinite, and scale comes from its value in 64 bits.  Deterministic.
  */
 typedef struct {
     const void *dW;

@@ -690,8 +690,9 @@ __global__ void __launch_bounds__(kThreads) grad_norm_fold_kernel(const double *
     for (int i = threadIdx.x; i < count; i += kThreads) a += parts[i];
     a = block_sum(a, warps);
     if (threadIdx.x == 0) {
+        // (a norm of finite gradients that is above all numbers of fp32 still clips them)
         const float root = (float)sqrt(a);
-        const double r = max_norm / ((double)root + 1e-6);
+        const double r = max_norm / ((isinf(root) ? sqrt(a) : (double)root) + 1e-6);
         if (norm) *norm = root;
         if (scale) *scale = r >= 1.0 ? 1.0f : (float)r;              // a NaN stays one
     }
