@@ -95,10 +95,14 @@ template <int V> struct Channels {
             a[i] = mul2(two(one ? r.rstd[0] : r.rstd[l], one ? r.rstd[0] : r.rstd[h]), two(r.gamma[l], r.gamma[h]));
             b[i] = two(r.beta[l], r.beta[h]);
         }
-        // (z is right to a few roundings of its two terms, 2^-24 each; the first is as large as z and beta together at most)
-        doubt = 0.0f;
+        // (z is right to a few roundings of its two terms, 2^-24 each; the first is as large as z and beta together at most.  Below 2^-126 a product may have lost its sign, and
+        // where a factor has come down there any z may have)
+        doubt = 0x1p-126f;
 #pragma unroll
-        for (int i = 0; i < V; ++i) doubt = fmaxf(doubt, 0x1p-18f * fabsf(r.beta[i]));
+        for (int i = 0; i < V; ++i) {
+            const float rstd = one ? r.rstd[0] : r.rstd[i];
+            doubt = fmaxf(doubt, fabsf(rstd * r.gamma[i]) < 0x1p-100f && rstd != 0.0f && r.gamma[i] != 0.0f ? INFINITY : 0x1p-18f * fabsf(r.beta[i]));
+        }
     }
 };
 
@@ -108,6 +112,14 @@ __device__ __noinline__ bool positive_z(const GnBwd &p, long long b, int c, floa
     const long long g = b * p.cut.G + c / p.cut.Cg;
     const double xh = ((double)x - (double)p.mean[g]) * (double)p.rstd[g];
     return xh * (p.gamma ? (double)p.gamma[c] : 1.0) + (p.beta ? (double)p.beta[c] : 0.0) > 0.0;
+}
+
+// Where x is the mean z is beta, and of a sure sign.
+template <int V> __device__ __forceinline__ bool sure(const Channels<V> &ch, int i, float x)
+{
+    float lo, hi;
+    each(ch.m[i / 2], lo, hi);
+    return x == (i % 2 ? -hi : -lo);
 }
 
 // Pairs of a thread's vectors of J pixels: dz and the differences from the mean.
@@ -138,7 +150,7 @@ __device__ __forceinline__ void vector_dz(const GnBwd &p, const Tile<V> &t, cons
         if (doubt)
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (fabsf(z[i]) < ch.doubt) z[i] = positive_z(p, t.b, t.channel() + i, x[0][i]) ? 1.0f : 0.0f;
+                if (fabsf(z[i]) < ch.doubt && !sure(ch, i, x[0][i])) z[i] = positive_z(p, t.b, t.channel() + i, x[0][i]) ? 1.0f : 0.0f;
         // (a NaN goes on)
 #pragma unroll
         for (int i = 0; i < V; ++i) dy[0][i] = z[i] > 0.0f ? dy[0][i] : at_least(z[i], 0.0f);
