@@ -763,7 +763,7 @@ int twn_layer_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy, const voi
  *          and pitch).  Columns C.. of Y's rows are not touched.
  *   gamma, beta   fp32 [C] or NULL (1, 0);  mean, rstd  fp32 [B, groups], outputs for the backward pass, or NULL.
  *   workspace     at least twn_group_norm_fwd_workspace_bytes bytes (0 for sizes that the call refuses or that have nothing to do), 256-byte aligned;
- *                 contents need not be preserved or initialised.  Two calls that overlap on the device must not share it.
+ *                 contents need not be preserved or initialised.  One for B images serves fewer of them too.  Two calls that overlap on the device must not share it.
  *   What the call writes lies apart from all else that it reads or writes, but for Y in the place of X (else TWN_ERR_INVALID_ARG); rows of
  *   one buffer that lie between each other's are apart.
  *   1 <= C <= 2^20, C % groups = 0, eps >= 0, B and HW at most 2^31, B * HW at most 2^40.  B = 0 or HW = 0 is fine and launches nothing.

@@ -604,34 +604,31 @@ __global__ void __launch_bounds__(kGnThreads) gn_apply_kernel(const __grid_const
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------
-size_t parts_bytes(const Cut &k, long long B) { return (size_t)B * k.G * k.pieces * k.tiles * sizeof(Moments); }
+size_t parts_bytes(const Cut &k, long long tiles) { return (size_t)tiles * k.G * k.pieces * sizeof(Moments); }
 
-template <typename TX, typename TY, int V> int fwd(GnFwd &P, long long B, const twn_device_info &dev, void *workspace, size_t workspace_bytes, cudaStream_t s)
+template <typename TX, typename TY, int V> int fwd(GnFwd &P, const Plan &plan, long long B, const twn_device_info &dev, void *workspace, cudaStream_t s)
 {
-    Cut &k = P.cut;
-    size_t smem;
-    if (cut_resident(k, B, V, sizeof(TX), sizeof(TX), fwd_beside, dev.sm_count, &smem)) {
+    const Cut &k = P.cut;
+    if (plan.resident) {
         static bool done[64] = {false};
         const int rc = allow_tile(gn_fwd_kernel<TX, TY, V>, dev.ordinal, done);
         if (rc != TWN_OK) return rc;
-        TWN_CUDA_OK(launch_clusters(gn_fwd_kernel<TX, TY, V>, B * k.slabs * k.tiles, k.tiles, smem, s, P));
+        TWN_CUDA_OK(launch_clusters(gn_fwd_kernel<TX, TY, V>, B * k.slabs * k.tiles, k.tiles, plan.smem, s, P));
         return TWN_OK;
     }
-    if (!cut_streamed(k, B, V)) return TWN_ERR_TOO_LARGE;
-    TWN_REQUIRE(workspace != nullptr && workspace_bytes >= parts_bytes(k, B), TWN_ERR_WORKSPACE);
     P.parts = static_cast<Moments *>(workspace);
     const int grid = (int)(B * k.slabs * k.tiles);
     TWN_CUDA_OK(twn_launch_pdl(true, gn_sums_kernel<TX, V>, grid, kGnThreads, (size_t)k.rows_of_sums * k.sets * sizeof(Moments), s, P));
     TWN_CUDA_OK(twn_launch_pdl(true, gn_apply_kernel<TX, TY, V>, grid, kGnThreads, (size_t)k.groups * 8, s, P));
     return TWN_OK;
 }
-template <typename TX, typename TY> int fwd_any(GnFwd &P, long long B, int V, const twn_device_info &dev, void *workspace, size_t workspace_bytes, cudaStream_t s)
+template <typename TX, typename TY> int fwd_any(GnFwd &P, const Plan &plan, long long B, int V, const twn_device_info &dev, void *workspace, cudaStream_t s)
 {
     if constexpr (sizeof(TX) + sizeof(TY) == 4)
-        if (V == 8) return fwd<TX, TY, 8>(P, B, dev, workspace, workspace_bytes, s);
-    if (V == 4) return fwd<TX, TY, 4>(P, B, dev, workspace, workspace_bytes, s);
-    if (V == 2) return fwd<TX, TY, 2>(P, B, dev, workspace, workspace_bytes, s);
-    return fwd<TX, TY, 1>(P, B, dev, workspace, workspace_bytes, s);
+        if (V == 8) return fwd<TX, TY, 8>(P, plan, B, dev, workspace, s);
+    if (V == 4) return fwd<TX, TY, 4>(P, plan, B, dev, workspace, s);
+    if (V == 2) return fwd<TX, TY, 2>(P, plan, B, dev, workspace, s);
+    return fwd<TX, TY, 1>(P, plan, B, dev, workspace, s);
 }
 
 }  // namespace
@@ -643,7 +640,7 @@ extern "C" size_t twn_group_norm_fwd_workspace_bytes(int64_t B, int64_t HW, int6
     for (int V : {1, 2, 4, 8}) {
         Cut k = cut_of(HW, (int)C, groups);
         if (C % V || !vectors_fit(k.Cg, V) || !cut_streamed(k, B, V)) continue;
-        most = std::max(most, parts_bytes(k, B));
+        most = std::max(most, parts_bytes(k, tiles_at_most(k, B, V, false)));
     }
     return (most + 255) / 256 * 256;
 }
@@ -661,24 +658,29 @@ extern "C" int twn_group_norm_fwd(const void *X, int32_t x_dtype, int64_t ldx, i
     if (rc != TWN_OK) return rc;
     for (const void *p : {(const void *)gamma, (const void *)beta, (const void *)mean, (const void *)rstd}) TWN_REQUIRE(twn_aligned(p, 4), TWN_ERR_MISALIGNED);
     if (M == 0) return TWN_OK;
-    const size_t need = twn_group_norm_fwd_workspace_bytes(B, HW, C, groups);
+    Cut k = cut_of(HW, (int)C, groups);
+    const int V = widest(x_dtype == TWN_BF16 && y_dtype == TWN_BF16 ? 8 : 4, (int)C, k.Cg,
+                         [&](int v) { return vector_rows(X, x_dtype, ldx, v) && vector_rows(Y, y_dtype, ldy, v); });
+    Plan p;
+    rc = plan(k, p, B, V, (int)size_of(x_dtype), (int)size_of(x_dtype), fwd_beside);
+    if (rc != TWN_OK) return rc;
+    // (a tile in shared memory needs none of it)
+    const size_t need = std::max<size_t>(256, p.resident ? 0 : parts_bytes(k, B * k.tiles));
     TWN_REQUIRE(workspace != nullptr && workspace_bytes >= need, TWN_ERR_WORKSPACE);
     TWN_REQUIRE(twn_aligned(workspace, 256), TWN_ERR_MISALIGNED);
     Places places;
     places.matrix(Y, y_dtype, ldy, M, C, true);
     places.matrix(X, x_dtype, ldx, M, C, false);
-    for (const void *p : {(const void *)gamma, (const void *)beta}) places.vector(p, 4 * C, false);
-    for (const void *p : {(const void *)mean, (const void *)rstd}) places.vector(p, 4 * B * groups, true);
+    for (const void *q : {(const void *)gamma, (const void *)beta}) places.vector(q, 4 * C, false);
+    for (const void *q : {(const void *)mean, (const void *)rstd}) places.vector(q, 4 * B * groups, true);
     places.vector(workspace, (long long)need, true);
     TWN_REQUIRE(places.apart(), TWN_ERR_INVALID_ARG);
     twn_device_info dev;
     rc = twn_current_device(&dev);
     if (rc != TWN_OK) return rc;
-    GnFwd P = {X, Y, gamma, beta, mean, rstd, nullptr, ldx, ldy, cut_of(HW, (int)C, groups), act, (float)eps};
-    const int V = widest(x_dtype == TWN_BF16 && y_dtype == TWN_BF16 ? 8 : 4, (int)C, P.cut.Cg,
-                         [&](int v) { return vector_rows(X, x_dtype, ldx, v) && vector_rows(Y, y_dtype, ldy, v); });
+    GnFwd P = {X, Y, gamma, beta, mean, rstd, nullptr, ldx, ldy, k, act, (float)eps};
     cudaStream_t s = twn_cu(stream);
-#define TWN_GN_FWD(TX, TY) fwd_any<TX, TY>(P, B, V, dev, workspace, workspace_bytes, s)
+#define TWN_GN_FWD(TX, TY) fwd_any<TX, TY>(P, p, B, V, dev, workspace, s)
     if (x_dtype == TWN_BF16) return y_dtype == TWN_BF16 ? TWN_GN_FWD(bf16, bf16) : TWN_GN_FWD(bf16, float);
     return y_dtype == TWN_BF16 ? TWN_GN_FWD(float, bf16) : TWN_GN_FWD(float, float);
 #undef TWN_GN_FWD

@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kGnThreads = 256;
 constexpr int kMaxCluster = 8;
-constexpr int kSms = 148;            // that the tiles of two launches are for: their workspace is the same on any device
+constexpr int kSms = 148;            // that tiles are made for: the workspace is the same on any device, and without one
 constexpr int kRun = 64;             // pixels that a thread adds up by themselves: sums of millions of them keep their digits
 constexpr size_t kTileTwo = 112 * 1024, kTileMost = 224 * 1024;     // shared memory of a block where there are two an SM, and of one at most
 constexpr size_t kTileLeast = 64 * 1024;                            // what small images' blocks grow to
@@ -305,7 +305,7 @@ void finish_cut(Cut &k, int V)
 // up to 64 KB, as long as there is a block for each SM (64 x 49 x 512 bf16 5.1 us for 14.0, its backward pass 9.0 for 26.8; with a half of that least 64 x 784 x 512 took 34 us for 29, with
 // twice as much its backward pass 75 for 55).  Smaller tiles, three or
 // four blocks an SM, took longer: what a block does beside its elements is half of its instructions.
-template <typename Beside> bool cut_resident(Cut &k, long long B, int V, int least_size, int bytes, Beside beside, int sm_count, size_t *smem)
+template <typename Beside> bool cut_resident(Cut &k, long long B, int V, int least_size, int bytes, Beside beside, size_t *smem)
 {
     const int unit = (int)std::lcm((long long)k.Cg, (long long)V), units = k.C / unit;
     if (unit / V > kGnThreads) return false;
@@ -319,24 +319,31 @@ template <typename Beside> bool cut_resident(Cut &k, long long B, int V, int lea
         while (tiles <= kMaxCluster && need(tiles) > most) tiles *= 2;
         return tiles;
     };
-    int tiles = kMaxCluster + 1;
+    int tiles = kMaxCluster + 1, slab = 0;                           // tiles that a cluster holds, and their slab's channels
     for (const int channels : {64 / bytes, 32 / least_size}) {
         int of = std::max(1, std::min(units, channels / unit));
         while (units % of) --of;
         while (of < units && k.HW * unit * of * bytes < (long long)kTileLeast) {
             int more = of + 1;
             while (units % more) ++more;
-            if (B * (units / more) < sm_count || more * (unit / V) > kGnThreads || k.HW * unit * more * bytes > (long long)kTileTwo) break;
+            if (B * (units / more) < kSms || more * (unit / V) > kGnThreads || k.HW * unit * more * bytes > (long long)kTileTwo) break;
             of = more;
         }
         k.slab = unit * of;
         k.slabs = units / of;
-        tiles = tiles_for(kTileTwo);
-        if (tiles > kMaxCluster) continue;
-        while (B * k.slabs * tiles < sm_count && tiles < kMaxCluster && k.HW * (k.slab / V) / (2 * tiles) >= 4 * kGnThreads) tiles *= 2;
-        if (B * k.slabs * tiles >= sm_count) break;
+        const int fit = tiles_for(kTileTwo);
+        if (fit > kMaxCluster) continue;
+        tiles = fit;
+        slab = k.slab;
+        while (B * k.slabs * tiles < kSms && tiles < kMaxCluster && k.HW * (k.slab / V) / (2 * tiles) >= 4 * kGnThreads) tiles *= 2;
+        if (B * k.slabs * tiles >= kSms) break;
     }
-    if (tiles > kMaxCluster) tiles = tiles_for(kTileMost);
+    if (slab) {
+        k.slab = slab;
+        k.slabs = k.C / slab;
+    } else {
+        tiles = tiles_for(kTileMost);
+    }
     if (tiles > kMaxCluster) return false;
     *smem = need(tiles);
     return B * k.slabs * k.tiles < 1ll << 31;
@@ -366,6 +373,24 @@ bool cut_streamed(Cut &k, long long B, int V)
     k.tiles = (int)std::min(read, std::min(want, most));
     finish_cut(k, V);
     return B * k.slabs * k.tiles < 1ll << 31 && k.rows < 1ll << 31;
+}
+
+// How a call of vectors of V elements is cut, `bytes` an element of all that it keeps and `least` of the smallest.  TWN_OK or why not.
+struct Plan {
+    bool resident;
+    size_t smem;
+};
+template <typename Beside> int plan(Cut &k, Plan &p, long long B, int V, int least, int bytes, Beside beside)
+{
+    p.resident = cut_resident(k, B, V, least, bytes, beside, &p.smem);
+    return p.resident || cut_streamed(k, B, V) ? TWN_OK : TWN_ERR_TOO_LARGE;
+}
+// Tiles that a workspace has room for: those of the call, and those of any batch of fewer images, which may have more tiles each.
+long long tiles_at_most(const Cut &k, long long B, int V, bool resident)
+{
+    Cut one = k;
+    if (!resident) cut_streamed(one, 1, V);
+    return std::max(B * k.tiles, resident ? std::min<long long>(B * kMaxCluster, 2 * kSms) : std::min<long long>(B * one.tiles, 8 * kSms));
 }
 
 // That a block is there, and nothing about its memory: no write has to arrive before it.

@@ -602,8 +602,8 @@ __global__ void __launch_bounds__(32 * kFoldRows) gn_fold_kernel(const float *ch
 
 // ---- host ---------------------------------------------------------------------------------------------------------------------
 // Sums of channels in front, those of groups behind them.
-size_t channel_bytes(const Cut &k, long long B, int tiles) { return ((size_t)B * tiles * 2 * k.C * sizeof(float) + 255) / 256 * 256; }
-size_t part_bytes(const Cut &k, long long B) { return (size_t)B * k.G * k.pieces * k.tiles * sizeof(float2); }
+size_t channel_bytes(const Cut &k, long long tiles) { return ((size_t)tiles * 2 * k.C * sizeof(float) + 255) / 256 * 256; }
+size_t workspace_of(const Cut &k, long long tiles, bool resident) { return channel_bytes(k, tiles) + (resident ? 0 : (size_t)tiles * k.G * k.pieces * sizeof(float2)); }
 
 int fold(const GnBwd &P, long long B, float *dgamma, float *dbeta, cudaStream_t s)
 {
@@ -613,38 +613,36 @@ int fold(const GnBwd &P, long long B, float *dgamma, float *dbeta, cudaStream_t 
 }
 
 template <typename TD, typename TX, typename TO, int V>
-int bwd(GnBwd &P, long long B, const twn_device_info &dev, float *dgamma, float *dbeta, void *workspace, cudaStream_t s)
+int bwd(GnBwd &P, const Plan &plan, long long B, const twn_device_info &dev, float *dgamma, float *dbeta, void *workspace, cudaStream_t s)
 {
-    Cut &k = P.cut;
-    size_t smem;
-    if (cut_resident(k, B, V, (int)std::min(sizeof(TD), sizeof(TX)), sizeof(TD) + sizeof(TX), bwd_beside, dev.sm_count, &smem)) {
+    const Cut &k = P.cut;
+    if (plan.resident) {
         static bool done[64] = {false};
         const int rc = allow_tile(gn_bwd_kernel<TD, TX, TO, V>, dev.ordinal, done);
         if (rc != TWN_OK) return rc;
-        TWN_CUDA_OK(launch_clusters(gn_bwd_kernel<TD, TX, TO, V>, B * k.slabs * k.tiles, k.tiles, smem, s, P));
+        TWN_CUDA_OK(launch_clusters(gn_bwd_kernel<TD, TX, TO, V>, B * k.slabs * k.tiles, k.tiles, plan.smem, s, P));
         return fold(P, B, dgamma, dbeta, s);
     }
-    if (!cut_streamed(k, B, V)) return TWN_ERR_TOO_LARGE;
-    P.parts = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + channel_bytes(k, B, k.tiles));
+    P.parts = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + channel_bytes(k, B * k.tiles));
     const int grid = (int)(B * k.slabs * k.tiles);
     TWN_CUDA_OK(twn_launch_pdl(true, gn_bwd_sums_kernel<TD, TX, V>, grid, kGnThreads, sums_bytes(k), s, P));
     if (P.dX) TWN_CUDA_OK(twn_launch_pdl(true, gn_bwd_apply_kernel<TD, TX, TO, V>, grid, kGnThreads, (size_t)k.groups * 12, s, P));
     return fold(P, B, dgamma, dbeta, s);
 }
 template <typename TD, typename TX, typename TO>
-int bwd_any(GnBwd &P, long long B, int V, const twn_device_info &dev, float *dgamma, float *dbeta, void *workspace, cudaStream_t s)
+int bwd_any(GnBwd &P, const Plan &plan, long long B, int V, const twn_device_info &dev, float *dgamma, float *dbeta, void *workspace, cudaStream_t s)
 {
     if constexpr (sizeof(TD) + sizeof(TX) + sizeof(TO) == 6)
-        if (V == 8) return bwd<TD, TX, TO, 8>(P, B, dev, dgamma, dbeta, workspace, s);
-    if (V == 4) return bwd<TD, TX, TO, 4>(P, B, dev, dgamma, dbeta, workspace, s);
-    if (V == 2) return bwd<TD, TX, TO, 2>(P, B, dev, dgamma, dbeta, workspace, s);
-    return bwd<TD, TX, TO, 1>(P, B, dev, dgamma, dbeta, workspace, s);
+        if (V == 8) return bwd<TD, TX, TO, 8>(P, plan, B, dev, dgamma, dbeta, workspace, s);
+    if (V == 4) return bwd<TD, TX, TO, 4>(P, plan, B, dev, dgamma, dbeta, workspace, s);
+    if (V == 2) return bwd<TD, TX, TO, 2>(P, plan, B, dev, dgamma, dbeta, workspace, s);
+    return bwd<TD, TX, TO, 1>(P, plan, B, dev, dgamma, dbeta, workspace, s);
 }
 template <typename TD, typename TX>
-int bwd_to(GnBwd &P, int dx_dtype, long long B, int V, const twn_device_info &dev, float *dgamma, float *dbeta, void *workspace, cudaStream_t s)
+int bwd_to(GnBwd &P, const Plan &plan, int dx_dtype, long long B, int V, const twn_device_info &dev, float *dgamma, float *dbeta, void *workspace, cudaStream_t s)
 {
-    return dx_dtype == TWN_BF16 ? bwd_any<TD, TX, bf16>(P, B, V, dev, dgamma, dbeta, workspace, s)
-                                : bwd_any<TD, TX, float>(P, B, V, dev, dgamma, dbeta, workspace, s);
+    return dx_dtype == TWN_BF16 ? bwd_any<TD, TX, bf16>(P, plan, B, V, dev, dgamma, dbeta, workspace, s)
+                                : bwd_any<TD, TX, float>(P, plan, B, V, dev, dgamma, dbeta, workspace, s);
 }
 
 }  // namespace
@@ -652,12 +650,14 @@ int bwd_to(GnBwd &P, int dx_dtype, long long B, int V, const twn_device_info &de
 extern "C" size_t twn_group_norm_bwd_workspace_bytes(int64_t B, int64_t HW, int64_t C, int32_t groups)
 {
     if (check_groups(B, HW, C, groups) != TWN_OK || B == 0 || HW == 0) return 0;
-    Cut k = cut_of(HW, (int)C, groups);
-    size_t most = channel_bytes(k, B, kMaxCluster);
-    for (int V : {1, 2, 4, 8}) {
-        if (C % V || !vectors_fit(k.Cg, V) || !cut_streamed(k, B, V)) continue;
-        most = std::max(most, channel_bytes(k, B, k.tiles) + part_bytes(k, B));
-    }
+    size_t most = 0;
+    for (int V : {1, 2, 4, 8})
+        for (int bytes : {4, 6, 8}) {                                // of dY and X together
+            Cut k = cut_of(HW, (int)C, groups);
+            Plan p;
+            if (C % V || !vectors_fit(k.Cg, V) || (V == 8 && bytes > 4) || plan(k, p, B, V, bytes == 8 ? 4 : 2, bytes, bwd_beside) != TWN_OK) continue;
+            most = std::max(most, workspace_of(k, tiles_at_most(k, B, V, p.resident), p.resident));
+        }
     return (most + 255) / 256 * 256;
 }
 
@@ -685,7 +685,16 @@ extern "C" int twn_group_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy
             if (p) TWN_CUDA_OK(cudaMemsetAsync(p, 0, (size_t)C * sizeof(float), s));
         return TWN_OK;
     }
-    const size_t need = twn_group_norm_bwd_workspace_bytes(B, HW, C, groups);
+    const int out = dX ? dx_dtype : dy_dtype;
+    Cut k = cut_of(HW, (int)C, groups);
+    const int V = widest(dy_dtype == TWN_BF16 && x_dtype == TWN_BF16 && out == TWN_BF16 ? 8 : 4, (int)C, k.Cg, [&](int v) {
+        return vector_rows(dY, dy_dtype, lddy, v) && vector_rows(X, x_dtype, ldx, v) && (!dX || vector_rows(dX, dx_dtype, lddx, v)) &&
+               (!residual || vector_rows(residual, dx_dtype, lddx, v));
+    });
+    Plan p;
+    rc = plan(k, p, B, V, (int)std::min(size_of(dy_dtype), size_of(x_dtype)), (int)(size_of(dy_dtype) + size_of(x_dtype)), bwd_beside);
+    if (rc != TWN_OK) return rc;
+    const size_t need = workspace_of(k, B * k.tiles, p.resident);
     TWN_REQUIRE(workspace != nullptr && workspace_bytes >= need, TWN_ERR_WORKSPACE);
     TWN_REQUIRE(twn_aligned(workspace, 256), TWN_ERR_MISALIGNED);
     Places places;
@@ -693,22 +702,16 @@ extern "C" int twn_group_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy
     places.matrix(dY, dy_dtype, lddy, M, C, false);
     places.matrix(X, x_dtype, ldx, M, C, false);
     places.matrix(residual, dx_dtype, lddx, M, C, false);
-    for (const void *p : {(const void *)gamma, (const void *)beta}) places.vector(p, 4 * C, false);
-    for (const void *p : {(const void *)mean, (const void *)rstd}) places.vector(p, 4 * B * groups, false);
-    for (const void *p : {(const void *)dgamma, (const void *)dbeta}) places.vector(p, 4 * C, true);
+    for (const void *q : {(const void *)gamma, (const void *)beta}) places.vector(q, 4 * C, false);
+    for (const void *q : {(const void *)mean, (const void *)rstd}) places.vector(q, 4 * B * groups, false);
+    for (const void *q : {(const void *)dgamma, (const void *)dbeta}) places.vector(q, 4 * C, true);
     places.vector(workspace, (long long)need, true);
     TWN_REQUIRE(places.apart(), TWN_ERR_INVALID_ARG);
     twn_device_info dev;
     rc = twn_current_device(&dev);
     if (rc != TWN_OK) return rc;
-    GnBwd P = {dY, X, dX, residual, gamma, beta, mean, rstd, dgamma || dbeta ? static_cast<float *>(workspace) : nullptr, nullptr, lddy, ldx, lddx,
-               cut_of(HW, (int)C, groups), act};
-    const int out = dX ? dx_dtype : dy_dtype;
-    const int V = widest(dy_dtype == TWN_BF16 && x_dtype == TWN_BF16 && out == TWN_BF16 ? 8 : 4, (int)C, P.cut.Cg, [&](int v) {
-        return vector_rows(dY, dy_dtype, lddy, v) && vector_rows(X, x_dtype, ldx, v) && (!dX || vector_rows(dX, dx_dtype, lddx, v)) &&
-               (!residual || vector_rows(residual, dx_dtype, lddx, v));
-    });
+    GnBwd P = {dY, X, dX, residual, gamma, beta, mean, rstd, dgamma || dbeta ? static_cast<float *>(workspace) : nullptr, nullptr, lddy, ldx, lddx, k, act};
     if (dy_dtype == TWN_BF16)
-        return x_dtype == TWN_BF16 ? bwd_to<bf16, bf16>(P, out, B, V, dev, dgamma, dbeta, workspace, s) : bwd_to<bf16, float>(P, out, B, V, dev, dgamma, dbeta, workspace, s);
-    return x_dtype == TWN_BF16 ? bwd_to<float, bf16>(P, out, B, V, dev, dgamma, dbeta, workspace, s) : bwd_to<float, float>(P, out, B, V, dev, dgamma, dbeta, workspace, s);
+        return x_dtype == TWN_BF16 ? bwd_to<bf16, bf16>(P, p, out, B, V, dev, dgamma, dbeta, workspace, s) : bwd_to<bf16, float>(P, p, out, B, V, dev, dgamma, dbeta, workspace, s);
+    return x_dtype == TWN_BF16 ? bwd_to<float, bf16>(P, p, out, B, V, dev, dgamma, dbeta, workspace, s) : bwd_to<float, float>(P, p, out, B, V, dev, dgamma, dbeta, workspace, s);
 }
