@@ -271,6 +271,8 @@ template <int V, typename Write> __device__ __forceinline__ void join_groups(con
     }
 }
 
+// Pixels that are worked on at once: SiLU's reciprocals serve two.
+template <int ACT> constexpr int kAtOnce = ACT == kSilu ? 2 : 1;
 // Of two channels of J pixels.
 template <int ACT, int J> __device__ __forceinline__ void activate(two_f32 (&z)[J])
 {
@@ -287,9 +289,12 @@ template <int ACT, int J> __device__ __forceinline__ void activate(two_f32 (&z)[
 // Of one channel of two pixels.
 __device__ __forceinline__ two_f32 silu(two_f32 z)
 {
-    two_f32 e;
+    float t0, t1, s0, s1;
     z = at_least2(z, kLeastZ);
-    return mul2(z, sigmoid2(z, e));
+    each(mul2(z, two(kMinusLog2e, kMinusLog2e)), t0, t1);
+    each(fma2(two(ex2(t0), ex2(t1)), two(1.0f, 0x1p-126f), two(1.0f, 0x1p-126f)), s0, s1);
+    const float r = reciprocal(s0 * s1);
+    return mul2(z, two(r * s1, r * s0 * 0x1p-126f));
 }
 
 // (gamma and beta may lie on any multiple of four bytes)

@@ -206,11 +206,9 @@ __device__ __forceinline__ float at_least(float x, float least)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(least));
     return r;
 }
-// Pixels that are worked on at once: SiLU's reciprocals serve two.
-template <int ACT> constexpr int kAtOnce = ACT == kSilu ? 2 : 1;
-// exp(-z) and 1 / (1 + exp(-z)) of two neighbouring channels of J pixels, z at least kLeastZ.  One reciprocal serves a channel of two pixels, whose z are NaN together, and never two
-// channels, which may be of different groups.  The factor of 2^-126 keeps the product of two sums
-// from 1 to 2^126 inside the numbers.  (One for each z: 64 x 3136 x 256 bf16 in 57.4 us for 54.9.)
+// exp(-z) and 1 / (1 + exp(-z)) of two neighbouring channels of J pixels, z at least kLeastZ.  With two pixels one reciprocal serves a channel of both, whose z are NaN together, and
+// never two channels, which may be of different groups (forward, 64 x 3136 x 256 bf16: 54.4 us, with one for each z 57.4); the factor of 2^-126 keeps the product of
+// two sums from 1 to 2^126 inside the numbers.
 template <int J> __device__ __forceinline__ void sigmoids(const two_f32 (&z)[J], two_f32 (&e)[J], two_f32 (&f)[J])
 {
     const two_f32 one = two(1.0f, 1.0f), scale = two(0x1p-126f, 0x1p-126f);
@@ -229,16 +227,6 @@ template <int J> __device__ __forceinline__ void sigmoids(const two_f32 (&z)[J],
         f[J - 1] = mul2(mul2(f[0], s[0]), scale);
         f[0] = mul2(f[0], s[J - 1]);
     }
-}
-// Of one channel of two pixels.
-__device__ __forceinline__ two_f32 sigmoid2(two_f32 z, two_f32 &e)
-{
-    float t0, t1, s0, s1;
-    each(mul2(z, two(kMinusLog2e, kMinusLog2e)), t0, t1);
-    e = two(ex2(t0), ex2(t1));
-    each(fma2(e, two(1.0f, 0x1p-126f), two(1.0f, 0x1p-126f)), s0, s1);
-    const float r = reciprocal(s0 * s1);
-    return two(r * s1, r * s0 * 0x1p-126f);
 }
 __device__ __forceinline__ two_f32 at_least2(two_f32 z, float least)
 {

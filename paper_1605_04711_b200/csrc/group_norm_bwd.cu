@@ -1,8 +1,6 @@
 // Group norm with an activation, backward (see group_norm.cuh).
 #include "group_norm.cuh"
 
-#include <type_traits>
-
 namespace {
 
 struct GnBwd {
@@ -122,26 +120,22 @@ template <int V> __device__ __forceinline__ bool sure(const Channels<V> &ch, int
     return x == (i % 2 ? -hi : -lo);
 }
 
-// Pairs of a thread's vectors of J pixels: dz and the differences from the mean.
-template <typename TD, typename TX, int V, int ACT, int J>
-__device__ __forceinline__ void vector_dz(const GnBwd &p, const Tile<V> &t, const Channels<V> &ch, const Vec<TD, V> (&vd)[J], const Vec<TX, V> (&vx)[J],
-                                          two_f32 (&dz)[J][Channels<V>::P], two_f32 (&d)[J][Channels<V>::P])
+// Pairs of a thread's vector: dz and the differences from the mean.
+template <typename TD, typename TX, int V, int ACT>
+__device__ __forceinline__ void vector_dz(const GnBwd &p, const Tile<V> &t, const Channels<V> &ch, const Vec<TD, V> &vd, const Vec<TX, V> &vx,
+                                          two_f32 (&dz)[Channels<V>::P], two_f32 (&d)[Channels<V>::P])
 {
-    float dy[J][V], x[J][V];
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-        vd[j].get(dy[j]);
-        vx[j].get(x[j]);
-    }
-    if constexpr (ACT == kRelu) {
-        static_assert(J == 1, "");
-        float z[V];
+    float dy[V], x[V];
+    vd.get(dy);
+    vx.get(x);
+    float z[V];
+    if (ACT == kRelu) {
         bool doubt = false;
 #pragma unroll
         for (int i = 0; i < Channels<V>::P; ++i) {
             const int l = 2 * i < V ? 2 * i : 0, h = V > 1 ? 2 * i + 1 : 0;
             float lo, hi;
-            each(fma2(add2(two(x[0][l], V > 1 ? x[0][h] : 0.0f), ch.m[i]), ch.a[i], ch.b[i]), lo, hi);
+            each(fma2(add2(two(x[l], V > 1 ? x[h] : 0.0f), ch.m[i]), ch.a[i], ch.b[i]), lo, hi);
             z[l] = lo;
             if (V > 1) z[h] = hi;
         }
@@ -150,64 +144,39 @@ __device__ __forceinline__ void vector_dz(const GnBwd &p, const Tile<V> &t, cons
         if (doubt)
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (fabsf(z[i]) < ch.doubt && !sure(ch, i, x[0][i])) z[i] = positive_z(p, t.b, t.channel() + i, x[0][i]) ? 1.0f : 0.0f;
+                if (fabsf(z[i]) < ch.doubt && !sure(ch, i, x[i])) z[i] = positive_z(p, t.b, t.channel() + i, x[i]) ? 1.0f : 0.0f;
         // (a NaN goes on)
 #pragma unroll
-        for (int i = 0; i < V; ++i) dy[0][i] = z[i] > 0.0f ? dy[0][i] : at_least(z[i], 0.0f);
+        for (int i = 0; i < V; ++i) dy[i] = z[i] > 0.0f ? dy[i] : at_least(z[i], 0.0f);
     }
 #pragma unroll
     for (int i = 0; i < Channels<V>::P; ++i) {
         const int l = 2 * i < V ? 2 * i : 0, h = V > 1 ? 2 * i + 1 : 0;
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            d[j][i] = add2(two(x[j][l], V > 1 ? x[j][h] : 0.0f), ch.m[i]);
-            dz[j][i] = two(dy[j][l], V > 1 ? dy[j][h] : 0.0f);
-        }
-        if constexpr (ACT == kSilu) {
-            // dy f (1 + z (1 - f)) = dy f (1 + z e f),  e = exp(-z), f = 1 / (1 + e)
-            if constexpr (V == 1 && J == 2) {
-                // (one channel: the two pixels are a pair)
-                float d0, d1, o0, o1;
-                each(d[0][0], d0, o0);
-                each(d[1][0], d1, o1);
-                const two_f32 z = at_least2(fma2(two(d0, d1), ch.a[0], ch.b[0]), kLeastZ);
-                two_f32 e;
-                const two_f32 f = sigmoid2(z, e);
-                each(mul2(mul2(two(dy[0][0], dy[1][0]), f), fma2(z, mul2(e, f), two(1.0f, 1.0f))), o0, o1);
-                dz[0][0] = two(o0, 0.0f);
-                dz[1][0] = two(o1, 0.0f);
-            } else {
-                two_f32 z[J], e[J], f[J];
-#pragma unroll
-                for (int j = 0; j < J; ++j) z[j] = at_least2(fma2(d[j][i], ch.a[i], ch.b[i]), kLeastZ);
-                sigmoids(z, e, f);
-#pragma unroll
-                for (int j = 0; j < J; ++j) dz[j][i] = mul2(mul2(dz[j][i], f[j]), fma2(z[j], mul2(e[j], f[j]), two(1.0f, 1.0f)));
-            }
+        d[i] = add2(two(x[l], V > 1 ? x[h] : 0.0f), ch.m[i]);
+        dz[i] = two(dy[l], V > 1 ? dy[h] : 0.0f);
+        if (ACT == kSilu) {
+            // dy f (1 + z (1 - f)) = dy f (1 + z e f),  e = exp(-z), f = 1 / (1 + e).  (A reciprocal for two pixels, as the forward pass has it, takes more registers: 108 us for 104.)
+            const two_f32 z[1] = {at_least2(fma2(d[i], ch.a[i], ch.b[i]), kLeastZ)};
+            two_f32 e[1], f[1];
+            sigmoids<1>(z, e, f);
+            dz[i] = mul2(mul2(dz[i], f[0]), fma2(z[0], mul2(e[0], f[0]), two(1.0f, 1.0f)));
         }
     }
 }
 
-// Pixels from `begin` to `end` of a thread, which take(i, dY, X) loads: use(i, dz, differences) for each.  PIXELS a turn of the loop.
-template <typename TD, typename TX, int V, int ACT, int PIXELS, typename Take, typename Use>
+// Pixels from `begin` to `end` of a thread, which take(i, dY, X) loads: use(i, dz, differences) for each.
+template <typename TD, typename TX, int V, int ACT, typename Take, typename Use>
 __device__ __forceinline__ void pixel_by_pixel(const GnBwd &p, const Tile<V> &t, const Channels<V> &ch, int begin, int end, const Take &take, const Use &use)
 {
-    constexpr int J = kAtOnce<ACT>;
-    auto work = [&](int i, auto pixels) {
-        constexpr int n = decltype(pixels)::value;
-        Vec<TD, V> vd[n];
-        Vec<TX, V> vx[n];
-        two_f32 dz[n][Channels<V>::P], d[n][Channels<V>::P];
-#pragma unroll
-        for (int j = 0; j < n; ++j) take(i + j, vd[j], vx[j]);
-        vector_dz<TD, TX, V, ACT, n>(p, t, ch, vd, vx, dz, d);
-#pragma unroll
-        for (int j = 0; j < n; ++j) use(i + j, dz[j], d[j]);
-    };
-    int i = begin;
-#pragma unroll (PIXELS / J)
-    for (; i + J <= end; i += J) work(i, std::integral_constant<int, J>());
-    if (J > 1 && i < end) work(i, std::integral_constant<int, 1>());
+#pragma unroll 2
+    for (int i = begin; i < end; ++i) {
+        Vec<TD, V> vd;
+        Vec<TX, V> vx;
+        two_f32 dz[Channels<V>::P], d[Channels<V>::P];
+        take(i, vd, vx);
+        vector_dz<TD, TX, V, ACT>(p, t, ch, vd, vx, dz, d);
+        use(i, dz, d);
+    }
 }
 template <int N> __device__ __forceinline__ void add_sums(two_f32 (&A)[N], two_f32 (&D)[N], const two_f32 (&dz)[N], const two_f32 (&d)[N])
 {
@@ -405,7 +374,7 @@ __device__ __forceinline__ void resident(const GnBwd &P, const Tile<V> &t, const
         vx.load(xs + i * (kGnThreads * V));
     };
     if constexpr (kTileMost / (kGnThreads * V * (sizeof(TD) + sizeof(TX))) <= kRun) {
-        as_they_come(t.n, 0, [&](int begin, int end) { pixel_by_pixel<TD, TX, V, ACT, 2>(P, t, ch, begin, end, take, [&](int, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { add_sums<N>(A, D, dz, d); }); });
+        as_they_come(t.n, 0, [&](int begin, int end) { pixel_by_pixel<TD, TX, V, ACT>(P, t, ch, begin, end, take, [&](int, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { add_sums<N>(A, D, dz, d); }); });
     } else {
         two_f32 a[N], q[N];
 #pragma unroll
@@ -414,7 +383,7 @@ __device__ __forceinline__ void resident(const GnBwd &P, const Tile<V> &t, const
         as_they_come(t.n, 0, [&](int begin, int end) {
             while (begin < end) {
                 const int stop = min(end, next);
-                pixel_by_pixel<TD, TX, V, ACT, 2>(P, t, ch, begin, stop, take, [&](int, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { add_sums<N>(a, q, dz, d); });
+                pixel_by_pixel<TD, TX, V, ACT>(P, t, ch, begin, stop, take, [&](int, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { add_sums<N>(a, q, dz, d); });
                 begin = stop;
                 if (stop == next) {
                     end_run<N>(A, D, a, q);
@@ -444,7 +413,7 @@ __device__ __forceinline__ void resident(const GnBwd &P, const Tile<V> &t, const
         const long long to_at = (t.b * P.cut.HW + t.first + t.ty) * P.lddx + t.channel(), step = t.R * P.lddx;
         TO *to = static_cast<TO *>(P.dX) + to_at;
         const TO *add = P.add ? static_cast<const TO *>(P.add) + to_at : nullptr;
-        pixel_by_pixel<TD, TX, V, ACT, 2>(P, t, ch, 0, t.n, take,
+        pixel_by_pixel<TD, TX, V, ACT>(P, t, ch, 0, t.n, take,
                                  [&](int i, const two_f32 (&dz)[N], const two_f32 (&d)[N]) { write_dx<V>(ch, te, dz, d, to + i * step, add ? add + i * step : nullptr); });
     }
 }
@@ -493,28 +462,33 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_bwd_kernel(const __grid_cons
 template <typename TD, typename TX, int V, int ACT, typename Use>
 __device__ __forceinline__ void each_pixel(const GnBwd &P, const Tile<V> &t, const Channels<V> &ch, int i, int end, const Use &use)
 {
-    constexpr int N = Channels<V>::P, J = kAtOnce<ACT>;
     const long long pixel = t.b * P.cut.HW + t.first + t.ty;
     const TD *dy = static_cast<const TD *>(P.dY) + pixel * P.lddy + t.channel();
     const TX *x = static_cast<const TX *>(P.X) + pixel * P.ldx + t.channel();
     const long long step_d = t.R * P.lddy, step_x = t.R * P.ldx;
+    two_f32 dz[Channels<V>::P], d[Channels<V>::P];
     for (; i + 4 <= end; i += 4) {
-        Vec<TD, V> vd[4 / J][J];
-        Vec<TX, V> vx[4 / J][J];
+        Vec<TD, V> vd[4];
+        Vec<TX, V> vx[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            vd[j / J][j % J].load(dy + (i + j) * step_d);
-            vx[j / J][j % J].load(x + (i + j) * step_x);
+            vd[j].load(dy + (i + j) * step_d);
+            vx[j].load(x + (i + j) * step_x);
         }
 #pragma unroll
-        for (int j = 0; j < 4; j += J) {
-            two_f32 dz[J][N], d[J][N];
-            vector_dz<TD, TX, V, ACT, J>(P, t, ch, vd[j / J], vx[j / J], dz, d);
-#pragma unroll
-            for (int k = 0; k < J; ++k) use(i + j + k, dz[k], d[k]);
+        for (int j = 0; j < 4; ++j) {
+            vector_dz<TD, TX, V, ACT>(P, t, ch, vd[j], vx[j], dz, d);
+            use(i + j, dz, d);
         }
     }
-    pixel_by_pixel<TD, TX, V, ACT, J>(P, t, ch, i, end, [&](int k, Vec<TD, V> &vd, Vec<TX, V> &vx) { vd.load(dy + k * step_d); vx.load(x + k * step_x); }, use);
+    for (; i < end; ++i) {
+        Vec<TD, V> vd;
+        Vec<TX, V> vx;
+        vd.load(dy + i * step_d);
+        vx.load(x + i * step_x);
+        vector_dz<TD, TX, V, ACT>(P, t, ch, vd, vx, dz, d);
+        use(i, dz, d);
+    }
 }
 template <typename TD, typename TX, int V, int ACT>
 __device__ __forceinline__ void tile_sums(const GnBwd &P, const Tile<V> &t, two_f32 (&A)[Channels<V>::P], two_f32 (&D)[Channels<V>::P])

@@ -2,7 +2,6 @@
 import pytest
 import torch
 
-from paper_1605_04711_b200 import twn
 from test_gpu_group_norm import BF16, F32, bwd, fwd
 
 pytestmark = pytest.mark.gpu

@@ -3,7 +3,6 @@ import numpy as np
 import pytest
 import torch
 
-from paper_1605_04711_b200 import twn
 from test_gpu_group_norm import F32, K, U, bwd, fwd
 
 pytestmark = pytest.mark.gpu
