@@ -360,7 +360,7 @@ int twn_adamw_update_batch(const twn_adamw_item_t *items, int count, double lr, 
  * 0 has a code of 1 at least.  r, 16 bits, is the lower half (v: the upper half) of h(i + s), i the element's index in its tensor (of one past 2^32 the
  * upper part times 0x9E3779B9 is added), s = h(lo(seed) ^ h(hi(seed) ^ h(lo(t)))) of 32 bits, and
  *   h(x):  x ^= x >> 16;  x *= 0x7FEB352D;  x ^= x >> 15;  x *= 0x846CA68B;  x ^= x >> 16.
- * So seed and t fix every bit of the moments.  The weight's step, lr / c1 times the quotient, comes from a root and a reciprocal within 2^-23 each: within 2^-21 of it
+ * So seed and t fix every bit of the moments, whatever else a call updates; tensors of one seed are rounded with the same r at the same index.  The weight's step, lr / c1 times the quotient, comes from a root and a reciprocal within 2^-23 each: within 2^-21 of it
  * (a v below 2^-126 counts as 2^-126), and is added in one rounding.  A NaN, an infinity or a moment above 3.19e38 makes its block of that moment NaN.
  */
 typedef struct {
@@ -766,7 +766,7 @@ int twn_layer_norm_bwd(const void *dY, int32_t dy_dtype, int64_t lddy, const voi
  *                 contents need not be preserved or initialised.  One for B images serves fewer of them too.  Two calls that overlap on the device must not share it.
  *   What the call writes lies apart from all else that it reads or writes, but for Y in the place of X (else TWN_ERR_INVALID_ARG); rows of
  *   one buffer that lie between each other's are apart.
- *   1 <= C <= 2^20, C % groups = 0, eps >= 0, B and HW at most 2^31, B * HW at most 2^40.  B = 0 or HW = 0 is fine and launches nothing.
+ *   1 <= C <= 2^20, C % groups = 0, eps >= 0, B below 2^31, HW at most 2^31, B * HW at most 2^40.  B = 0 or HW = 0 is fine and launches nothing.
  * Arithmetic is fp32, each output rounded once.  The variance is that of differences, joined from parts with their means, never a difference of two
  * large sums.  SiLU takes z below -87 as -87, where it is -1.4e-36.  A group with a NaN or an infinity gives NaNs in that group of that image alone, a NaN in
  * gamma or beta in its channel; a NaN stays one through the activation.  With eps = 0 a group of equal values gives NaNs (0 * inf).  Deterministic; B, HW, C and

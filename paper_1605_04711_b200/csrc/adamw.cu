@@ -14,7 +14,7 @@
 // subnormals included, and the code is its upper bits: no conversion is needed in either direction.  E is the exponent of the block's largest value, one
 // more where rounding up would carry into the next, so no code ever overflows.
 // Roundings are stochastic: v moves by a thousandth of itself a step, a code by an eighth, and to nearest it would never move.  What is
-// added below the code are 16 bits of a hash of the weight's index, the seed and the count of steps.  A v that is not zero keeps a code that is not
+// added below the code are 16 bits of a hash of the weight's index in its tensor, the seed and the count of steps (the same for all tensors, which so do not depend on each other).  A v that is not zero keeps a code that is not
 // zero: m / (0 + eps) would be no step but a jump.
 #include <algorithm>
 #include <cmath>
@@ -62,7 +62,8 @@ struct Step {
     uint32_t key;
 };
 
-// A hash of 32 bits: two rounds of a shift, an exclusive or and a product, which flips every bit of its result with nearly even odds.
+// A hash of 32 bits: two rounds of a shift, an exclusive or and a product, which flips every bit of its result with nearly even odds.  Shifts and factors are those that Chris Wellons
+// found by search and published for anyone's use (2018).
 __device__ __forceinline__ uint32_t mix(uint32_t x)
 {
     x ^= x >> 16;

@@ -7,7 +7,7 @@ namespace {
 
 // Of n values of a group: their mean as it is in fp32, their sum less n times that, the sum of squares of their differences from the mean.  Parts are joined by the differences of their
 // means from one of those, which are no larger than what makes them differ: the group's mean keeps its digits however far from zero its values lie, and whichever of them is
-// far from the others.  (Sums in fp64 took as many digits and more time: four conversions a part, 80.2 us for 68.8 of 16 x 65536 x 24 fp32.)
+// far from the others.  (Sums in fp64 keep as many and took more time, four conversions a part: 7 x 1023 x 132 fp32 in 7.9 us for 7.1.)
 struct __align__(16) Moments {
     float c, r, m2, n;
 };
@@ -406,7 +406,7 @@ __device__ __forceinline__ void apply_tile(const GnFwd &P, const Tile<V> &t, con
     if (J > 1 && i < t.n) work(i, std::integral_constant<int, 1>());
 }
 
-// 64 x 12544 x 64 bf16 with a ReLU in 51 us, 4.0 TB/s: bound by latency.  Two blocks of 8 warps an SM issue on 40 % of the cycles, and half of what they issue joins sums; a
+// 64 x 12544 x 64 bf16 with a ReLU in 50 us, 4.1 TB/s: bound by latency.  Two blocks of 8 warps an SM issue on 39 % of the cycles, and half of what they issue joins sums; a
 // seventh of the SMs' room for warps is empty, as clusters of eight leave some and 128 of them are 3.5 rounds.
 // ---- resident -----------------------------------------------------------------------------------------------------------------
 template <typename TX, typename TY, int V>
@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_fwd_kernel(const __grid_cons
     }
 }
 
-// 131072 pixels of 512 channels, one group of 67 million values, in 122 us: three passes over 134 MB would take 61.
+// 131072 pixels of 512 channels, one group of 67 million values, in 121 us: three passes over 134 MB would take 61.
 // ---- two reads ----------------------------------------------------------------------------------------------------------------
 template <typename TX, int V>
 __global__ void __launch_bounds__(kGnThreads) gn_sums_kernel(const __grid_constant__ GnFwd P)

@@ -164,7 +164,7 @@ template <typename T> __device__ __forceinline__ T all_sum(T v, int lg)
 }
 
 // What the blocks of a cluster send each other, before they meet at its barrier.  (With an arrival on a barrier in the receiver's memory behind every store, each with a
-// fence of its own, 64 x 12544 x 64 took 61 us forward for 57.)
+// fence of its own, 64 x 12544 x 64 took 61 us forward for 57 at the time.)
 __device__ __forceinline__ void send(const void *own, int rank, float a)
 {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_smem(own, rank)), "f"(a) : "memory");
@@ -241,7 +241,7 @@ bool is_act(int a) { return a == TWN_ACT_NONE || a == TWN_ACT_RELU || a == TWN_A
 bool vectors_fit(int Cg, int V) { return std::lcm((long long)Cg, (long long)V) / V <= kGnThreads || Cg % V == 0; }
 
 // The widest vectors, of `most` elements or fewer, that C, the groups and the rows of all tensors (which rows(V) looks at) are made of.  (8 x 4096 pixels bf16 with SiLU: 924
-// channels in fours 49 us forward and 92 backward, 990 in twos 67 and 130, 1023 as single elements 86 and 179.)
+// channels in fours 49 us forward and 92 backward, 990 in twos 70 and 129, 1023 as single elements 87 and 170.)
 template <typename Rows> int widest(int most, int C, int Cg, Rows rows)
 {
     int V = most;
@@ -288,10 +288,10 @@ void finish_cut(Cut &k, int V)
 }
 
 // Slabs of a cluster: their data of `bytes` an element is resident in at most kMaxCluster blocks, beside beside(k) bytes of each.  False where they are not.
-// Two blocks an SM, and slabs whose pixels have 64 bytes of all tensors together (64 x 12544 x 64 bf16 forward 53.6 us, with 32 bytes 64.2; 64 x 3136 x 256 backward
-// 112 us with 32 of each tensor, 122 with 64); of 32 bytes of a tensor where that alone gives the SMs a block each, or leaves no more than a cluster holds.  Of small images a block has more channels,
-// up to 64 KB, as long as there is a block for each SM (64 x 49 x 512 bf16 5.1 us for 14.0, its backward pass 9.0 for 26.8; with a half of that least 64 x 784 x 512 took 34 us for 29, with
-// twice as much its backward pass 75 for 55).  Smaller tiles, three or
+// Two blocks an SM, and slabs whose pixels have 64 bytes of all tensors together (at the time 64 x 12544 x 64 bf16 forward 53.6 us, with 32 bytes 64.2; 64 x 3136 x 256
+// backward 112 us with 32 of each tensor, 122 with 64); of 32 bytes of a tensor where that alone gives the SMs a block each, or leaves no more than a cluster holds; where only the
+// first are held they stay.  Of small images a block has more channels, up to 64 KB, as long as there is a block for each SM (64 x 49 x 512 bf16 5.0 us for 14.0, its
+// backward pass 9.1 for 26.8; with a half of that least 64 x 784 x 512 took 34 us for 29, with twice as much its backward pass 75 for 55).  Smaller tiles, three or
 // four blocks an SM, took longer: what a block does beside its elements is half of its instructions.
 template <typename Beside> bool cut_resident(Cut &k, long long B, int V, int least_size, int bytes, Beside beside, size_t *smem)
 {
@@ -353,10 +353,11 @@ bool cut_streamed(Cut &k, long long B, int V)
         k.pieces = (k.Cg + k.slab - 1) / k.slab;
         k.slabs = k.G * k.pieces;
     }
-    // about eight blocks an SM, of eight pixels a thread at least
+    // about eight blocks an SM, of eight pixels a thread at least, and as many as there may be: where an image has many groups a slab,
+    // few images of them are fewer blocks than SMs (128 of one image of 32 groups)
     const int R = std::max(1, kGnThreads / (k.slab / V));
     const long long want = std::max(1ll, 8ll * kSms / (B * k.slabs)), most = std::max(1ll, k.HW / (8ll * R));
-    // (their sums are read by every block: sixteen of a thread at most, or 64 tiles)
+    // (their sums are read by every block: sixteen of a thread at most, or 64 tiles; not measured against more)
     const long long read = std::max(64ll, 16ll * kGnThreads / (std::max(1, k.slab / k.Cg) * k.pieces));
     k.tiles = (int)std::min(read, std::min(want, most));
     finish_cut(k, V);

@@ -155,7 +155,7 @@ __device__ __forceinline__ void vector_dz(const GnBwd &p, const Tile<V> &t, cons
         d[i] = add2(two(x[l], V > 1 ? x[h] : 0.0f), ch.m[i]);
         dz[i] = two(dy[l], V > 1 ? dy[h] : 0.0f);
         if (ACT == kSilu) {
-            // dy f (1 + z (1 - f)) = dy f (1 + z e f),  e = exp(-z), f = 1 / (1 + e).  (A reciprocal for two pixels, as the forward pass has it, takes more registers: 108 us for 104.)
+            // dy f (1 + z (1 - f)) = dy f (1 + z e f),  e = exp(-z), f = 1 / (1 + e).  (A reciprocal for two pixels, as the forward pass has it, takes more registers: 108 us for 105.)
             const two_f32 z[1] = {at_least2(fma2(d[i], ch.a[i], ch.b[i]), kLeastZ)};
             two_f32 e[1], f[1];
             sigmoids<1>(z, e, f);
@@ -356,10 +356,10 @@ __device__ __forceinline__ void write_dx(const Channels<V> &ch, const Terms<V> &
     store(to, o);
 }
 
-// 64 x 3136 x 256 bf16 with SiLU in 104 us, 3.0 TB/s: bound by instructions and their latency (54 % of the issue slots with 16 warps an SM, three quarters of them elementwise;
+// 64 x 3136 x 256 bf16 with SiLU in 105 us, 2.9 TB/s: bound by instructions and their latency (52 % of the issue slots with 16 warps an SM, three quarters of them elementwise;
 // exp and the reciprocal keep their unit at a third).
 // ---- resident -------------------------------------------------------------------------------------------------------------------
-// dz is taken anew for the outputs: to keep it in fp32 beside X costs half of the room for tiles (64 x 3136 x 256 with SiLU: 144 us, 118 this way).
+// dz is taken anew for the outputs: to keep it in fp32 beside X costs half of the room for tiles (64 x 3136 x 256 with SiLU: 144 us, 118 this way at the time).
 template <typename TD, typename TX, typename TO, int V, int ACT>
 __device__ __forceinline__ void resident(const GnBwd &P, const Tile<V> &t, const Raw<V> &raw, const OfChannel<V> &of, const Beside &at, const TD *ds, const TX *xs)
 {
@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_bwd_kernel(const __grid_cons
     else resident<TD, TX, TO, V, kNone>(P, t, raw, of, at, ds, xs);
 }
 
-// 131072 pixels of 512 channels, one group, in 175 us: five passes over 134 MB would take 102.
+// 131072 pixels of 512 channels, one group, in 152 us: five passes over 134 MB would take 102.  (Two blocks an SM, at 128 registers; with one, at 172, it took 176.)
 // ---- two reads ------------------------------------------------------------------------------------------------------------------
 // A thread's pixels from `i` to `end`, the loads of four at a time: use(i, dz, differences) for each.
 template <typename TD, typename TX, int V, int ACT, typename Use>
